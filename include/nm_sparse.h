@@ -506,6 +506,123 @@ typedef struct nm_layer_desc {
 int32_t nm_pack_prepare_batched(const nm_layer_desc* descs, int32_t count, void* stream);
 
 /*
+ * Between the linear layers of a transformer block (Section 3, "Problem Formulation": the four linears of a block are what
+ * carries an N:M level; these are the operators that stand between them).  Type codes of inputs are those of outputs:
+ * NM_OUT_F32 or NM_OUT_BF16.  Outputs must not overlap inputs unless a call says so.
+ *
+ * nm_layer_norm -- layer norm of each row, of the sum of two inputs where R is given:
+ *   s = x (+ r),  mean and variance over the C elements,  rstd = 1 / sqrt(variance + eps),  y = (s - mean) rstd w + b
+ *   X       in   [T, C], ld ldx, type x_dtype      R  in  [T, C], ld ldr, type of X, or NULL
+ *   weight, bias in  float [C], or NULL (1, 0)
+ *   Y       out  [T, C], ld ldy, type y_dtype
+ *   S       out  [T, C], ld lds, type of X: the sum, rounded once; NULL to skip; not used without R.  (Y is that of the sum
+ *                before it was rounded.)  May be the same matrix as R or as X (a residual stream kept in place).
+ *   stats   out  float [T, 2], 8-byte aligned: (mean, rstd) of each row, for the backward pass; NULL to skip
+ * All arithmetic is in 32-bit floats, the variance from the differences to the mean.
+ * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0, T above 2^31, C above 2^24, T * C above
+ * 2^40, a leading dimension smaller than its row, eps < 0 or NaN),
+ * NM_ERR_DTYPE, NM_ERR_ALIGN (element alignment), NM_ERR_DEVICE.
+ *
+ * nm_layer_norm_backward -- with n = (s - mean) rstd and g = dy w:
+ *   dx = rstd (g - mean(g) - n mean(g n)) (+ ds),  dw = sum over rows of dy n,  db = sum over rows of dy
+ *   dY      in   [T, C], ld lddy, type dy_dtype
+ *   S       in   [T, C], ld lds, type s_dtype: what was normalised (X, or the sum)
+ *   stats   in   as nm_layer_norm wrote them
+ *   weight  in   float [C] or NULL
+ *   dS      in   [T, C], ld ldds, type of dY, or NULL: the gradient that reaches the sum by its other use
+ *   dX      out  [T, C], ld lddx, type dx_dtype: the gradient of X (and of R)
+ *   dweight, dbias  out  float [C]; both NULL to skip them
+ *   workspace scratch of nm_layer_norm_backward_workspace_bytes(T, C) bytes, 256-byte aligned (sums over runs of rows, which
+ *                are added in a fixed order: results repeat bit for bit); NULL allowed when that size is 0 or dweight is
+ *                NULL.  Contents undefined afterwards; concurrent calls need distinct workspaces.
+ * Errors: as above, and NM_ERR_WORKSPACE.
+ * C % 8 == 0, 16-byte aligned matrices and leading dimensions that are multiples of 8 run with wide accesses.
+ */
+int32_t nm_layer_norm(const void* X, int64_t ldx, int32_t x_dtype, const void* R, int64_t ldr, int64_t T, int64_t C,
+                      const float* weight, const float* bias, float eps, void* Y, int64_t ldy, int32_t y_dtype, void* S,
+                      int64_t lds, float* stats, void* stream);
+size_t nm_layer_norm_backward_workspace_bytes(int64_t T, int64_t C);
+int32_t nm_layer_norm_backward(const void* dY, int64_t lddy, int32_t dy_dtype, const void* S, int64_t lds, int32_t s_dtype,
+                               const float* stats, const float* weight, const void* dS, int64_t ldds, int64_t T, int64_t C,
+                               void* dX, int64_t lddx, int32_t dx_dtype, float* dweight, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * nm_rotary -- rotary positions with one to four axes (one for text; height and width for an image; time too for a video).
+ * The first `rotated` elements of a head are pairs (i, i + rotated / 2), or (2 i, 2 i + 1) where interleaved != 0.  The pairs are
+ * divided among the axes in order, sections[x] of them to axis x; pair i of axis x is turned by positions[t, x] * freqs[i]:
+ *   (u, v) -> (u cos - v sin, v cos + u sin),   by the negative angle where inverse != 0 (the backward pass)
+ * The product that gives the angle is one of 32-bit floats.  Elements from `rotated` on are copied.
+ *   X  in   [T, H, D] of type x_dtype, elements of a head contiguous, x_token and x_head elements between tokens and heads
+ *   Y  out  the same with y_token, y_head and y_dtype; may be X itself (same type and strides)
+ *   positions  in  [T, axes] contiguous: int32 (positions_f32 == 0) or float
+ *   freqs   in   float [rotated / 2]        sections  HOST array of `axes` numbers >= 0 whose sum is rotated / 2
+ * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0 or above 2^31, H or D above 2^20, rotated odd, <= 0 or above D, axes outside [1, 4],
+ * a sum of sections other than rotated / 2, negative strides, tokens or heads of Y that overlap), NM_ERR_DTYPE, NM_ERR_ALIGN,
+ * NM_ERR_DEVICE.
+ */
+int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t D, int64_t x_token, int64_t x_head,
+                  const void* positions, int32_t positions_f32, const float* freqs, const int32_t* sections, int32_t axes,
+                  int64_t rotated, int32_t interleaved, int32_t inverse, void* Y, int32_t y_dtype, int64_t y_token,
+                  int64_t y_head, void* stream);
+
+/*
+ * nm_attention -- softmax attention over packed sequences.  Query head h reads key head h / (heads_q / heads_kv).  For query i
+ * of a sequence of Lq queries and Lk keys, over the keys j that it sees (all; causal: j <= i + Lk - Lq, so that the last query
+ * sees every key):
+ *   s_j = scale q_i . k_j,  lse_i = log sum_j exp(s_j),  o_i = sum_j exp(s_j - lse_i) v_j
+ * A query that sees no key (no keys, or Lq > Lk under the causal mask) gets o = 0 and lse = -infinity.
+ *   Q, O        [Tq, heads_q, head_size] bfloat16, K, V [Tk, heads_kv, head_size]; elements of a head contiguous, strides in
+ *               elements between tokens and heads (a view of a joint projection's output, or of a cache, is an input as it is).
+ *               head_size 1 .. 128.  K and V are not read where Tk = 0.
+ *   offsets_q   int32 [sequences + 1] on the device: sequence b holds tokens offsets_q[b] .. offsets_q[b + 1] - 1, from 0
+ *               to Tq, not decreasing.  NULL: one sequence.  offsets_k likewise for the keys.  (Offsets outside the tensors
+ *               are taken as their ends.  A token that no sequence holds is not computed.)
+ *   lengths_k   int32 [sequences] or NULL: keys of sequence b in use, from its offset on (a cache of fixed capacity).  Rows past
+ *               them are not read.
+ *   max_q, max_k  the longest sequences, as far as the caller knows: the launch is shaped for them.  Longer ones are computed
+ *               too, only later.
+ *   lse         out float [heads_q, Tq], or NULL
+ *   workspace   scratch of nm_attention_workspace_bytes() bytes, 256-byte aligned (few queries against many keys: the keys are
+ *               cut into chunks for different blocks, whose results a second launch joins); NULL allowed when that size is 0.
+ *               Contents undefined afterwards; concurrent calls need distinct workspaces.
+ * Scores, their maximum, sums and outputs are 32-bit floats; exp(s_j - ..) is rounded to bfloat16 as operand of the product with
+ * the values.  Values that a query does not see inside its sequence are multiplied by zero, so they have to be finite.
+ *
+ * nm_attention_backward -- the gradients, from the O and lse that nm_attention wrote and the same arguments otherwise:
+ *   p_ij = exp(s_ij - lse_i),  dS_ij = p_ij (dO_i . v_j - dO_i . o_i)
+ *   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i p_ij dO_i, the latter two summed over the
+ *   query heads that share the key head; keys past lengths_k get zeros.
+ *   workspace   nm_attention_backward_workspace_bytes() bytes, 256-byte aligned.
+ * Every sum is taken in a fixed order: results repeat bit for bit.
+ * Errors: NM_ERR_NULL, NM_ERR_SHAPE (Tq <= 0, Tk < 0, either above 2^30; sequences outside [1, 65535], heads_q no multiple of heads_kv,
+ * sequences * heads_q above 2^20, head_size outside [1, 128], max_q, max_k < 0, negative strides, tokens or heads of an output that
+ * overlap, scale not positive and finite), NM_ERR_ALIGN, NM_ERR_WORKSPACE, NM_ERR_DEVICE.
+ * head_size % 8 == 0, 16-byte aligned tensors and strides that are multiples of 8 run with wide accesses.
+ */
+typedef struct nm_heads {
+  nm_bf16* data;  /* inputs are only read */
+  int64_t token, head;
+} nm_heads;
+typedef struct nm_attention_desc {
+  nm_heads Q, K, V, O;
+  nm_heads dO, dQ, dK, dV;  /* nm_attention_backward only: dO in, the others out */
+  float* lse;               /* out; in of nm_attention_backward */
+  const int32_t* offsets_q;
+  const int32_t* offsets_k;
+  const int32_t* lengths_k;
+  int64_t Tq, Tk, max_q, max_k;
+  int32_t sequences, heads_q, heads_kv, head_size;
+  int32_t causal;
+  float scale;
+} nm_attention_desc;
+size_t nm_attention_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size,
+                                    int64_t max_q, int64_t max_k);
+int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+size_t nm_attention_backward_workspace_bytes(int64_t Tq, int32_t heads_q);
+int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aids -- no part of the layer and of no passage of the paper: the two rates the kernels above are
  * priced against, measured on the device at hand rather than taken from a data sheet.
  *   nm_probe_matrix_rate  a loop of nothing but matrix instructions on register operands, every compute unit

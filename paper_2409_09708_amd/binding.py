@@ -37,6 +37,8 @@ EXPORTS = (
     "nm_backward_weight_scratch_bytes", "nm_linear_backward_weight_scratch",
     "nm_linear_forward_prepared_batched", "nm_prepared_scratch_bytes", "nm_linear_forward_prepared_scratch",
     "nm_prepared_batched_scratch_bytes", "nm_linear_forward_prepared_batched_scratch", "nm_prune_scored", "nm_i8_workspace_bytes", "nm_linear_forward_i8", "nm_i8_prepare", "nm_linear_forward_i8_prepared",
+    "nm_layer_norm", "nm_layer_norm_backward_workspace_bytes", "nm_layer_norm_backward", "nm_rotary",
+    "nm_attention_workspace_bytes", "nm_attention", "nm_attention_backward_workspace_bytes", "nm_attention_backward",
 )
 
 
@@ -82,6 +84,18 @@ class ForwardDesc(ctypes.Structure):
                 ("M", c_int32), ("X", c_void_p), ("T", c_int64), ("ldx", c_int64), ("bias", c_void_p), ("Y", c_void_p),
                 ("ldy", c_int64), ("out_dtype", c_int32), ("reserved", c_int32), ("workspace", c_void_p),
                 ("workspace_bytes", c_size_t)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("token", c_int64), ("head", c_int64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(name, Heads) for name in ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV")] + [
+        ("lse", c_void_p), ("offsets_q", c_void_p), ("offsets_k", c_void_p), ("lengths_k", c_void_p),
+        ("Tq", c_int64), ("Tk", c_int64), ("max_q", c_int64), ("max_k", c_int64),
+        ("sequences", c_int32), ("heads_q", c_int32), ("heads_kv", c_int32), ("head_size", c_int32),
+        ("causal", c_int32), ("scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -227,6 +241,26 @@ def load_library() -> ctypes.CDLL:
     lib.nm_i8_prepare_packed.restype = c_int32
     lib.nm_i8_prepare_packed.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_int32, c_int32, c_int64, c_void_p, c_size_t,
                                          c_void_p]
+    lib.nm_layer_norm.restype = c_int32
+    lib.nm_layer_norm.argtypes = [c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p,
+                                  ctypes.c_float, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p, c_void_p]
+    lib.nm_layer_norm_backward_workspace_bytes.restype = c_size_t
+    lib.nm_layer_norm_backward_workspace_bytes.argtypes = [c_int64, c_int64]
+    lib.nm_layer_norm_backward.restype = c_int32
+    lib.nm_layer_norm_backward.argtypes = [c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p,
+                                           c_int64, c_int64, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p,
+                                           c_size_t, c_void_p]
+    lib.nm_rotary.restype = c_int32
+    lib.nm_rotary.argtypes = [c_void_p, c_int32, c_int64, c_int64, c_int64, c_int64, c_int64, c_void_p, c_int32, c_void_p,
+                              c_int32_p, c_int32, c_int64, c_int32, c_int32, c_void_p, c_int32, c_int64, c_int64, c_void_p]
+    lib.nm_attention_workspace_bytes.restype = c_size_t
+    lib.nm_attention_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32, c_int32, c_int64, c_int64]
+    lib.nm_attention.restype = c_int32
+    lib.nm_attention.argtypes = [ctypes.POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
+    lib.nm_attention_backward_workspace_bytes.restype = c_size_t
+    lib.nm_attention_backward_workspace_bytes.argtypes = [c_int64, c_int32]
+    lib.nm_attention_backward.restype = c_int32
+    lib.nm_attention_backward.argtypes = lib.nm_attention.argtypes
     _LIB = lib
     return lib
 
@@ -998,3 +1032,227 @@ def nm_spmm(values, indices, K: int, N: int, M: int, X, out_dtype=None, out=None
             from_packed=False):
     return nm_linear_forward(values, indices, K, N, M, X, None, out_dtype, out, workspace, stream,
                              from_packed=from_packed)
+
+
+# ------------------------------------------------------------------------------------------------
+# between the linear layers of a block
+# ------------------------------------------------------------------------------------------------
+def _typed(t, what: str, like=None) -> int:
+    """Type code of a float32 or bfloat16 device tensor (of `like`'s type, where one is given)."""
+    torch = _torch()
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError(f"{what} must be {like.dtype}, got {t.dtype}")
+    if t.dtype == torch.float32:
+        return NM_OUT_F32
+    if t.dtype == torch.bfloat16:
+        return NM_OUT_BF16
+    raise ValueError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _rows_of(t, what: str, rows: int, cols: int) -> int:
+    """Leading dimension of a [rows, cols] matrix."""
+    r, c, ld = _rows(t, what)
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{what} must be [{rows}, {cols}]")
+    return ld
+
+
+def nm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5, residual=None, train: bool = False, out_dtype=None, out=None,
+                  sum_out=None, stream=None):
+    """Layer norm of the rows of X [T, C] (float32 or bfloat16), of X + residual where one is given (type of X); weight and
+    bias are float32 [C].  Returns Y (float32 or bfloat16, default float32) -- with a residual (Y, S), S the sum in X's type
+    (sum_out, which may be the residual itself), and with train=True the rows' statistics [T, 2] behind them, which
+    nm_layer_norm_backward takes."""
+    torch = _torch()
+    code = _typed(X, "X")
+    T, C, ldx = _rows(X, "X")
+    Y, ldy, y_code = _out_matrix(out, out_dtype, T, C, X, "out")
+    r_ptr = s_ptr = stats_ptr = None
+    ldr = lds = C
+    result = (Y,)
+    if residual is not None:
+        _typed(residual, "residual", X)
+        ldr = _rows_of(residual, "residual", T, C)
+        r_ptr = residual.data_ptr()
+        if sum_out is None:
+            sum_out = X.new_empty((T, C))
+        _typed(sum_out, "sum_out", X)
+        lds = _rows_of(sum_out, "sum_out", T, C)
+        s_ptr = sum_out.data_ptr()
+        result += (sum_out,)
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    if train:
+        stats = X.new_empty((T, 2), dtype=torch.float32)
+        stats_ptr = stats.data_ptr()
+        result += (stats,)
+    _check(load_library().nm_layer_norm(X.data_ptr(), ldx, code, r_ptr, ldr, T, C, _per_feature(weight, C, "weight"),
+                                        _per_feature(bias, C, "bias"), eps, Y.data_ptr(), ldy, y_code, s_ptr, lds, stats_ptr,
+                                        _stream_handle(stream)))
+    return result if len(result) > 1 else Y
+
+
+def nm_layer_norm_backward(dY, S, stats, weight=None, dS=None, out_dtype=None, out=None, params: bool = True, workspace=None,
+                           stream=None):
+    """(dX, dweight, dbias) of nm_layer_norm from the gradient dY of its output, what was normalised (X, or the sum S) and its
+    statistics; dS (type of dY) is the gradient that reaches the sum by its other use and is added to dX.  dX is float32
+    (default) or bfloat16, dweight and dbias float32 [C], or None where params=False."""
+    torch = _torch()
+    dy_code, s_code = _typed(dY, "dY"), _typed(S, "S")
+    T, C, lddy = _rows(dY, "dY")
+    lds = _rows_of(S, "S", T, C)
+    _need(stats, torch.float32, "stats")
+    if stats.shape != (T, 2) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous [T, 2]")
+    ds_ptr, ldds = None, C
+    if dS is not None:
+        _typed(dS, "dS", dY)
+        ldds = _rows_of(dS, "dS", T, C)
+        ds_ptr = dS.data_ptr()
+    dX, lddx, dx_code = _out_matrix(out, out_dtype, T, C, dY, "dX")
+    lib = load_library()
+    dweight = dbias = None
+    if params:
+        dweight, dbias = (dY.new_empty((C,), dtype=torch.float32) for _ in range(2))
+        need = lib.nm_layer_norm_backward_workspace_bytes(T, C)
+        if workspace is None and need:
+            workspace = _workspace(need, dY.device, stream)
+    ws_ptr, ws_bytes = _scratch(workspace)
+    _check(lib.nm_layer_norm_backward(dY.data_ptr(), lddy, dy_code, S.data_ptr(), lds, s_code, stats.data_ptr(),
+                                      _per_feature(weight, C, "weight"), ds_ptr, ldds, T, C, dX.data_ptr(), lddx, dx_code,
+                                      dweight.data_ptr() if params else None, dbias.data_ptr() if params else None, ws_ptr,
+                                      ws_bytes, _stream_handle(stream)))
+    return dX, dweight, dbias
+
+
+def _head_strides(t, what: str, shape=None) -> Tuple[int, int]:
+    """(token, head) strides of a [tokens, heads, elements] tensor whose heads are contiguous."""
+    if len(t.shape) != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} must be [tokens, heads, elements]" if shape is None else f"{what} must be {list(shape)}")
+    token, head, step = t.stride()
+    if step != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what} must have contiguous heads")
+    return token, head
+
+
+def nm_rotary(X, positions, freqs, sections=None, interleaved: bool = False, inverse: bool = False, out_dtype=None, out=None,
+              stream=None):
+    """Rotary positions on X [T, H, D] (float32 or bfloat16; any strides between tokens and heads): pair i of the
+    2 * len(freqs) rotated elements of a head is turned by positions[t, axis of i] * freqs[i], its axis given by `sections`
+    (pairs per axis, in order; default: all on one axis).  positions are int32 or float32 [T, axes] ([T] for one), freqs
+    float32.  Pairs are (i, i + len(freqs)), or (2 i, 2 i + 1) with interleaved=True; inverse=True turns back, which is the
+    backward pass.  Y has X's type unless out_dtype says otherwise; out=X turns in place."""
+    torch = _torch()
+    code = _typed(X, "X")
+    token, head = _head_strides(X, "X")
+    T, H, D = X.shape
+    _need(freqs, torch.float32, "freqs")
+    if len(freqs.shape) != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be contiguous [pairs]")
+    pairs = freqs.shape[0]
+    sections = (pairs,) if sections is None else tuple(sections)
+    if positions.dtype != torch.int32:
+        _need(positions, torch.float32, "positions")
+    elif not positions.is_cuda:
+        raise ValueError("positions must be a device tensor")
+    if tuple(positions.shape) not in ((T, len(sections)),) + (((T,),) if len(sections) == 1 else ()) or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous [T, axes]")
+    if out is None:
+        out = X.new_empty((T, H, D), dtype=X.dtype if out_dtype is None else out_dtype)
+    y_code = _typed(out, "out")
+    y_token, y_head = _head_strides(out, "out", X.shape)
+    _check(load_library().nm_rotary(X.data_ptr(), code, T, H, D, token, head, positions.data_ptr(),
+                                    int(positions.dtype == torch.float32), freqs.data_ptr(), _ints(sections), len(sections),
+                                    2 * pairs, int(interleaved), int(inverse), out.data_ptr(), y_code, y_token, y_head,
+                                    _stream_handle(stream)))
+    return out
+
+
+def _heads(t, what: str, shape=None) -> Heads:
+    _need(t, _torch().bfloat16, what)
+    token, head = _head_strides(t, what, shape)
+    return Heads(t.data_ptr(), token, head)
+
+
+def _per_sequence(t, count: int, what: str):
+    """Device pointer of an optional int32 [count] tensor."""
+    if t is None:
+        return None
+    _need(t, _torch().int32, what)
+    if tuple(t.shape) != (count,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous [{count}]")
+    return t.data_ptr()
+
+
+def _attention_desc(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k) -> AttentionDesc:
+    d = AttentionDesc()
+    d.Q = _heads(Q, "Q")
+    Tq, Hq, D = Q.shape
+    d.K = _heads(K, "K")
+    Tk, Hkv, DK = K.shape
+    if DK != D:
+        raise ValueError("Q and K must have heads of one size")
+    d.V = _heads(V, "V", K.shape)
+    sequences = 1 if offsets_q is None else offsets_q.shape[0] - 1
+    if offsets_q is None and offsets_k is not None:
+        sequences = offsets_k.shape[0] - 1
+    d.offsets_q = _per_sequence(offsets_q, sequences + 1, "offsets_q")
+    d.offsets_k = _per_sequence(offsets_k, sequences + 1, "offsets_k")
+    d.lengths_k = _per_sequence(lengths_k, sequences, "lengths_k")
+    if sequences > 1 and (offsets_q is None or offsets_k is None):
+        raise ValueError("several sequences need offsets_q and offsets_k")
+    # (what the launch is shaped for where the caller does not say: sequences of one length)
+    d.max_q = max_q if max_q is not None else -(-Tq // max(sequences, 1))
+    d.max_k = max_k if max_k is not None else -(-Tk // max(sequences, 1))
+    d.Tq, d.Tk, d.sequences, d.heads_q, d.heads_kv, d.head_size = Tq, Tk, sequences, Hq, Hkv, D
+    d.causal = int(causal)
+    d.scale = D ** -0.5 if scale is None else scale
+    return d
+
+
+def nm_attention(Q, K, V, causal: bool = False, scale=None, offsets_q=None, offsets_k=None, lengths_k=None, max_q=None,
+                 max_k=None, lse: bool = False, out=None, workspace=None, stream=None):
+    """Softmax attention, bfloat16: O [Tq, heads, D] from Q [Tq, heads, D] and K, V [Tk, key heads, D] (any strides between
+    tokens and heads), scale 1 / sqrt(D) by default; (O, lse) with lse=True, lse float32 [heads, Tq].  Sequences are packed:
+    offsets_q and offsets_k (int32 [sequences + 1], from 0 to Tq and Tk) say where each begins, lengths_k how many of its keys are in use
+    (a cache of fixed capacity); none of them: one sequence.  Causal: a sequence's last query sees all its keys.  max_q and
+    max_k are the longest lengths as far as known: the launch is shaped for them."""
+    desc = _attention_desc(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k)
+    if out is None:
+        out = Q.new_empty(Q.shape)
+    desc.O = _heads(out, "out", Q.shape)
+    sums = None
+    if lse:
+        sums = Q.new_empty((desc.heads_q, desc.Tq), dtype=_torch().float32)
+        desc.lse = sums.data_ptr()
+    lib = load_library()
+    if workspace is None:
+        need = lib.nm_attention_workspace_bytes(desc.Tq, desc.sequences, desc.heads_q, desc.heads_kv, desc.head_size, desc.max_q,
+                                                min(desc.max_k, desc.Tk))
+        if need:
+            workspace = _workspace(need, Q.device, stream)
+    _check(lib.nm_attention(ctypes.byref(desc), *_scratch(workspace), _stream_handle(stream)))
+    return (out, sums) if lse else out
+
+
+def nm_attention_backward(dO, Q, K, V, O, lse, causal: bool = False, scale=None, offsets_q=None, offsets_k=None, lengths_k=None,
+                          max_q=None, max_k=None, out=None, workspace=None, stream=None):
+    """(dQ, dK, dV) of nm_attention, bfloat16 in the shapes of Q, K and V, from dO, the O and lse it returned and the same
+    arguments otherwise; gradients of a key head are sums over the query heads that share it.  out: the three tensors to
+    write (views of a joint projection's gradient, say)."""
+    torch = _torch()
+    desc = _attention_desc(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k)
+    desc.O, desc.dO = _heads(O, "O", Q.shape), _heads(dO, "dO", Q.shape)
+    _need(lse, torch.float32, "lse")
+    if tuple(lse.shape) != (desc.heads_q, desc.Tq) or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous [heads, Tq]")
+    desc.lse = lse.data_ptr()
+    dQ, dK, dV = out if out is not None else (Q.new_empty(Q.shape), K.new_empty(K.shape), V.new_empty(V.shape))
+    desc.dQ, desc.dK, desc.dV = _heads(dQ, "dQ", Q.shape), _heads(dK, "dK", K.shape), _heads(dV, "dV", K.shape)
+    lib = load_library()
+    if workspace is None:
+        workspace = _workspace(lib.nm_attention_backward_workspace_bytes(desc.Tq, desc.heads_q), Q.device, stream)
+    _check(lib.nm_attention_backward(ctypes.byref(desc), *_scratch(workspace), _stream_handle(stream)))
+    return dQ, dK, dV

@@ -537,6 +537,161 @@ int32_t nm_prune_scored(const float* score, int64_t O, int64_t K, int64_t lds, i
   return device_status(nm::launch_score_mask(score, O, K, lds, N, M, mask, (hipStream_t)stream));
 }
 
+namespace {
+constexpr int64_t kMost = (int64_t)1 << 31, kMostColumns = (int64_t)1 << 24;
+inline bool type_ok(int32_t t) { return t == NM_OUT_F32 || t == NM_OUT_BF16; }
+inline bool type_aligned(const void* p, int32_t t) { return aligned(p, t == NM_OUT_F32 ? 4 : 2); }
+inline bool workspace_ok(const void* p, size_t bytes, size_t need) { return need == 0 || (p && bytes >= need && aligned(p, 256)); }
+
+// rows of D elements at two strides: an input may repeat itself, an output's rows must not overlap
+inline bool strides_ok(int64_t T, int64_t H, int64_t D, int64_t token, int64_t head, bool output) {
+  if (token < 0 || head < 0) return false;
+  if (!output) return true;
+  if (T == 1 || H == 1) return (T == 1 || token >= D) && (H == 1 || head >= D);
+  // the heads of a token side by side (or those of all tokens, head after head)
+  return (head >= D && token >= (H - 1) * head + D) || (token >= D && head >= (T - 1) * token + D);
+}
+}  // namespace
+
+int32_t nm_layer_norm(const void* X, int64_t ldx, int32_t x_dtype, const void* R, int64_t ldr, int64_t T, int64_t C,
+                      const float* weight, const float* bias, float eps, void* Y, int64_t ldy, int32_t y_dtype, void* S,
+                      int64_t lds, float* stats, void* stream) {
+  if (!X || !Y) return NM_ERR_NULL;
+  if (T <= 0 || C <= 0 || T > kMost || C > kMostColumns || T * C > (int64_t)1 << 40) return NM_ERR_SHAPE;
+  const bool sum = R != nullptr && S != nullptr;
+  if (ldx < C || ldy < C || (R && ldr < C) || (sum && lds < C) || !(eps >= 0.f)) return NM_ERR_SHAPE;
+  if (!type_ok(x_dtype) || !type_ok(y_dtype)) return NM_ERR_DTYPE;
+  if (!type_aligned(X, x_dtype) || !type_aligned(R, x_dtype) || !type_aligned(S, x_dtype) || !type_aligned(Y, y_dtype) ||
+      !aligned(weight, 4) || !aligned(bias, 4) || !aligned(stats, 8))
+    return NM_ERR_ALIGN;
+  nm::NormCall c;
+  c.X = X; c.R = R; c.w = weight; c.b = bias; c.Y = Y; c.S = sum ? S : nullptr; c.stats = stats;
+  c.T = T; c.C = C; c.ldx = ldx; c.ldr = ldr; c.ldy = ldy; c.lds = lds; c.eps = eps;
+  c.x_f32 = x_dtype == NM_OUT_F32; c.y_f32 = y_dtype == NM_OUT_F32;
+  return device_status(nm::launch_norm(c, (hipStream_t)stream));
+}
+
+size_t nm_layer_norm_backward_workspace_bytes(int64_t T, int64_t C) {
+  if (T <= 0 || C <= 0 || T > kMost || C > kMostColumns) return 0;
+  return nm::norm_grad_workspace_bytes(T, C);
+}
+
+int32_t nm_layer_norm_backward(const void* dY, int64_t lddy, int32_t dy_dtype, const void* S, int64_t lds, int32_t s_dtype,
+                               const float* stats, const float* weight, const void* dS, int64_t ldds, int64_t T, int64_t C,
+                               void* dX, int64_t lddx, int32_t dx_dtype, float* dweight, float* dbias, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (!dY || !S || !stats || !dX || (dweight == nullptr) != (dbias == nullptr)) return NM_ERR_NULL;
+  if (T <= 0 || C <= 0 || T > kMost || C > kMostColumns || T * C > (int64_t)1 << 40) return NM_ERR_SHAPE;
+  if (lddy < C || lds < C || lddx < C || (dS && ldds < C)) return NM_ERR_SHAPE;
+  if (!type_ok(dy_dtype) || !type_ok(s_dtype) || !type_ok(dx_dtype)) return NM_ERR_DTYPE;
+  if (!type_aligned(dY, dy_dtype) || !type_aligned(dS, dy_dtype) || !type_aligned(S, s_dtype) || !type_aligned(dX, dx_dtype) ||
+      !aligned(stats, 8) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
+    return NM_ERR_ALIGN;
+  if (dweight && !workspace_ok(workspace, workspace_bytes, nm::norm_grad_workspace_bytes(T, C))) return NM_ERR_WORKSPACE;
+  nm::NormGradCall c;
+  c.dY = dY; c.S = S; c.stats = stats; c.w = weight; c.dS = dS; c.dX = dX; c.dw = dweight; c.db = dbias;
+  c.T = T; c.C = C; c.lddy = lddy; c.lds = lds; c.ldds = ldds; c.lddx = lddx;
+  c.dy_f32 = dy_dtype == NM_OUT_F32; c.s_f32 = s_dtype == NM_OUT_F32; c.dx_f32 = dx_dtype == NM_OUT_F32;
+  c.workspace = workspace;
+  return device_status(nm::launch_norm_grad(c, (hipStream_t)stream));
+}
+
+int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t D, int64_t x_token, int64_t x_head,
+                  const void* positions, int32_t positions_f32, const float* freqs, const int32_t* sections, int32_t axes,
+                  int64_t rotated, int32_t interleaved, int32_t inverse, void* Y, int32_t y_dtype, int64_t y_token,
+                  int64_t y_head, void* stream) {
+  if (!X || !Y || !positions || !freqs || !sections) return NM_ERR_NULL;
+  if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 1 << 20) return NM_ERR_SHAPE;
+  if (rotated <= 0 || rotated > D || rotated % 2 || axes < 1 || axes > nm::kMaxRotaryAxes) return NM_ERR_SHAPE;
+  if (!strides_ok(T, H, D, x_token, x_head, false) || !strides_ok(T, H, D, y_token, y_head, true)) return NM_ERR_SHAPE;
+  nm::RotaryCall c;
+  int64_t end = 0;
+  for (int x = 0; x < nm::kMaxRotaryAxes; ++x) {
+    if (x < axes && (sections[x] < 0 || sections[x] > rotated / 2)) return NM_ERR_SHAPE;
+    end += x < axes ? sections[x] : 0;
+    c.section_end[x] = x < axes - 1 ? (int)end : (int)(rotated / 2);
+  }
+  if (end != rotated / 2) return NM_ERR_SHAPE;
+  if (!type_ok(x_dtype) || !type_ok(y_dtype)) return NM_ERR_DTYPE;
+  if (!type_aligned(X, x_dtype) || !type_aligned(Y, y_dtype) || !aligned(positions, 4) || !aligned(freqs, 4)) return NM_ERR_ALIGN;
+  c.X = X; c.Y = Y; c.positions = positions; c.freqs = freqs;
+  c.T = T; c.H = H; c.D = D; c.R = rotated;
+  c.x_token = x_token; c.x_head = x_head; c.y_token = y_token; c.y_head = y_head;
+  c.axes = axes;
+  c.positions_f32 = positions_f32 != 0; c.interleaved = interleaved != 0; c.inverse = inverse != 0;
+  c.x_f32 = x_dtype == NM_OUT_F32; c.y_f32 = y_dtype == NM_OUT_F32;
+  return device_status(nm::launch_rotary(c, (hipStream_t)stream));
+}
+
+namespace {
+bool attention_sizes_ok(int64_t Tq, int64_t sequences, int64_t heads_q, int64_t heads_kv, int64_t head_size, int64_t max_q,
+                        int64_t max_k) {
+  return Tq > 0 && Tq <= (int64_t)1 << 30 && sequences >= 1 && sequences <= 65535 && heads_q >= 1 && heads_kv >= 1 &&
+         heads_q % heads_kv == 0 && sequences * heads_q <= 1 << 20 && head_size >= 1 && head_size <= 128 && max_q >= 0 && max_k >= 0;
+}
+
+int32_t attention_check(const nm_attention_desc* d, bool backward, nm::AttentionCall* c) {
+  if (!d) return NM_ERR_NULL;
+  const bool keys = d->Tk != 0;
+  if (!d->Q.data || !d->O.data || (keys && (!d->K.data || !d->V.data))) return NM_ERR_NULL;
+  if (backward && (!d->dO.data || !d->dQ.data || (keys && (!d->dK.data || !d->dV.data)) || !d->lse)) return NM_ERR_NULL;
+  if ((!d->offsets_q || !d->offsets_k) && d->sequences != 1) return d->sequences < 1 ? NM_ERR_SHAPE : NM_ERR_NULL;
+  if (!attention_sizes_ok(d->Tq, d->sequences, d->heads_q, d->heads_kv, d->head_size, d->max_q, d->max_k)) return NM_ERR_SHAPE;
+  if (d->Tk < 0 || d->Tk > (int64_t)1 << 30) return NM_ERR_SHAPE;
+  if (!(d->scale > 0.f) || d->scale > 3.0e38f) return NM_ERR_SHAPE;
+  auto take = [&](const nm_heads& h, nm::HeadRows* r, int64_t T, int64_t H, bool output) {
+    *r = nm::HeadRows{h.data, h.token, h.head};
+    return T == 0 || strides_ok(T, H, d->head_size, h.token, h.head, output);
+  };
+  *c = nm::AttentionCall{};
+  if (!take(d->Q, &c->Q, d->Tq, d->heads_q, false) || !take(d->K, &c->K, d->Tk, d->heads_kv, false) ||
+      !take(d->V, &c->V, d->Tk, d->heads_kv, false) || !take(d->O, &c->O, d->Tq, d->heads_q, !backward))
+    return NM_ERR_SHAPE;
+  if (backward && (!take(d->dO, &c->dO, d->Tq, d->heads_q, false) || !take(d->dQ, &c->dQ, d->Tq, d->heads_q, true) ||
+                   !take(d->dK, &c->dK, d->Tk, d->heads_kv, true) || !take(d->dV, &c->dV, d->Tk, d->heads_kv, true)))
+    return NM_ERR_SHAPE;
+  for (const void* p : {d->Q.data, d->K.data, d->V.data, d->O.data, c->dO.p, c->dQ.p, c->dK.p, c->dV.p})
+    if (!aligned(p, 2)) return NM_ERR_ALIGN;
+  for (const void* p : {(const void*)d->lse, (const void*)d->offsets_q, (const void*)d->offsets_k, (const void*)d->lengths_k})
+    if (!aligned(p, 4)) return NM_ERR_ALIGN;
+  c->lse = d->lse; c->offsets_q = d->offsets_q; c->offsets_k = d->offsets_k; c->lengths_k = d->lengths_k;
+  c->Tq = d->Tq; c->Tk = d->Tk;
+  c->B = d->sequences; c->Hq = d->heads_q; c->Hkv = d->heads_kv; c->D = d->head_size;
+  c->max_q = d->max_q < d->Tq ? d->max_q : d->Tq;
+  c->max_k = d->max_k < d->Tk ? d->max_k : d->Tk;
+  c->causal = d->causal != 0;
+  c->scale = d->scale;
+  return NM_OK;
+}
+}  // namespace
+
+size_t nm_attention_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size,
+                                    int64_t max_q, int64_t max_k) {
+  if (!attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, max_k)) return 0;
+  return nm::attention_workspace_bytes(Tq, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq, max_k);
+}
+
+int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
+  nm::AttentionCall c;
+  if (int32_t st = attention_check(desc, false, &c)) return st;
+  if (!workspace_ok(workspace, workspace_bytes, nm::attention_workspace_bytes(c.Tq, c.B, c.Hq, c.Hkv, c.D, c.max_q, c.max_k)))
+    return NM_ERR_WORKSPACE;
+  c.workspace = workspace;
+  return device_status(nm::launch_attention(c, (hipStream_t)stream));
+}
+
+size_t nm_attention_backward_workspace_bytes(int64_t Tq, int32_t heads_q) {
+  return Tq <= 0 || heads_q <= 0 ? 0 : nm::attention_grad_workspace_bytes(Tq, heads_q);
+}
+
+int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
+  nm::AttentionCall c;
+  if (int32_t st = attention_check(desc, true, &c)) return st;
+  if (!workspace_ok(workspace, workspace_bytes, nm::attention_grad_workspace_bytes(c.Tq, c.Hq))) return NM_ERR_WORKSPACE;
+  c.workspace = workspace;
+  return device_status(nm::launch_attention_grad(c, (hipStream_t)stream));
+}
+
 size_t nm_probe_sink_bytes(void) { return nm::probe_sink_bytes(); }
 
 int32_t nm_probe_matrix_rate(int32_t kind, int32_t iters, void* sink, int64_t* ops, void* stream) {

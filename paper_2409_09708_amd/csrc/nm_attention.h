@@ -1,0 +1,192 @@
+// What the attention kernels share: sequences, tiles of rows in LDS and the fragments that the 32 x 32 matrix instruction
+// takes from them.
+//
+// Scores are computed transposed, S^T = K Q^T (or S = Q K^T where the keys stay put), so that a lane holds values of one
+// column -- one query (one key) -- in the accumulator layout of v_mfma_f32_32x32x16_bf16: lane l has column l % 32, and its
+// register r row 8 (r / 4) + 4 (l / 32) + r % 4.  A softmax over the rows is then a reduction over the lane's own registers
+// and its partner 32 lanes away, and the probabilities are, rounded to bfloat16, already the second operand of the next
+// product: of a run of 16 rows the instruction wants 8 from each half of the wave, in any order that its first operand
+// shares, and registers 8 s .. 8 s + 7 are rows {0 .. 3, 8 .. 11} + 4 (l / 32) of run s.  The first operand is read in that
+// order by the transposing LDS read.
+#ifndef NM_ATTENTION_H
+#define NM_ATTENTION_H
+
+#include "nm_launch.h"
+#include "nm_mma.h"
+
+#include <type_traits>
+
+namespace nm {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_ptr;
+
+__device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// row of register r in the accumulator, without the lane's 4 (lane / 32)
+__host__ __device__ constexpr int acc_row(int r) { return 8 * (r / 4) + r % 4; }
+
+// The value of the lane 32 away, combined.
+__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+
+// exp2 of a difference: the hardware instruction, whose results below 2^-126 are zero
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kMinusInf = -__builtin_huge_valf();
+
+// Sequence b of a packed tensor: its first row and length.  Offsets are the caller's; whatever they hold, rows stay inside
+// the tensor.
+struct Span {
+  int64_t first;
+  int len;
+};
+__device__ __forceinline__ Span sequence(const int32_t* offsets, const int32_t* lengths, int b, int64_t total) {
+  int64_t lo = 0, hi = total;
+  if (offsets != nullptr) {
+    lo = offsets[b];
+    hi = offsets[b + 1];
+    lo = lo < 0 ? 0 : lo > total ? total : lo;
+    hi = hi < lo ? lo : hi > total ? total : hi;
+  }
+  int64_t len = hi - lo;
+  if (lengths != nullptr) {
+    const int64_t n = lengths[b];
+    len = n < 0 ? 0 : n < len ? n : len;
+  }
+  return {lo, (int)len};
+}
+
+// A tile of rows of DP bfloat16 in LDS.  The 16-byte pieces of a row are permuted so that both ways of reading it touch every
+// bank once: 16 rows at one piece (fragments of rows), and runs of four pieces from four rows (transposing reads).
+template <int DP>
+struct RowTile {
+  static constexpr int kRowBytes = DP * 2, kPieces = DP / 8;
+  static __host__ __device__ constexpr int swizzle(int row) {
+    return DP == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : DP == 64 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : (row >> 2) & 3;
+  }
+  static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ swizzle(row)) << 4); }
+
+  // rows row0 .. row0 + 31 (row0 a multiple of 32) as an operand: elements 16 step + 8 (lane / 32) .. + 7 of row lane % 32
+  static __device__ __forceinline__ u32x4_t rows(const unsigned char* tile, int row0, int step, int lane) {
+    return *reinterpret_cast<const u32x4_t*>(tile + row0 * kRowBytes + place(lane & 31, 2 * step + (lane >> 5)));
+  }
+  // columns 32 block .. + 31 of rows row0 .. row0 + 15 (row0 a multiple of 16) as the first operand, rows in the order
+  // {0 .. 3, 8 .. 11} + 4 (lane / 32)
+  static __device__ __forceinline__ u32x4_t columns(const unsigned char* tile, int row0, int block, int lane) {
+    const int row = 4 * (lane >> 5) + ((lane >> 2) & 3);
+    const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    const unsigned char* at = tile + row0 * kRowBytes + (lane & 1) * 8;
+    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + place(row, piece)));
+    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + place(row + 8, piece)));
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    const u32x2_t l = __builtin_bit_cast(u32x2_t, lo), h = __builtin_bit_cast(u32x2_t, hi);
+    return u32x4_t{l[0], l[1], h[0], h[1]};
+  }
+};
+
+// Eight elements of a row, zeros past element D or where `there` is false.  ALIGNED: rows are whole 16-byte pieces.
+template <bool ALIGNED>
+__device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, bool there) {
+  u32x4_t v = {0, 0, 0, 0};
+  if constexpr (ALIGNED) {
+    if (there && d < D) v = *reinterpret_cast<const u32x4_t*>(row + d);
+  } else if (there) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (d + e < D) v[e / 2] |= (uint32_t)row[d + e] << (16 * (e & 1));
+  }
+  return v;
+}
+
+// probabilities (registers 8 s .. 8 s + 7 of an accumulator) as an operand
+__device__ __forceinline__ u32x4_t acc_operand(const f32x16_t& p, int s) {
+  return u32x4_t{pack_bf16x2(p[8 * s], p[8 * s + 1]), pack_bf16x2(p[8 * s + 2], p[8 * s + 3]),
+                 pack_bf16x2(p[8 * s + 4], p[8 * s + 5]), pack_bf16x2(p[8 * s + 6], p[8 * s + 7])};
+}
+
+// One column of a transposed product (DP / 32 accumulators: the elements of one row of the output) to memory, times `by`.
+template <int DP, bool ALIGNED>
+__device__ __forceinline__ void store_column(bf16_t* row, const f32x16_t (&acc)[DP / 32], int lane, int D, float by) {
+  const int h = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int d = 32 * b + 8 * q + 4 * h;
+      const uint32_t lo = pack_bf16x2(acc[b][4 * q] * by, acc[b][4 * q + 1] * by);
+      const uint32_t hi = pack_bf16x2(acc[b][4 * q + 2] * by, acc[b][4 * q + 3] * by);
+      if constexpr (ALIGNED) {
+        if (d < D) *reinterpret_cast<uint2*>(row + d) = uint2{lo, hi};
+      } else {
+        if (d < D) row[d] = (bf16_t)lo;
+        if (d + 1 < D) row[d + 1] = (bf16_t)(lo >> 16);
+        if (d + 2 < D) row[d + 2] = (bf16_t)hi;
+        if (d + 3 < D) row[d + 3] = (bf16_t)(hi >> 16);
+      }
+    }
+}
+
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+
+// Scores of the rows from `limit` on (relative to the lane's first row, 4 (lane / 32)) are not seen.
+__device__ __forceinline__ void hide_rows(f32x16_t& s, int limit) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = acc_row(r) < limit ? s[r] : kMinusInf;
+}
+
+// Block -> (sequence, key head, head of its group, tile).  Consecutive blocks go to consecutive XCDs, each with an L2
+// of its own.  Where a head has many tiles, XCD x takes tiles x, x + 8, ... of one key head after another, so that at any time
+// an L2 holds the keys of about one head, and the longest tiles of a causal mask come first (the last queries: `last_first`; the
+// first keys).  Where a head has few tiles, XCD x takes all tiles of every eighth key head.
+constexpr int kManyTiles = 16;
+struct TilePlace {
+  int seq, kv_head, sub, tile;
+};
+__device__ __forceinline__ bool tile_place(int sequences, int kv_heads, int group, int n_tiles, bool last_first, TilePlace* p) {
+  const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  int unit, t;
+  if (n_tiles >= kManyTiles) {
+    const int per_unit = (n_tiles + 7) / 8 * group;
+    unit = slot / per_unit;
+    t = slot % per_unit / group * 8 + xcd;
+    p->sub = slot % per_unit % group;
+    if (t >= n_tiles) return false;
+  } else {
+    const int per_unit = n_tiles * group;
+    unit = slot / per_unit * 8 + xcd;
+    t = slot % per_unit / group;
+    p->sub = slot % per_unit % group;
+  }
+  if (unit >= sequences * kv_heads) return false;
+  p->seq = unit / kv_heads;
+  p->kv_head = unit % kv_heads;
+  p->tile = last_first ? n_tiles - 1 - t : t;
+  return true;
+}
+inline int64_t tile_blocks(int sequences, int kv_heads, int group, int n_tiles) {
+  const int64_t units = (int64_t)sequences * kv_heads;
+  if (n_tiles >= kManyTiles) return units * ((n_tiles + 7) / 8) * group * 8;
+  return (units + 7) / 8 * n_tiles * group * 8;
+}
+
+// A launch holds fewer than 2^32 lanes, 2^24 blocks of 256.
+constexpr int64_t kMostBlocks = (int64_t)1 << 24;
+
+constexpr int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
+
+template <bool ALIGNED, class F>
+void with_head(int D, F&& f) {
+  if (D <= 32) f(std::integral_constant<int, 32>{}, std::bool_constant<ALIGNED>{});
+  else if (D <= 64) f(std::integral_constant<int, 64>{}, std::bool_constant<ALIGNED>{});
+  else f(std::integral_constant<int, 128>{}, std::bool_constant<ALIGNED>{});
+}
+
+inline bool head_rows_aligned(const HeadRows& r) { return ((uintptr_t)r.p & 15) == 0 && (r.token | r.head) % 8 == 0; }
+
+}  // namespace nm
+
+#endif  // NM_ATTENTION_H

@@ -1,0 +1,438 @@
+// Softmax attention over packed sequences, grouped heads, causal or not.  For query i of a sequence of Lq queries and Lk keys
+// and each of the query heads that share key head h
+//
+//   s_j = scale q_i . k_j for the keys it sees (all, or j <= i + Lk - Lq),  o_i = sum_j exp(s_j - lse_i) v_j,
+//   lse_i = log sum_j exp(s_j);   a query that sees no key gets o_i = 0 and lse_i = -infinity.
+//
+// One pass over the keys with a running maximum and sum; scores, maximum, sum and output are 32-bit floats, the
+// probabilities are rounded to bfloat16 as operands of the second product (as the values are; the sum takes them unrounded).
+//
+// Two kernels.  prompt_kernel: a block of four waves takes 128 queries of one head, 32 to a wave, and walks over the keys 64
+// at a time, staged in LDS for its waves.  cache_kernel, where queries are few: its columns are the (query, head of the
+// group) pairs that share a key head, its waves walk over different keys, and keys are cut into chunks for different blocks;
+// what they leave (output, maximum, sum) a second launch joins in order.
+#include "nm_attention.h"
+
+namespace nm {
+
+namespace {
+
+struct AttnArgs {
+  AttentionCall c;
+  int group;          // Hq / Hkv
+  float scale_log2;   // scale * log2(e)
+  int n_tiles;        // prompt: query tiles the grid has per head
+  int chunk;          // cache: keys per block
+  int n_chunks, n_row_tiles;
+  float* part_o;      // cache: [column][chunk][DP], column = query * Hq + head
+  float2* part_ml;    // [column][chunk]: (maximum of the scaled scores in the exponent's base 2, sum)
+};
+
+// A column's running maximum and sum.  The reference that exponentials are taken against only follows the maximum when that
+// has grown by more than kSlack powers of two: sums and products of values up to 2^kSlack are as exact, and the
+// accumulators are rescaled a few times per row instead of once per tile.
+constexpr float kSlack = 8.f;
+
+// One tile of scores (KB accumulators of 32 keys) into the running softmax of a column: on return s holds the probabilities
+// against `ref` (scaled, base 2; -infinity: nothing seen yet), `sum` is this lane's share.
+template <int KB, int NB>
+__device__ __forceinline__ void softmax_step(f32x16_t (&s)[KB], float c, float& ref, float& sum, f32x16_t (&acc)[NB]) {
+  float top = s[0][0];
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
+  top = half_max(top) * c;
+  if (__any(top > ref + kSlack)) {  // (also where nothing has been seen yet: ref is -infinity)
+    const float next = fmaxf(top, ref);
+    const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - next);
+    ref = next;
+    sum *= by;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] *= by;
+  }
+  const float base = ref == kMinusInf ? 0.f : ref;
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[k][r] = fast_exp2(fmaf(s[k][r], c, -base));
+      sum += s[k][r];
+    }
+}
+
+constexpr int kKeys = 64;             // per tile
+constexpr int kQueries = kWaves * 32; // per block
+
+template <int DP, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
+  using Tile = RowTile<DP>;
+  constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
+  constexpr int LOADS = kKeys * Tile::kPieces / kThreads;  // pieces of a tile per lane
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of keys and values
+  TilePlace at;
+  if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_tiles, true, &at)) return;
+  const int kv_head = at.kv_head, head = kv_head * a.group + at.sub, seq = at.seq;
+  const int D = a.c.D;
+  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
+  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5;
+  const int shift = sk.len - sq.len;  // causal: query i sees keys up to i + shift
+  const bf16_t* Kh = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
+  const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+
+  for (int tile = at.tile; (int64_t)tile * kQueries < sq.len; tile += a.n_tiles) {
+    const int q_wave = tile * kQueries + wave * 32;
+    const int qi = q_wave + (lane & 31);
+    const bool live = qi < sq.len;
+    const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
+    u32x4_t q[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece<ALIGNED>(q_row, 16 * st + 8 * half, D, live);
+
+    // keys that any query of the block, of the wave, and this lane's sees
+    const int last_q = (tile + 1) * kQueries < sq.len ? (tile + 1) * kQueries : sq.len;
+    int end = sk.len, wave_end = sk.len, first_hidden = sk.len, limit = sk.len;
+    if (a.c.causal) {
+      auto upto = [&](int i) { const int n = i + shift + 1; return n < 0 ? 0 : n < sk.len ? n : sk.len; };
+      end = upto(last_q - 1);
+      wave_end = upto(q_wave + 31 < last_q ? q_wave + 31 : last_q - 1);
+      first_hidden = upto(q_wave);
+      limit = upto(qi);
+    }
+    if (q_wave >= sq.len) wave_end = 0;
+
+    f32x16_t acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+    float ref = kMinusInf, sum = 0.f;
+
+    u32x4_t k_in[LOADS], v_in[LOADS];
+    auto fetch = [&](int k0) {
+#pragma unroll
+      for (int n = 0; n < LOADS; ++n) {
+        const int i = n * kThreads + tid, row = k0 + i / Tile::kPieces, d = i % Tile::kPieces * 8;
+        const bool there = row < sk.len;
+        k_in[n] = load_piece<ALIGNED>(Kh + (int64_t)row * a.c.K.token, d, D, there);
+        v_in[n] = load_piece<ALIGNED>(Vh + (int64_t)row * a.c.V.token, d, D, there);
+      }
+    };
+    auto settle = [&](int stage) {
+#pragma unroll
+      for (int n = 0; n < LOADS; ++n) {
+        const int i = n * kThreads + tid, at = Tile::place(i / Tile::kPieces, i % Tile::kPieces);
+        *reinterpret_cast<u32x4_t*>(smem[stage] + at) = k_in[n];
+        *reinterpret_cast<u32x4_t*>(smem[stage] + TILE_BYTES + at) = v_in[n];
+      }
+    };
+    const int n_key_tiles = (end + kKeys - 1) / kKeys;
+    __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
+    if (n_key_tiles > 0) {
+      fetch(0);
+      settle(0);
+    }
+    __syncthreads();
+    for (int kt = 0; kt < n_key_tiles; ++kt) {
+      const int k0 = kt * kKeys;
+      if (kt + 1 < n_key_tiles) fetch(k0 + kKeys);
+      const unsigned char* k_tile = smem[kt & 1];
+      const unsigned char* v_tile = k_tile + TILE_BYTES;
+      if (k0 < wave_end) {
+        f32x16_t s[kKeys / 32];
+#pragma unroll
+        for (int kb = 0; kb < kKeys / 32; ++kb) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+          for (int st = 0; st < STEPS; ++st) s[kb] = mma32(Tile::rows(k_tile, 32 * kb, st, lane), q[st], s[kb]);
+        }
+        if (k0 + kKeys > first_hidden) {
+#pragma unroll
+          for (int kb = 0; kb < kKeys / 32; ++kb) hide_rows(s[kb], limit - k0 - 32 * kb - 4 * half);
+        }
+        softmax_step(s, a.scale_log2, ref, sum, acc);
+#pragma unroll
+        for (int st = 0; st < kKeys / 16; ++st) {
+          const u32x4_t p = acc_operand(s[st / 2], st % 2);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(v_tile, 16 * st, b, lane), p, acc[b]);
+        }
+      }
+      if (kt + 1 < n_key_tiles) settle((kt + 1) & 1);
+      __syncthreads();
+    }
+    sum = half_sum(sum);
+    if (live) {
+      bf16_t* o_row = a.c.O.p + (sq.first + qi) * a.c.O.token + head * a.c.O.head;
+      store_column<DP, ALIGNED>(o_row, acc, lane, D, sum == 0.f ? 0.f : 1.f / sum);
+      if (a.c.lse != nullptr && half == 0)
+        a.c.lse[(int64_t)head * a.c.Tq + sq.first + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
+    }
+  }
+}
+
+// Few queries.  Column n of a row tile is query (32 tile + n) / group of the sequence and head (32 tile + n) % group of the
+// key head's group.  Each wave takes every fourth run of 32 keys of the block's chunk through LDS of its own.
+template <int DP, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
+  using Tile = RowTile<DP>;
+  constexpr int NB = DP / 32, STEPS = DP / 16, RUN = 32, TILE_BYTES = RUN * Tile::kRowBytes;
+  constexpr int LOADS = RUN * Tile::kPieces / 64;
+  constexpr int JOIN = 32 * (DP + 4) * 4;  // one wave's output, columns padded against bank conflicts
+  constexpr int OWN = 2 * TILE_BYTES;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * (OWN > JOIN ? OWN : JOIN)];
+  __shared__ float2 wave_ml[kWaves][32];
+  int place = blockIdx.x;
+  const int chunk = place % a.n_chunks;
+  place /= a.n_chunks;
+  const int row_tile0 = place % a.n_row_tiles;
+  place /= a.n_row_tiles;
+  const int kv_head = place % a.c.Hkv, seq = place / a.c.Hkv;
+  const int D = a.c.D;
+  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
+  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int shift = sk.len - sq.len;
+  // the chunks of this sequence: as many as its keys need, the last block of a too short grid takes what is left
+  const int first_key = chunk * a.chunk;
+  const int end_key = chunk == a.n_chunks - 1 || first_key + a.chunk > sk.len ? sk.len : first_key + a.chunk;
+  const bool alone = a.n_chunks == 1;
+  if (!alone && first_key >= sk.len && chunk > 0) return;  // (the first chunk reports where no key is seen)
+  const bf16_t* Kh = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
+  const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+  const int64_t columns = (int64_t)sq.len * a.group;
+  unsigned char* own = smem + wave * OWN;
+
+  for (int row_tile = row_tile0; (int64_t)row_tile * 32 < columns; row_tile += a.n_row_tiles) {
+    const int64_t n = (int64_t)row_tile * 32 + col;
+    const bool live = n < columns;
+    const int qi = (int)(n / a.group), head = kv_head * a.group + (int)(n % a.group);
+    const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
+    u32x4_t q[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece<ALIGNED>(q_row, 16 * st + 8 * half, D, live);
+    int limit = end_key, first_hidden = end_key;
+    if (a.c.causal) {
+      const int sees = qi + shift + 1, first_sees = row_tile * 32 / a.group + shift + 1;
+      limit = sees < end_key ? sees : end_key;
+      first_hidden = first_sees < end_key ? first_sees : end_key;
+    }
+    f32x16_t acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+    float ref = kMinusInf, sum = 0.f;
+    u32x4_t k_in[LOADS], v_in[LOADS];
+    auto fetch = [&](int k0) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int at = i * 64 + lane, row = k0 + at / Tile::kPieces, d = at % Tile::kPieces * 8;
+        k_in[i] = load_piece<ALIGNED>(Kh + (int64_t)row * a.c.K.token, d, D, row < end_key);
+        v_in[i] = load_piece<ALIGNED>(Vh + (int64_t)row * a.c.V.token, d, D, row < end_key);
+      }
+    };
+    __syncthreads();  // (a further row tile: what the waves joined has been read)
+    int k0 = first_key + wave * RUN;
+    if (k0 < end_key) fetch(k0);
+    for (; k0 < end_key; k0 += kWaves * RUN) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int at = i * 64 + lane, to = Tile::place(at / Tile::kPieces, at % Tile::kPieces);
+        *reinterpret_cast<u32x4_t*>(own + to) = k_in[i];
+        *reinterpret_cast<u32x4_t*>(own + TILE_BYTES + to) = v_in[i];
+      }
+      if (k0 + kWaves * RUN < end_key) fetch(k0 + kWaves * RUN);
+      __builtin_amdgcn_wave_barrier();
+      f32x16_t s[1];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) s[0] = mma32(Tile::rows(own, 0, st, lane), q[st], s[0]);
+      if (k0 + RUN > first_hidden) hide_rows(s[0], limit - k0 - 4 * half);
+      softmax_step(s, a.scale_log2, ref, sum, acc);
+#pragma unroll
+      for (int st = 0; st < RUN / 16; ++st) {
+        const u32x4_t p = acc_operand(s[0], st);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(own + TILE_BYTES, 16 * st, b, lane), p, acc[b]);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
+    sum = half_sum(sum);
+    if (half == 0) wave_ml[wave][col] = float2{ref, sum};
+    __syncthreads();
+    float top = kMinusInf, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_ml[w][col].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      total += wave_ml[w][col].x == kMinusInf ? 0.f : wave_ml[w][col].y * fast_exp2(wave_ml[w][col].x - top);
+    const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - top);
+    float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4*>(joined + col * (DP + 4) + 32 * b + acc_row(r) + 4 * half) =
+            float4{acc[b][r] * by, acc[b][r + 1] * by, acc[b][r + 2] * by, acc[b][r + 3] * by};
+    __syncthreads();
+    // lane -> (column, four elements)
+    constexpr int PER_COL = DP / 4;
+#pragma unroll
+    for (int i = 0; i < 32 * PER_COL / kThreads; ++i) {
+      const int at = i * kThreads + tid, c = at / PER_COL, d = at % PER_COL * 4;
+      const int64_t cn = (int64_t)row_tile * 32 + c;
+      if (cn >= columns || d >= D) continue;
+      const float* from = reinterpret_cast<const float*>(smem) + c * (DP + 4) + d;
+      float4 o = *reinterpret_cast<const float4*>(from);
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(from + w * 32 * (DP + 4));
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+      }
+      const int64_t tok = sq.first + cn / a.group;
+      const int hd = kv_head * a.group + (int)(cn % a.group);
+      if (alone) {
+        float t = kMinusInf, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) t = fmaxf(t, wave_ml[w][c].x);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].x == kMinusInf ? 0.f : wave_ml[w][c].y * fast_exp2(wave_ml[w][c].x - t);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16_t* out = a.c.O.p + tok * a.c.O.token + hd * a.c.O.head + d;
+        const uint32_t lo = pack_bf16x2(o.x * inv, o.y * inv), hi = pack_bf16x2(o.z * inv, o.w * inv);
+        if constexpr (ALIGNED) {
+          *reinterpret_cast<uint2*>(out) = uint2{lo, hi};
+        } else {
+          out[0] = (bf16_t)lo;
+          if (d + 1 < D) out[1] = (bf16_t)(lo >> 16);
+          if (d + 2 < D) out[2] = (bf16_t)hi;
+          if (d + 3 < D) out[3] = (bf16_t)(hi >> 16);
+        }
+      } else {
+        *reinterpret_cast<float4*>(a.part_o + ((tok * a.c.Hq + hd) * a.n_chunks + chunk) * DP + d) = o;
+      }
+    }
+    if (wave == 0 && half == 0 && live) {
+      const int64_t tok = sq.first + qi;
+      if (!alone) a.part_ml[(tok * a.c.Hq + head) * a.n_chunks + chunk] = float2{top, total};
+      else if (a.c.lse != nullptr)
+        a.c.lse[(int64_t)head * a.c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
+    }
+  }
+}
+
+// Joins the chunks of a column: a wave per (query, head), lanes along its elements.
+template <int DP>
+__global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t n = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);  // query * Hq + head
+  const int seq = blockIdx.y;
+  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
+  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const int used = (sk.len + a.chunk - 1) / a.chunk;
+  const int chunks = used < 1 ? 1 : used < a.n_chunks ? used : a.n_chunks;
+  for (int64_t i = n; i < (int64_t)sq.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
+    const int64_t tok = sq.first + i / a.c.Hq;
+    const int head = (int)(i % a.c.Hq);
+    const int64_t at = (tok * a.c.Hq + head) * a.n_chunks;
+    float top = kMinusInf;
+    for (int k = lane; k < chunks; k += 64) top = fmaxf(top, a.part_ml[at + k].x);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+    float total = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int k = 0; k < chunks; ++k) {
+      const float2 ml = a.part_ml[at + k];
+      const float by = ml.x == kMinusInf ? 0.f : fast_exp2(ml.x - top);
+      total += ml.y * by;
+      const float* o = a.part_o + (at + k) * DP;
+      if (lane < a.c.D) o0 = fmaf(o[lane], by, o0);
+      if (DP > 64 && lane + 64 < a.c.D) o1 = fmaf(o[lane + 64], by, o1);
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    bf16_t* out = a.c.O.p + tok * a.c.O.token + head * a.c.O.head;
+    if (lane < a.c.D) out[lane] = (bf16_t)f32_to_bf16_rne(o0 * inv);
+    if (DP > 64 && lane + 64 < a.c.D) out[lane + 64] = (bf16_t)f32_to_bf16_rne(o1 * inv);
+    if (a.c.lse != nullptr && lane == 0)
+      a.c.lse[(int64_t)head * a.c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
+  }
+}
+
+// How a call is cut: few queries per key head take the cache kernel.
+constexpr int64_t kFewColumns = 128;
+struct CachePlan {
+  bool taken;
+  int chunk, n_chunks, n_row_tiles;
+};
+CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
+  CachePlan p = {};
+  p.taken = max_q * group <= kFewColumns;
+  if (!p.taken) return p;
+  p.n_row_tiles = (int)((max_q * group + 31) / 32);
+  // chunks so that there are about eight blocks to a compute unit (sequences differ in length), of 256 keys at least
+  const int64_t blocks = (int64_t)B * Hkv * p.n_row_tiles, target = 2048;
+  int64_t chunk = (max_k * blocks + target - 1) / target;
+  chunk = (chunk < 256 ? 256 : chunk + 127) / 128 * 128;
+  p.chunk = (int)chunk;
+  p.n_chunks = (int)((max_k + chunk - 1) / chunk);
+  if (p.n_chunks < 1) p.n_chunks = 1;
+  return p;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k) {
+  const CachePlan p = cache_plan(B, Hkv, Hq / Hkv, max_q, max_k);
+  if (!p.taken || p.n_chunks == 1) return 0;
+  const size_t columns = (size_t)Tq * Hq * p.n_chunks;
+  return round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2);
+}
+
+hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
+  AttnArgs a = {};
+  a.c = c;
+  a.group = c.Hq / c.Hkv;
+  a.scale_log2 = c.scale * kLog2e;
+  const bool aligned = c.D % 8 == 0 && head_rows_aligned(c.Q) && head_rows_aligned(c.K) && head_rows_aligned(c.V) &&
+                       head_rows_aligned(c.O);
+  const CachePlan plan = cache_plan(c.B, c.Hkv, a.group, c.max_q, c.max_k);
+  a.chunk = plan.chunk; a.n_chunks = plan.n_chunks; a.n_row_tiles = plan.n_row_tiles;
+  a.n_tiles = (int)((c.max_q + kQueries - 1) / kQueries);
+  if (a.n_tiles < 1) a.n_tiles = 1;
+  while (tile_blocks(c.B, c.Hkv, a.group, a.n_tiles) >= kMostBlocks) a.n_tiles = (a.n_tiles + 1) / 2;  // (blocks take several then)
+  if (plan.n_chunks > 1) {
+    a.part_o = static_cast<float*>(c.workspace);
+    const size_t columns = (size_t)c.Tq * c.Hq * plan.n_chunks;
+    a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) +
+                                          round256(columns * padded_head(c.D) * sizeof(float)));
+  }
+  auto launch = [&](auto dp, auto al) {
+    constexpr int DP = decltype(dp)::value;
+    constexpr bool ALIGNED = decltype(al)::value;
+    if (plan.taken) {
+      const int64_t blocks = (int64_t)a.n_chunks * a.n_row_tiles * c.B * c.Hkv;
+      cache_kernel<DP, ALIGNED><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
+      if (a.n_chunks > 1) {
+        const dim3 join((unsigned)((c.max_q * c.Hq + kWaves - 1) / kWaves), (unsigned)c.B);
+        cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
+      }
+    } else {
+      prompt_kernel<DP, ALIGNED><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
+    }
+  };
+  if (aligned) with_head<true>(c.D, launch);
+  else with_head<false>(c.D, launch);
+  return hipGetLastError();
+}
+
+}  // namespace nm

@@ -232,4 +232,73 @@ hipError_t launch_pack_i8(const int8_t* Wq, int64_t O, int64_t K, int64_t ldw, i
 hipError_t launch_unpack_i8(const int8_t* values, const uint32_t* indices, int64_t O, int64_t K, int N, int M, int8_t* Wd,
                             int64_t ldw, hipStream_t s);
 
+// nm_norm.hip: layer norm of rows (of the sum of X and R) and its backward pass
+struct NormCall {
+  const void* X;
+  const void* R;  // nullable, type of X
+  const float* w; // nullable
+  const float* b; // nullable
+  void* Y;
+  void* S;        // nullable: X + R, type of X
+  float* stats;   // nullable: (mean, rstd) per row
+  int64_t T, C, ldx, ldr, ldy, lds;
+  float eps;
+  bool x_f32, y_f32;
+};
+hipError_t launch_norm(const NormCall& c, hipStream_t s);
+struct NormGradCall {
+  const void* dY;
+  const void* S;
+  const float* stats;
+  const float* w;  // nullable
+  const void* dS;  // nullable, type of dY: added to the gradient
+  void* dX;
+  float* dw;       // nullable, with db
+  float* db;
+  int64_t T, C, lddy, lds, ldds, lddx;
+  bool dy_f32, s_f32, dx_f32;
+  void* workspace; // norm_grad_workspace_bytes, needed where dw is asked for
+};
+size_t norm_grad_workspace_bytes(int64_t T, int64_t C);
+hipError_t launch_norm_grad(const NormGradCall& c, hipStream_t s);
+
+// nm_rotary.hip
+constexpr int kMaxRotaryAxes = 4;
+struct RotaryCall {
+  const void* X;
+  void* Y;
+  const void* positions;  // [T, axes]
+  const float* freqs;     // [R / 2]
+  int64_t T, H, D, R;
+  int64_t x_token, x_head, y_token, y_head;  // strides in elements
+  int section_end[kMaxRotaryAxes];           // pairs below section_end[0] belong to axis 0, ...
+  int axes;
+  bool positions_f32, interleaved, inverse, x_f32, y_f32;
+};
+hipError_t launch_rotary(const RotaryCall& c, hipStream_t s);
+
+// nm_attention.hip, nm_attention_grad.hip.  Rows of D elements; strides in elements.
+struct HeadRows {
+  bf16_t* p;
+  int64_t token, head;
+};
+struct AttentionCall {
+  HeadRows Q, K, V, O;
+  HeadRows dO, dQ, dK, dV;  // backward only
+  float* lse;               // [Hq, Tq]; nullable in the forward pass
+  const int32_t* offsets_q; // nullable: one sequence
+  const int32_t* offsets_k;
+  const int32_t* lengths_k; // nullable
+  int64_t Tq, Tk;
+  int B, Hq, Hkv, D;
+  int64_t max_q, max_k;     // what the launch is shaped for; longer sequences are computed too
+  bool causal;
+  float scale;
+  void* workspace;
+};
+size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k);
+hipError_t launch_attention(const AttentionCall& c, hipStream_t s);
+size_t attention_grad_workspace_bytes(int64_t Tq, int Hq);
+hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s);
+
 }  // namespace nm
