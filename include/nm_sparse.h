@@ -593,7 +593,9 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
  *   p_ij = exp(s_ij - lse_i),  dS_ij = p_ij (dO_i . v_j - dO_i . o_i)
  *   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i p_ij dO_i, the latter two summed over the
  *   query heads that share the key head; keys past lengths_k get zeros.
- *   workspace   nm_attention_backward_workspace_bytes() bytes, 256-byte aligned.
+ *   workspace   nm_attention_backward_workspace_bytes() bytes, 256-byte aligned: D, and where few key tiles are there for many
+ *               queries, 32-bit sums of runs of queries, which a further launch adds in order.  Contents undefined afterwards;
+ *               concurrent calls need distinct workspaces.
  * Every sum is taken in a fixed order: results repeat bit for bit.
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (Tq <= 0, Tk < 0, either above 2^30; sequences outside [1, 65535], heads_q no multiple of heads_kv,
  * sequences * heads_q above 2^20, head_size outside [1, 128], max_q, max_k < 0, negative strides, tokens or heads of an output that
@@ -619,7 +621,8 @@ typedef struct nm_attention_desc {
 size_t nm_attention_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size,
                                     int64_t max_q, int64_t max_k);
 int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
-size_t nm_attention_backward_workspace_bytes(int64_t Tq, int32_t heads_q);
+size_t nm_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int32_t sequences, int32_t heads_q, int32_t heads_kv,
+                                             int32_t head_size, int64_t max_q, int64_t max_k, int32_t causal);
 int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
 /*

@@ -258,7 +258,8 @@ def load_library() -> ctypes.CDLL:
     lib.nm_attention.restype = c_int32
     lib.nm_attention.argtypes = [ctypes.POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
     lib.nm_attention_backward_workspace_bytes.restype = c_size_t
-    lib.nm_attention_backward_workspace_bytes.argtypes = [c_int64, c_int32]
+    lib.nm_attention_backward_workspace_bytes.argtypes = [c_int64, c_int64, c_int32, c_int32, c_int32, c_int32, c_int64, c_int64,
+                                                          c_int32]
     lib.nm_attention_backward.restype = c_int32
     lib.nm_attention_backward.argtypes = lib.nm_attention.argtypes
     _LIB = lib
@@ -1253,6 +1254,7 @@ def nm_attention_backward(dO, Q, K, V, O, lse, causal: bool = False, scale=None,
     desc.dQ, desc.dK, desc.dV = _heads(dQ, "dQ", Q.shape), _heads(dK, "dK", K.shape), _heads(dV, "dV", K.shape)
     lib = load_library()
     if workspace is None:
-        workspace = _workspace(lib.nm_attention_backward_workspace_bytes(desc.Tq, desc.heads_q), Q.device, stream)
+        workspace = _workspace(lib.nm_attention_backward_workspace_bytes(
+            desc.Tq, desc.Tk, desc.sequences, desc.heads_q, desc.heads_kv, desc.head_size, desc.max_q, desc.max_k, desc.causal), Q.device, stream)
     _check(lib.nm_attention_backward(ctypes.byref(desc), *_scratch(workspace), _stream_handle(stream)))
     return dQ, dK, dV

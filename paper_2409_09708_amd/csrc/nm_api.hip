@@ -680,14 +680,19 @@ int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t work
   return device_status(nm::launch_attention(c, (hipStream_t)stream));
 }
 
-size_t nm_attention_backward_workspace_bytes(int64_t Tq, int32_t heads_q) {
-  return Tq <= 0 || heads_q <= 0 ? 0 : nm::attention_grad_workspace_bytes(Tq, heads_q);
+size_t nm_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int32_t sequences, int32_t heads_q, int32_t heads_kv,
+                                             int32_t head_size, int64_t max_q, int64_t max_k, int32_t causal) {
+  if (!attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, max_k) || Tk < 0 || Tk > (int64_t)1 << 30) return 0;
+  return nm::attention_grad_workspace_bytes(Tq, Tk, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq,
+                                            max_k < Tk ? max_k : Tk, causal != 0);
 }
 
 int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
   nm::AttentionCall c;
   if (int32_t st = attention_check(desc, true, &c)) return st;
-  if (!workspace_ok(workspace, workspace_bytes, nm::attention_grad_workspace_bytes(c.Tq, c.Hq))) return NM_ERR_WORKSPACE;
+  if (!workspace_ok(workspace, workspace_bytes, nm::attention_grad_workspace_bytes(c.Tq, c.Tk, c.B, c.Hq, c.Hkv, c.D, c.max_q,
+                                                                                 c.max_k, c.causal)))
+    return NM_ERR_WORKSPACE;
   c.workspace = workspace;
   return device_status(nm::launch_attention_grad(c, (hipStream_t)stream));
 }

@@ -88,6 +88,8 @@ struct RowTile {
   }
 };
 
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+
 // Eight elements of a row, zeros past element D or where `there` is false.  ALIGNED: rows are whole 16-byte pieces.
 template <bool ALIGNED>
 __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, bool there) {
@@ -101,6 +103,75 @@ __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, b
   }
   return v;
 }
+
+// Two tiles of ROWS rows (of keys and values, or of queries and dO) from memory to LDS, by a block of kThreads lanes.
+// WHOLE (rows of exactly DP elements, all 16-byte aligned): asynchronous copies straight to LDS, one wave-load a kilobyte; rows past
+// the last one repeat it, so the scores of those have to be hidden.  Otherwise through registers, with zeros past the last row
+// and the last element.
+//   fetch(stage, row0)   starts the loads of a tile (rows row0 ..)
+//   settle(stage)        the tile is in LDS, as far as this wave brought it: a barrier follows
+template <int DP, int ROWS, bool WHOLE, bool ALIGNED>
+struct TilePair {
+  using Tile = RowTile<DP>;
+  static constexpr int kBytes = ROWS * Tile::kRowBytes, kPieces = ROWS * Tile::kPieces;
+  static constexpr int kLoads = (kPieces + kThreads - 1) / kThreads;
+  const bf16_t* base[2];  // row 0 of the sequence and head
+  int64_t stride[2];
+  int rows, D;            // of the sequence
+  unsigned char* smem;    // stages of 2 * kBytes
+  uint32_t lds;           // its address
+  u32x4_t in[WHOLE ? 1 : 2][WHOLE ? 1 : kLoads];
+
+  __device__ __forceinline__ void fetch(int stage, int row0) {
+    const int tid = threadIdx.x;
+    if constexpr (WHOLE) {
+      const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (uint32_t)stage * 2 * kBytes);
+      const int last = rows - 1 - row0;  // >= 0
+      if (kPieces % kThreads == 0 || wave * 64 < kPieces) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uniform_ptr_t from = make_uniform(base[t] + (int64_t)row0 * stride[t]);
+          const uint32_t bytes = (uint32_t)stride[t] * 2;
+#pragma unroll
+          for (int n = 0; n < kLoads; ++n) {
+            const int i = (n * kWaves + wave) * 64 + lane;
+            int row = i / Tile::kPieces;
+            const int piece = (i % Tile::kPieces) ^ Tile::swizzle(row);
+            row = row < last ? row : last;
+            dma16(from, (uint32_t)row * bytes + piece * 16, to + t * kBytes + (n * kWaves + wave) * 1024);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          const int i = n * kThreads + tid, row = row0 + i / Tile::kPieces;
+          in[t][n] = load_piece<ALIGNED>(base[t] + (int64_t)row * stride[t], i % Tile::kPieces * 8, D,
+                                         row < rows && (kPieces % kThreads == 0 || i < kPieces));
+        }
+    }
+  }
+  __device__ __forceinline__ void settle(int stage) {
+    if constexpr (WHOLE) {
+      wait_loads_outstanding<0>();
+    } else {
+      const int tid = threadIdx.x;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          const int i = n * kThreads + tid;
+          if (kPieces % kThreads == 0 || i < kPieces)
+            *reinterpret_cast<u32x4_t*>(smem + (2 * stage + t) * kBytes + Tile::place(i / Tile::kPieces, i % Tile::kPieces)) = in[t][n];
+        }
+    }
+  }
+};
+// WHOLE tiles address their rows by 32-bit offsets
+constexpr int64_t kMostStride = (int64_t)1 << 24;
 
 // probabilities (registers 8 s .. 8 s + 7 of an accumulator) as an operand
 __device__ __forceinline__ u32x4_t acc_operand(const f32x16_t& p, int s) {
@@ -130,7 +201,6 @@ __device__ __forceinline__ void store_column(bf16_t* row, const f32x16_t (&acc)[
     }
 }
 
-constexpr int kWaves = 4, kThreads = kWaves * 64;
 
 // Scores of the rows from `limit` on (relative to the lane's first row, 4 (lane / 32)) are not seen.
 __device__ __forceinline__ void hide_rows(f32x16_t& s, int limit) {
@@ -176,14 +246,23 @@ inline int64_t tile_blocks(int sequences, int kv_heads, int group, int n_tiles) 
 // A launch holds fewer than 2^32 lanes, 2^24 blocks of 256.
 constexpr int64_t kMostBlocks = (int64_t)1 << 24;
 
+inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-template <bool ALIGNED, class F>
-void with_head(int D, F&& f) {
-  if (D <= 32) f(std::integral_constant<int, 32>{}, std::bool_constant<ALIGNED>{});
-  else if (D <= 64) f(std::integral_constant<int, 64>{}, std::bool_constant<ALIGNED>{});
-  else f(std::integral_constant<int, 128>{}, std::bool_constant<ALIGNED>{});
+// calls f(padded head size, WHOLE, ALIGNED) as integral constants
+template <class F>
+void with_head(int D, bool aligned, bool short_strides, F&& f) {
+  auto sized = [&](auto dp) {
+    if (!aligned) f(dp, std::false_type{}, std::false_type{});
+    else if (D == decltype(dp)::value && short_strides) f(dp, std::true_type{}, std::true_type{});
+    else f(dp, std::false_type{}, std::true_type{});
+  };
+  if (D <= 32) sized(std::integral_constant<int, 32>{});
+  else if (D <= 64) sized(std::integral_constant<int, 64>{});
+  else sized(std::integral_constant<int, 128>{});
 }
+
+#define NM_LDS_ADDRESS(p) ((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(p))
 
 inline bool head_rows_aligned(const HeadRows& r) { return ((uintptr_t)r.p & 15) == 0 && (r.token | r.head) % 8 == 0; }
 

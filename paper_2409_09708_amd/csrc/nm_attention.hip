@@ -66,11 +66,10 @@ __device__ __forceinline__ void softmax_step(f32x16_t (&s)[KB], float c, float& 
 constexpr int kKeys = 64;             // per tile
 constexpr int kQueries = kWaves * 32; // per block
 
-template <int DP, bool ALIGNED>
+template <int DP, bool WHOLE, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
-  constexpr int LOADS = kKeys * Tile::kPieces / kThreads;  // pieces of a tile per lane
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of keys and values
   TilePlace at;
   if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_tiles, true, &at)) return;
@@ -81,8 +80,15 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;  // causal: query i sees keys up to i + shift
-  const bf16_t* Kh = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
-  const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+  TilePair<DP, kKeys, WHOLE, ALIGNED> load;
+  load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
+  load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+  load.stride[0] = a.c.K.token;
+  load.stride[1] = a.c.V.token;
+  load.rows = sk.len;
+  load.D = D;
+  load.smem = smem[0];
+  load.lds = NM_LDS_ADDRESS(smem[0]);
 
   for (int tile = at.tile; (int64_t)tile * kQueries < sq.len; tile += a.n_tiles) {
     const int q_wave = tile * kQueries + wave * 32;
@@ -112,34 +118,14 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
       for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
     float ref = kMinusInf, sum = 0.f;
 
-    u32x4_t k_in[LOADS], v_in[LOADS];
-    auto fetch = [&](int k0) {
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, row = k0 + i / Tile::kPieces, d = i % Tile::kPieces * 8;
-        const bool there = row < sk.len;
-        k_in[n] = load_piece<ALIGNED>(Kh + (int64_t)row * a.c.K.token, d, D, there);
-        v_in[n] = load_piece<ALIGNED>(Vh + (int64_t)row * a.c.V.token, d, D, there);
-      }
-    };
-    auto settle = [&](int stage) {
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, at = Tile::place(i / Tile::kPieces, i % Tile::kPieces);
-        *reinterpret_cast<u32x4_t*>(smem[stage] + at) = k_in[n];
-        *reinterpret_cast<u32x4_t*>(smem[stage] + TILE_BYTES + at) = v_in[n];
-      }
-    };
     const int n_key_tiles = (end + kKeys - 1) / kKeys;
     __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
-    if (n_key_tiles > 0) {
-      fetch(0);
-      settle(0);
-    }
-    __syncthreads();
+    if (n_key_tiles > 0) load.fetch(0, 0);
     for (int kt = 0; kt < n_key_tiles; ++kt) {
       const int k0 = kt * kKeys;
-      if (kt + 1 < n_key_tiles) fetch(k0 + kKeys);
+      load.settle(kt & 1);
+      __syncthreads();
+      if (kt + 1 < n_key_tiles) load.fetch((kt + 1) & 1, k0 + kKeys);
       const unsigned char* k_tile = smem[kt & 1];
       const unsigned char* v_tile = k_tile + TILE_BYTES;
       if (k0 < wave_end) {
@@ -163,8 +149,6 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
           for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(v_tile, 16 * st, b, lane), p, acc[b]);
         }
       }
-      if (kt + 1 < n_key_tiles) settle((kt + 1) & 1);
-      __syncthreads();
     }
     sum = half_sum(sum);
     if (live) {
@@ -387,8 +371,6 @@ CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
   return p;
 }
 
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-
 }  // namespace
 
 size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k) {
@@ -416,9 +398,9 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) +
                                           round256(columns * padded_head(c.D) * sizeof(float)));
   }
-  auto launch = [&](auto dp, auto al) {
+  auto launch = [&](auto dp, auto whole, auto al) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool ALIGNED = decltype(al)::value;
+    constexpr bool WHOLE = decltype(whole)::value, ALIGNED = decltype(al)::value;
     if (plan.taken) {
       const int64_t blocks = (int64_t)a.n_chunks * a.n_row_tiles * c.B * c.Hkv;
       cache_kernel<DP, ALIGNED><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
@@ -427,11 +409,10 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
         cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
       }
     } else {
-      prompt_kernel<DP, ALIGNED><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
+      prompt_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
     }
   };
-  if (aligned) with_head<true>(c.D, launch);
-  else with_head<false>(c.D, launch);
+  with_head(c.D, aligned, c.K.token <= kMostStride && c.V.token <= kMostStride, launch);
   return hipGetLastError();
 }
 

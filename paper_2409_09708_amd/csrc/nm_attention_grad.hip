@@ -20,18 +20,20 @@ struct GradArgs {
   int group;
   float scale_log2;
   int n_q_tiles, n_k_tiles;
-  float* delta;  // D: [Hq, Tq]
+  int chunk, n_chunks;  // of a key tile's steps
+  float* delta;         // D: [Hq, Tq]
+  float* part;          // [chunk][key][key head][dK, dV][DP]
 };
 
 constexpr int kKeys = 64;              // keys per tile of grad_query_kernel
 constexpr int kRows = kWaves * 32;     // queries (keys) that a block keeps
 constexpr int kQueries = 32;           // queries per tile of grad_key_kernel
+constexpr int64_t kKeyBlocks = 512;    // blocks that grad_key_kernel's work is cut for
 
-template <int DP, bool ALIGNED>
+template <int DP, bool WHOLE, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
-  constexpr int LOADS = kKeys * Tile::kPieces / kThreads;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];
   TilePlace at;
   if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_q_tiles, true, &at)) return;
@@ -42,8 +44,15 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
-  const bf16_t* Kh = a.c.K.p + sk.first * a.c.K.token + at.kv_head * a.c.K.head;
-  const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + at.kv_head * a.c.V.head;
+  TilePair<DP, kKeys, WHOLE, ALIGNED> load;
+  load.base[0] = a.c.K.p + sk.first * a.c.K.token + at.kv_head * a.c.K.head;
+  load.base[1] = a.c.V.p + sk.first * a.c.V.token + at.kv_head * a.c.V.head;
+  load.stride[0] = a.c.K.token;
+  load.stride[1] = a.c.V.token;
+  load.rows = sk.len;
+  load.D = D;
+  load.smem = smem[0];
+  load.lds = NM_LDS_ADDRESS(smem[0]);
 
   for (int tile = at.tile; (int64_t)tile * kRows < sq.len; tile += a.n_q_tiles) {
     const int q_wave = tile * kRows + wave * 32;
@@ -92,34 +101,14 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
 
-    u32x4_t k_in[LOADS], v_in[LOADS];
-    auto fetch = [&](int k0) {
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, row = k0 + i / Tile::kPieces, d = i % Tile::kPieces * 8;
-        const bool there = row < sk.len;
-        k_in[n] = load_piece<ALIGNED>(Kh + (int64_t)row * a.c.K.token, d, D, there);
-        v_in[n] = load_piece<ALIGNED>(Vh + (int64_t)row * a.c.V.token, d, D, there);
-      }
-    };
-    auto settle = [&](int stage) {
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, to = Tile::place(i / Tile::kPieces, i % Tile::kPieces);
-        *reinterpret_cast<u32x4_t*>(smem[stage] + to) = k_in[n];
-        *reinterpret_cast<u32x4_t*>(smem[stage] + TILE_BYTES + to) = v_in[n];
-      }
-    };
     const int n_key_tiles = (end + kKeys - 1) / kKeys;
-    __syncthreads();
-    if (n_key_tiles > 0) {
-      fetch(0);
-      settle(0);
-    }
-    __syncthreads();
+    __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
+    if (n_key_tiles > 0) load.fetch(0, 0);
     for (int kt = 0; kt < n_key_tiles; ++kt) {
       const int k0 = kt * kKeys;
-      if (kt + 1 < n_key_tiles) fetch(k0 + kKeys);
+      load.settle(kt & 1);
+      __syncthreads();
+      if (kt + 1 < n_key_tiles) load.fetch((kt + 1) & 1, k0 + kKeys);
       const unsigned char* k_tile = smem[kt & 1];
       const unsigned char* v_tile = k_tile + TILE_BYTES;
       if (k0 < wave_end) {
@@ -143,22 +132,39 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
           }
         }
       }
-      if (kt + 1 < n_key_tiles) settle((kt + 1) & 1);
-      __syncthreads();
     }
     if (live) store_column<DP, ALIGNED>(a.c.dQ.p + tok * a.c.dQ.token + head * a.c.dQ.head, acc, lane, D, a.c.scale);
   }
 }
 
-template <int DP, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(const GradArgs a) {
+// Key tiles differ in how many queries see them, and shared key heads leave few of them, so the (head, query tile) steps of a key
+// tile are cut into chunks of `chunk` for different blocks; where there is more than one, 32-bit sums of each go to the
+// workspace and grad_key_sum_kernel adds them in order.
+struct KeySteps {
+  int first_q, per_head, steps, chunks;
+};
+__device__ __forceinline__ KeySteps key_steps(const GradArgs& a, int tile, int q_len, int k_len) {
+  const int shift = k_len - q_len;
+  KeySteps s;
+  // query tiles from the first one that sees a key of the tile on, for each head of the group: one list
+  s.first_q = !a.c.causal || tile * kRows - shift < 0 ? 0 : (tile * kRows - shift) / kQueries * kQueries;
+  s.per_head = tile * kRows < k_len && s.first_q < q_len ? (q_len - s.first_q + kQueries - 1) / kQueries : 0;
+  s.steps = s.per_head * a.group;
+  s.chunks = (s.steps + a.chunk - 1) / a.chunk;
+  if (s.chunks < 1) s.chunks = 1;
+  if (s.chunks > a.n_chunks) s.chunks = a.n_chunks;  // (the last one takes the rest)
+  return s;
+}
+
+template <int DP, bool WHOLE, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_key_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kQueries * Tile::kRowBytes;
-  constexpr int PIECES = kQueries * Tile::kPieces, LOADS = (PIECES + kThreads - 1) / kThreads;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of queries and dO
   __shared__ __attribute__((aligned(16))) float rows[2][2][kQueries];               // ... and of lse (base 2) and D
   TilePlace at;
-  if (!tile_place(a.c.B, a.c.Hkv, 1, a.n_k_tiles, false, &at)) return;
+  if (!tile_place(a.c.B, a.c.Hkv, a.n_chunks, a.n_k_tiles, false, &at)) return;
+  const int chunk = at.sub;
   const int D = a.c.D;
   const Span sq = sequence(a.c.offsets_q, nullptr, at.seq, a.c.Tq);
   const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, at.seq, a.c.Tk);
@@ -166,8 +172,19 @@ __global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(c
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
+  TilePair<DP, kQueries, WHOLE, ALIGNED> load;
+  load.stride[0] = a.c.Q.token;
+  load.stride[1] = a.c.dO.token;
+  load.rows = sq.len;
+  load.D = D;
+  load.smem = smem[0];
+  load.lds = NM_LDS_ADDRESS(smem[0]);
 
   for (int tile = at.tile; (int64_t)tile * kRows < room.len; tile += a.n_k_tiles) {
+    const KeySteps list = key_steps(a, tile, sq.len, sk.len);
+    if (chunk >= list.chunks) continue;
+    const int first_step = chunk * a.chunk;
+    const int end_step = chunk == list.chunks - 1 ? list.steps : first_step + a.chunk;
     const int k_wave = tile * kRows + wave * 32;
     const int kj = k_wave + (lane & 31);
     const int64_t tok = sk.first + kj;
@@ -185,56 +202,40 @@ __global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(c
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.f;
 
-    // query tiles from the first one that sees a key of the block, for each head of the group: one list
-    int first_q = 0;
-    if (a.c.causal) first_q = tile * kRows - shift < 0 ? 0 : (tile * kRows - shift) / kQueries * kQueries;
-    const int per_head = tile * kRows < sk.len && first_q < sq.len ? (sq.len - first_q + kQueries - 1) / kQueries : 0;
-    const int n_steps = per_head * a.group;
-
-    u32x4_t q_in[LOADS], g_in[LOADS];
+    int head = at.kv_head * a.group, q0 = list.first_q;  // of the step whose loads are started next
+    if (list.per_head > 0) {
+      head += first_step / list.per_head;
+      q0 += first_step % list.per_head * kQueries;
+    }
     float row_in = 0.f;
-    auto fetch = [&](int step) {
-      const int head = at.kv_head * a.group + step / per_head, q0 = first_q + step % per_head * kQueries;
-      const bf16_t* Qh = a.c.Q.p + sq.first * a.c.Q.token + head * a.c.Q.head;
-      const bf16_t* Gh = a.c.dO.p + sq.first * a.c.dO.token + head * a.c.dO.head;
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, row = q0 + i / Tile::kPieces, d = i % Tile::kPieces * 8;
-        const bool there = row < sq.len && (PIECES % kThreads == 0 || i < PIECES);
-        q_in[n] = load_piece<ALIGNED>(Qh + (int64_t)row * a.c.Q.token, d, D, there);
-        g_in[n] = load_piece<ALIGNED>(Gh + (int64_t)row * a.c.dO.token, d, D, there);
-      }
+    auto fetch = [&](int stage) {
+      load.base[0] = a.c.Q.p + sq.first * a.c.Q.token + head * a.c.Q.head;
+      load.base[1] = a.c.dO.p + sq.first * a.c.dO.token + head * a.c.dO.head;
       if (tid < 2 * kQueries) {
         const int row = q0 + tid % kQueries;
         const int64_t n = (int64_t)head * a.c.Tq + sq.first + row;
-        row_in = row >= sq.len ? 0.f : tid < kQueries ? a.c.lse[n] * kLog2e : a.delta[n];
+        // (no row: a log-sum of infinity, and so probabilities of zero)
+        row_in = row >= sq.len ? (tid < kQueries ? -kMinusInf : 0.f) : tid < kQueries ? a.c.lse[n] * kLog2e : a.delta[n];
         if (row_in == kMinusInf) row_in = 0.f;
       }
+      load.fetch(stage, q0);
     };
-    auto settle = [&](int stage) {
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        const int i = n * kThreads + tid, to = Tile::place(i / Tile::kPieces, i % Tile::kPieces);
-        if (PIECES % kThreads == 0 || i < PIECES) {
-          *reinterpret_cast<u32x4_t*>(smem[stage] + to) = q_in[n];
-          *reinterpret_cast<u32x4_t*>(smem[stage] + TILE_BYTES + to) = g_in[n];
-        }
-      }
+    __syncthreads();  // (a block's second key tile)
+    if (first_step < end_step) fetch(0);
+    for (int step = first_step; step < end_step; ++step) {
+      const int stage = (step - first_step) & 1, q_now = q0;
       if (tid < 2 * kQueries) rows[stage][tid / kQueries][tid % kQueries] = row_in;
-    };
-    __syncthreads();
-    if (n_steps > 0) {
-      fetch(0);
-      settle(0);
-    }
-    __syncthreads();
-    for (int step = 0; step < n_steps; ++step) {
-      const int q0 = first_q + step % per_head * kQueries;
-      if (step + 1 < n_steps) fetch(step + 1);
-      const unsigned char* q_tile = smem[step & 1];
+      load.settle(stage);
+      __syncthreads();
+      if (step + 1 < end_step) {
+        q0 += kQueries;
+        if (q0 >= sq.len) { q0 = list.first_q; ++head; }
+        fetch(stage ^ 1);
+      }
+      const unsigned char* q_tile = smem[stage];
       const unsigned char* g_tile = q_tile + TILE_BYTES;
       // (a wave whose keys none of these queries sees, or without keys)
-      if (k_wave < sk.len && (!a.c.causal || q0 + kQueries - 1 + shift >= k_wave)) {
+      if (k_wave < sk.len && (!a.c.causal || q_now + kQueries - 1 + shift >= k_wave)) {
         f32x16_t s, dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
@@ -242,9 +243,9 @@ __global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(c
         for (int st = 0; st < STEPS; ++st) s = mma32(Tile::rows(q_tile, 0, st, lane), k[st], s);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) dp = mma32(Tile::rows(g_tile, 0, st, lane), v[st], dp);
-        const float* row = rows[step & 1][0] + 4 * half;
-        if (a.c.causal && q0 + shift < k_wave + 31) {
-          const int first = kj - shift - q0 - 4 * half;  // rows before it do not see the lane's key
+        const float* row = rows[stage][0] + 4 * half;
+        if (a.c.causal && q_now + shift < k_wave + 31) {
+          const int first = kj - shift - q_now - 4 * half;  // rows before it do not see the lane's key
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = acc_row(r) >= first ? s[r] : kMinusInf;
         }
@@ -269,10 +270,19 @@ __global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(c
           }
         }
       }
-      if (step + 1 < n_steps) settle((step + 1) & 1);
-      __syncthreads();
     }
-    if (kj < room.len) {
+    if (list.chunks > 1) {
+      if (kj < sk.len) {
+        float* to = a.part + ((((int64_t)chunk * a.c.Tk + tok) * a.c.Hkv + at.kv_head) * 2) * DP + 4 * half;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            *reinterpret_cast<float4*>(to + 32 * b + acc_row(r)) = float4{dk[b][r], dk[b][r + 1], dk[b][r + 2], dk[b][r + 3]};
+            *reinterpret_cast<float4*>(to + DP + 32 * b + acc_row(r)) = float4{dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]};
+          }
+      }
+    } else if (kj < room.len) {
       if (kj >= sk.len) {  // (it was multiplied as a row of zeros: what came of that, infinities included, is not its gradient)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -285,6 +295,63 @@ __global__ void __launch_bounds__(kThreads, DP == 128 ? 1 : 2) grad_key_kernel(c
   }
 }
 
+// dK and dV of the key tiles that were cut: a wave per key and head, four elements a lane (dK on the first half of the lanes of a
+// 32-element run, dV on the other).
+template <int DP>
+__global__ void __launch_bounds__(kThreads) grad_key_sum_kernel(const GradArgs a) {
+  const int seq = blockIdx.y;
+  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
+  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const Span room = sequence(a.c.offsets_k, nullptr, seq, a.c.Tk);
+  constexpr int LANES = 2 * DP / 4, PER_BLOCK = kThreads / LANES;  // lanes and rows of one (key, head)
+  const int lane = threadIdx.x % LANES;
+  const bool values = lane >= DP / 4;
+  const int d = lane % (DP / 4) * 4;
+  for (int64_t n = (int64_t)blockIdx.x * PER_BLOCK + threadIdx.x / LANES; n < (int64_t)room.len * a.c.Hkv;
+       n += (int64_t)gridDim.x * PER_BLOCK) {
+    const int kj = (int)(n / a.c.Hkv), head = (int)(n % a.c.Hkv);
+    const int chunks = key_steps(a, kj / kRows, sq.len, sk.len).chunks;
+    if (chunks == 1 || d >= a.c.D) continue;  // (written already)
+    const int64_t tok = sk.first + kj;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    if (kj < sk.len) {
+      const float* from = a.part + ((tok * a.c.Hkv + head) * 2 + (values ? 1 : 0)) * DP + d;
+      for (int c = 0; c < chunks; ++c) {
+        const float4 x = *reinterpret_cast<const float4*>(from + (int64_t)c * a.c.Tk * a.c.Hkv * 2 * DP);
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+      }
+      const float by = values ? 1.f : a.c.scale;
+      o.x *= by; o.y *= by; o.z *= by; o.w *= by;
+    }
+    const HeadRows& to = values ? a.c.dV : a.c.dK;
+    bf16_t* out = to.p + tok * to.token + head * to.head + d;
+    const float v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d + e < a.c.D) out[e] = (bf16_t)f32_to_bf16_rne(v[e]);
+  }
+}
+
+// How the key tiles' steps are cut: into about two blocks' worth per compute unit, from what the call says about the lengths;
+// not below 16 steps (512 queries), where the sums' way through memory would cost as much as the steps.
+constexpr int kLeastSteps = 16, kMostChunks = 32;
+struct KeyPlan {
+  int chunk, n_chunks;
+};
+KeyPlan key_plan(int64_t Tk, int B, int Hkv, int group, int64_t max_q, int64_t max_k, bool causal) {
+  const int64_t most = (max_q + kQueries - 1) / kQueries * group;  // steps of a key tile
+  const int64_t all_tiles = Tk / kRows + B, tiles = all_tiles < (int64_t)B * ((max_k + kRows - 1) / kRows) ? all_tiles : (int64_t)B * ((max_k + kRows - 1) / kRows);
+  const int64_t total = tiles * Hkv * (causal ? (most + 1) / 2 : most);
+  int64_t chunk = (total + kKeyBlocks - 1) / kKeyBlocks;
+  chunk = chunk < kLeastSteps ? kLeastSteps : chunk;
+  if ((most + chunk - 1) / chunk > kMostChunks) chunk = (most + kMostChunks - 1) / kMostChunks;
+  KeyPlan p;
+  p.chunk = (int)(chunk < (1 << 30) ? chunk : 1 << 30);
+  p.n_chunks = (int)((most + p.chunk - 1) / p.chunk);
+  if (p.n_chunks < 1) p.n_chunks = 1;
+  return p;
+}
+
 int tiles(int64_t most, int B, int Hkv, int group) {
   int n = (int)((most + kRows - 1) / kRows);
   if (n < 1) n = 1;
@@ -294,28 +361,44 @@ int tiles(int64_t most, int B, int Hkv, int group) {
 
 }  // namespace
 
-size_t attention_grad_workspace_bytes(int64_t Tq, int Hq) { return (size_t)Tq * Hq * sizeof(float); }
+size_t attention_grad_workspace_bytes(int64_t Tq, int64_t Tk, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k,
+                                      bool causal) {
+  const KeyPlan p = key_plan(Tk, B, Hkv, Hq / Hkv, max_q, max_k, causal);
+  const size_t parts = p.n_chunks > 1 ? (size_t)p.n_chunks * Tk * Hkv * 2 * padded_head(D) * sizeof(float) : 0;
+  return round256((size_t)Tq * Hq * sizeof(float)) + parts;
+}
 
 hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s) {
   GradArgs a = {};
   a.c = c;
   a.group = c.Hq / c.Hkv;
   a.scale_log2 = c.scale * kLog2e;
+  const KeyPlan plan = key_plan(c.Tk, c.B, c.Hkv, a.group, c.max_q, c.max_k, c.causal);
+  a.chunk = plan.chunk;
+  a.n_chunks = plan.n_chunks;
   a.n_q_tiles = tiles(c.max_q, c.B, c.Hkv, a.group);
-  a.n_k_tiles = tiles(c.max_k, c.B, c.Hkv, 1);
+  a.n_k_tiles = tiles(c.max_k, c.B, c.Hkv, a.n_chunks);
   a.delta = static_cast<float*>(c.workspace);
+  a.part = a.delta + round256((size_t)c.Tq * c.Hq * sizeof(float)) / sizeof(float);
   const bool aligned = c.D % 8 == 0 && head_rows_aligned(c.Q) && head_rows_aligned(c.K) && head_rows_aligned(c.V) &&
                        head_rows_aligned(c.O) && head_rows_aligned(c.dO) && head_rows_aligned(c.dQ) &&
                        head_rows_aligned(c.dK) && head_rows_aligned(c.dV);
-  auto launch = [&](auto dp, auto al) {
+  const bool short_strides = c.K.token <= kMostStride && c.V.token <= kMostStride && c.Q.token <= kMostStride && c.dO.token <= kMostStride;
+  with_head(c.D, aligned, short_strides, [&](auto dp, auto whole, auto al) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool ALIGNED = decltype(al)::value;
-    const int64_t q_blocks = tile_blocks(c.B, c.Hkv, a.group, a.n_q_tiles), k_blocks = tile_blocks(c.B, c.Hkv, 1, a.n_k_tiles);
-    grad_query_kernel<DP, ALIGNED><<<dim3((unsigned)q_blocks), kThreads, 0, s>>>(a);
-    if (c.Tk > 0) grad_key_kernel<DP, ALIGNED><<<dim3((unsigned)k_blocks), kThreads, 0, s>>>(a);
-  };
-  if (aligned) with_head<true>(c.D, launch);
-  else with_head<false>(c.D, launch);
+    constexpr bool WHOLE = decltype(whole)::value, ALIGNED = decltype(al)::value;
+    const int64_t q_blocks = tile_blocks(c.B, c.Hkv, a.group, a.n_q_tiles);
+    grad_query_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)q_blocks), kThreads, 0, s>>>(a);
+    if (c.Tk == 0) return;
+    const int64_t k_blocks = tile_blocks(c.B, c.Hkv, a.n_chunks, a.n_k_tiles);
+    grad_key_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)k_blocks), kThreads, 0, s>>>(a);
+    if (a.n_chunks > 1) {
+      constexpr int PER_BLOCK = kThreads / (2 * DP / 4);
+      int64_t blocks = (c.max_k * c.Hkv + PER_BLOCK - 1) / PER_BLOCK;
+      blocks = blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096;
+      grad_key_sum_kernel<DP><<<dim3((unsigned)blocks, (unsigned)c.B), kThreads, 0, s>>>(a);
+    }
+  });
   return hipGetLastError();
 }
 

@@ -298,7 +298,8 @@ struct AttentionCall {
 };
 size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k);
 hipError_t launch_attention(const AttentionCall& c, hipStream_t s);
-size_t attention_grad_workspace_bytes(int64_t Tq, int Hq);
+size_t attention_grad_workspace_bytes(int64_t Tq, int64_t Tk, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k,
+                                      bool causal);
 hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s);
 
 }  // namespace nm

@@ -124,7 +124,9 @@ def test_attention_workspace(lib):
     assert attention(lib, ws=None, bytes=0, Tq=1, Tk=16384, max_q=1, max_k=16384, heads_q=32, heads_kv=8, Q=H(FAKE, 4096, 128), O=H(FAKE, 4096, 128),
                      K=H(FAKE, 1024, 128), V=H(FAKE, 1024, 128), head_size=128) == WORKSPACE
     assert size(0, 1, 32, 8, 128, 1, 16384) == 0 and size(1, 1, 32, 7, 128, 1, 16384) == 0
-    assert lib.nm_attention_backward_workspace_bytes(100, 4) == 1600 and lib.nm_attention_backward_workspace_bytes(0, 4) == 0
+    back = lib.nm_attention_backward_workspace_bytes
+    assert back(100, 100, 1, 4, 2, 64, 100, 100, 0) == 1792 and back(0, 100, 1, 4, 2, 64, 100, 100, 0) == 0
+    assert back(8192, 8192, 1, 16, 4, 128, 8192, 8192, 1) > 8192 * 16 * 4
     assert attention(lib, True, ws=None, bytes=0) == WORKSPACE
 
 
