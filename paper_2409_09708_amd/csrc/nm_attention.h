@@ -21,12 +21,33 @@ namespace nm {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_ptr;
+typedef __attribute__((address_space(3))) const u32x4_t* lds_u32x4_ptr;
 
 __device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 // row of register r in the accumulator, without the lane's 4 (lane / 32)
 __host__ __device__ constexpr int acc_row(int r) { return 8 * (r / 4) + r % 4; }
+
+// N products whose first operands come from LDS, read kAhead of them ahead of their use and in just this order: left to
+// itself the compiler reads an operand right before the product that takes it, to spare registers, and waits for it.
+constexpr int kAhead = 4;
+template <int N, class Load>
+__device__ __forceinline__ void read_ahead(u32x4_t (&f)[kAhead], Load load) {
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (i < N) f[i] = load(i);
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <int N, class Load, class Use>
+__device__ __forceinline__ void products(u32x4_t (&f)[kAhead], Load load, Use use) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    use(i, f[i % kAhead]);
+    if (i + kAhead < N) f[i % kAhead] = load(i + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 // The value of the lane 32 away, combined.
 __device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
@@ -70,20 +91,23 @@ struct RowTile {
   }
   static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ swizzle(row)) << 4); }
 
-  // rows row0 .. row0 + 31 (row0 a multiple of 32) as an operand: elements 16 step + 8 (lane / 32) .. + 7 of row lane % 32
-  static __device__ __forceinline__ u32x4_t rows(const unsigned char* tile, int row0, int step, int lane) {
-    return *reinterpret_cast<const u32x4_t*>(tile + row0 * kRowBytes + place(lane & 31, 2 * step + (lane >> 5)));
+  // Operands from the tile at LDS address `tile` (a multiple of 256).  An operand's address is a lane's own constant with a few
+  // bits changed, one instruction each, so that none is kept.
+  //   rows     elements 16 step + 8 (lane / 32) .. + 7 of row row0 + lane % 32 (row0 a multiple of 32);  at = tile + row_base(lane)
+  //   columns  columns 32 block .. + 31 of rows row0 .. row0 + 15 (row0 a multiple of 16) as the first operand, rows in the order
+  //            {0 .. 3, 8 .. 11} + 4 (lane / 32);  at = tile + column_base(lane)
+  static __device__ __forceinline__ uint32_t row_base(int lane) { return place(lane & 31, lane >> 5); }
+  static __device__ __forceinline__ uint32_t column_base(int lane) {
+    return place(4 * (lane >> 5) + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + (lane & 1) * 8;
   }
-  // columns 32 block .. + 31 of rows row0 .. row0 + 15 (row0 a multiple of 16) as the first operand, rows in the order
-  // {0 .. 3, 8 .. 11} + 4 (lane / 32)
-  static __device__ __forceinline__ u32x4_t columns(const unsigned char* tile, int row0, int block, int lane) {
-    const int row = 4 * (lane >> 5) + ((lane >> 2) & 3);
-    const int piece = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-    const unsigned char* at = tile + row0 * kRowBytes + (lane & 1) * 8;
-    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + place(row, piece)));
-    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(at + place(row + 8, piece)));
+  static __device__ __forceinline__ u32x4_t rows(uint32_t at, int row0, int step) {
+    return *(lds_u32x4_ptr)(uintptr_t)((at ^ (step << 5)) + row0 * kRowBytes);
+  }
+  static __device__ __forceinline__ u32x4_t columns(uint32_t at, int row0, int block) {
     typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-    const u32x2_t l = __builtin_bit_cast(u32x2_t, lo), h = __builtin_bit_cast(u32x2_t, hi);
+    const uint32_t lo = (at ^ (block << 6)) + row0 * kRowBytes, hi = (at ^ (block << 6) ^ 32) + (row0 + 8) * kRowBytes;
+    const u32x2_t l = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(uintptr_t)lo));
+    const u32x2_t h = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(uintptr_t)hi));
     return u32x4_t{l[0], l[1], h[0], h[1]};
   }
 };
@@ -173,6 +197,14 @@ struct TilePair {
 // WHOLE tiles address their rows by 32-bit offsets
 constexpr int64_t kMostStride = (int64_t)1 << 24;
 
+// Operands that a loop keeps have arrived.  The compiler, which does not see the asynchronous copies, would wait for them at their
+// first use in the loop, and there for all copies that have just been started, on every round.
+template <int N>
+__device__ __forceinline__ void arrived(u32x4_t (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
 // probabilities (registers 8 s .. 8 s + 7 of an accumulator) as an operand
 __device__ __forceinline__ u32x4_t acc_operand(const f32x16_t& p, int s) {
   return u32x4_t{pack_bf16x2(p[8 * s], p[8 * s + 1]), pack_bf16x2(p[8 * s + 2], p[8 * s + 3]),
@@ -209,9 +241,9 @@ __device__ __forceinline__ void hide_rows(f32x16_t& s, int limit) {
 }
 
 // Block -> (sequence, key head, head of its group, tile).  Consecutive blocks go to consecutive XCDs, each with an L2
-// of its own.  Where a head has many tiles, XCD x takes tiles x, x + 8, ... of one key head after another, so that at any time
+// of its own.  Where a head has many tiles, each XCD takes one of every eight of one key head after another, so that at any time
 // an L2 holds the keys of about one head, and the longest tiles of a causal mask come first (the last queries: `last_first`; the
-// first keys).  Where a head has few tiles, XCD x takes all tiles of every eighth key head.
+// first keys); which of the eight alternates in direction, or the first XCDs would get the longer ones every time.  Where a head has few tiles, XCD x takes all tiles of every eighth key head.
 constexpr int kManyTiles = 16;
 struct TilePlace {
   int seq, kv_head, sub, tile;
@@ -222,7 +254,8 @@ __device__ __forceinline__ bool tile_place(int sequences, int kv_heads, int grou
   if (n_tiles >= kManyTiles) {
     const int per_unit = (n_tiles + 7) / 8 * group;
     unit = slot / per_unit;
-    t = slot % per_unit / group * 8 + xcd;
+    const int round = slot % per_unit / group;
+    t = round * 8 + (round % 2 ? 7 - xcd : xcd);
     p->sub = slot % per_unit % group;
     if (t >= n_tiles) return false;
   } else {

@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     float ref = kMinusInf, sum = 0.f;
 
     const int n_key_tiles = (end + kKeys - 1) / kKeys;
+    if constexpr (WHOLE) arrived(q);
     __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
     if (n_key_tiles > 0) load.fetch(0, 0);
     for (int kt = 0; kt < n_key_tiles; ++kt) {
@@ -126,28 +127,30 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
       load.settle(kt & 1);
       __syncthreads();
       if (kt + 1 < n_key_tiles) load.fetch((kt + 1) & 1, k0 + kKeys);
-      const unsigned char* k_tile = smem[kt & 1];
-      const unsigned char* v_tile = k_tile + TILE_BYTES;
       if (k0 < wave_end) {
+        const uint32_t k_tile = load.lds + (uint32_t)(kt & 1) * 2 * TILE_BYTES, v_tile = k_tile + TILE_BYTES;
+        const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
+        constexpr int NS = kKeys / 32 * STEPS, NV = kKeys / 16 * NB;
+        auto keys = [&](int i) { return Tile::rows(k_at, i / STEPS * 32, i % STEPS); };
+        auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
         f32x16_t s[kKeys / 32];
 #pragma unroll
-        for (int kb = 0; kb < kKeys / 32; ++kb) {
+        for (int kb = 0; kb < kKeys / 32; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-#pragma unroll
-          for (int st = 0; st < STEPS; ++st) s[kb] = mma32(Tile::rows(k_tile, 32 * kb, st, lane), q[st], s[kb]);
-        }
+        u32x4_t f[kAhead];
+        read_ahead<NS>(f, keys);
+        products<NS>(f, keys, [&](int i, u32x4_t k) { s[i / STEPS] = mma32(k, q[i % STEPS], s[i / STEPS]); });
+        read_ahead<NV>(f, values);
         if (k0 + kKeys > first_hidden) {
 #pragma unroll
           for (int kb = 0; kb < kKeys / 32; ++kb) hide_rows(s[kb], limit - k0 - 32 * kb - 4 * half);
         }
         softmax_step(s, a.scale_log2, ref, sum, acc);
+        u32x4_t p[kKeys / 16];
 #pragma unroll
-        for (int st = 0; st < kKeys / 16; ++st) {
-          const u32x4_t p = acc_operand(s[st / 2], st % 2);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(v_tile, 16 * st, b, lane), p, acc[b]);
-        }
+        for (int st = 0; st < kKeys / 16; ++st) p[st] = acc_operand(s[st / 2], st % 2);
+        products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, p[i / NB], acc[i % NB]); });
       }
     }
     sum = half_sum(sum);
@@ -192,6 +195,8 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
   const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
   const int64_t columns = (int64_t)sq.len * a.group;
   unsigned char* own = smem + wave * OWN;
+  const uint32_t k_at = NM_LDS_ADDRESS(smem) + wave * OWN + Tile::row_base(lane);
+  const uint32_t v_at = NM_LDS_ADDRESS(smem) + wave * OWN + TILE_BYTES + Tile::column_base(lane);
 
   for (int row_tile = row_tile0; (int64_t)row_tile * 32 < columns; row_tile += a.n_row_tiles) {
     const int64_t n = (int64_t)row_tile * 32 + col;
@@ -234,19 +239,20 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
       }
       if (k0 + kWaves * RUN < end_key) fetch(k0 + kWaves * RUN);
       __builtin_amdgcn_wave_barrier();
+      constexpr int NV = RUN / 16 * NB;
+      auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
+      auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
       f32x16_t s[1];
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
-#pragma unroll
-      for (int st = 0; st < STEPS; ++st) s[0] = mma32(Tile::rows(own, 0, st, lane), q[st], s[0]);
+      u32x4_t f[kAhead];
+      read_ahead<STEPS>(f, keys);
+      products<STEPS>(f, keys, [&](int i, u32x4_t k) { s[0] = mma32(k, q[i], s[0]); });
+      read_ahead<NV>(f, values);
       if (k0 + RUN > first_hidden) hide_rows(s[0], limit - k0 - 4 * half);
       softmax_step(s, a.scale_log2, ref, sum, acc);
-#pragma unroll
-      for (int st = 0; st < RUN / 16; ++st) {
-        const u32x4_t p = acc_operand(s[0], st);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(own + TILE_BYTES, 16 * st, b, lane), p, acc[b]);
-      }
+      const u32x4_t p[2] = {acc_operand(s[0], 0), acc_operand(s[0], 1)};
+      products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, p[i / NB], acc[i % NB]); });
       __builtin_amdgcn_wave_barrier();
     }
     // join the four waves: each scales its output to the common maximum, then the block adds them in wave order

@@ -28,7 +28,7 @@ struct GradArgs {
 constexpr int kKeys = 64;              // keys per tile of grad_query_kernel
 constexpr int kRows = kWaves * 32;     // queries (keys) that a block keeps
 constexpr int kQueries = 32;           // queries per tile of grad_key_kernel
-constexpr int64_t kKeyBlocks = 512;    // blocks that grad_key_kernel's work is cut for
+constexpr int64_t kKeyBlocks = 2048;    // blocks that grad_key_kernel's work is cut for
 
 template <int DP, bool WHOLE, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs a) {
@@ -102,6 +102,11 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
       for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
 
     const int n_key_tiles = (end + kKeys - 1) / kKeys;
+    if constexpr (WHOLE) {
+      arrived(q);
+      arrived(g);
+      asm volatile("" : "+v"(lse2), "+v"(delta));
+    }
     __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
     if (n_key_tiles > 0) load.fetch(0, 0);
     for (int kt = 0; kt < n_key_tiles; ++kt) {
@@ -109,27 +114,28 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
       load.settle(kt & 1);
       __syncthreads();
       if (kt + 1 < n_key_tiles) load.fetch((kt + 1) & 1, k0 + kKeys);
-      const unsigned char* k_tile = smem[kt & 1];
-      const unsigned char* v_tile = k_tile + TILE_BYTES;
       if (k0 < wave_end) {
+        const uint32_t k_tile = load.lds + (uint32_t)(kt & 1) * 2 * TILE_BYTES;
+        const uint32_t row_at = k_tile + Tile::row_base(lane), column_at = k_tile + Tile::column_base(lane);
 #pragma unroll
         for (int kb = 0; kb < kKeys / 32; ++kb) {
+          auto rows_of = [&](int i) { return Tile::rows(row_at + i % 2 * TILE_BYTES, 32 * kb, i / 2); };
+          auto columns_of = [&](int i) { return Tile::columns(column_at, 32 * kb + i / NB * 16, i % NB); };
           f32x16_t s, dp;
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
-          for (int st = 0; st < STEPS; ++st) s = mma32(Tile::rows(k_tile, 32 * kb, st, lane), q[st], s);
-#pragma unroll
-          for (int st = 0; st < STEPS; ++st) dp = mma32(Tile::rows(v_tile, 32 * kb, st, lane), g[st], dp);
+          u32x4_t f[kAhead];
+          read_ahead<2 * STEPS>(f, rows_of);
+          products<2 * STEPS>(f, rows_of, [&](int i, u32x4_t x) {
+            if (i % 2 == 0) s = mma32(x, q[i / 2], s);
+            else dp = mma32(x, g[i / 2], dp);
+          });
+          read_ahead<2 * NB>(f, columns_of);
           if (k0 + 32 * kb + 32 > first_hidden) hide_rows(s, limit - k0 - 32 * kb - 4 * half);
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], a.scale_log2, -lse2)) * (dp[r] - delta);
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            const u32x4_t ds = acc_operand(s, st);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) acc[b] = mma32(Tile::columns(k_tile, 32 * kb + 16 * st, b, lane), ds, acc[b]);
-          }
+          const u32x4_t ds[2] = {acc_operand(s, 0), acc_operand(s, 1)};
+          products<2 * NB>(f, columns_of, [&](int i, u32x4_t x) { acc[i % NB] = mma32(x, ds[i / NB], acc[i % NB]); });
         }
       }
     }
@@ -162,6 +168,10 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kQueries * Tile::kRowBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of queries and dO
   __shared__ __attribute__((aligned(16))) float rows[2][2][kQueries];               // ... and of lse (base 2) and D
+  // Heads of 128 elements: the keys' operands stay in LDS, each wave's its own, since 64 registers of keys and values beside 160 of
+  // sums leave too few for two waves a SIMD (65 were spilled: 638 us for the text case's kernel, 420 of the same with none).
+  constexpr bool KEEP = DP == 128;
+  __shared__ __attribute__((aligned(1024))) unsigned char kept[KEEP ? kRows * Tile::kRowBytes : 16];
   TilePlace at;
   if (!tile_place(a.c.B, a.c.Hkv, a.n_chunks, a.n_k_tiles, false, &at)) return;
   const int chunk = at.sub;
@@ -191,9 +201,12 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
     const bf16_t* k_row = a.c.K.p + tok * a.c.K.token + at.kv_head * a.c.K.head;
     const bf16_t* v_row = a.c.V.p + tok * a.c.V.token + at.kv_head * a.c.V.head;
     u32x4_t k[STEPS], v[STEPS];
+    unsigned char* own = kept + wave * 32 * Tile::kRowBytes;
+    const uint32_t kept_tile = NM_LDS_ADDRESS(kept) + wave * 32 * Tile::kRowBytes;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
       k[st] = load_piece<ALIGNED>(k_row, 16 * st + 8 * half, D, kj < sk.len);
+      if constexpr (KEEP) *reinterpret_cast<u32x4_t*>(own + Tile::place(lane & 31, 2 * st + half)) = k[st];
       v[st] = load_piece<ALIGNED>(v_row, 16 * st + 8 * half, D, kj < sk.len);
     }
     f32x16_t dk[NB], dv[NB];
@@ -211,20 +224,25 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
     auto fetch = [&](int stage) {
       load.base[0] = a.c.Q.p + sq.first * a.c.Q.token + head * a.c.Q.head;
       load.base[1] = a.c.dO.p + sq.first * a.c.dO.token + head * a.c.dO.head;
-      if (tid < 2 * kQueries) {
-        const int row = q0 + tid % kQueries;
-        const int64_t n = (int64_t)head * a.c.Tq + sq.first + row;
-        // (no row: a log-sum of infinity, and so probabilities of zero)
-        row_in = row >= sq.len ? (tid < kQueries ? -kMinusInf : 0.f) : tid < kQueries ? a.c.lse[n] * kLog2e : a.delta[n];
-        if (row_in == kMinusInf) row_in = 0.f;
+      if (tid < 2 * kQueries) {  // (looked at when it is stored, a step later)
+        const int row = q0 + tid % kQueries, there = row < sq.len ? row : sq.len - 1;
+        row_in = (tid < kQueries ? a.c.lse : a.delta)[(int64_t)head * a.c.Tq + sq.first + there];
       }
       load.fetch(stage, q0);
     };
+    if constexpr (WHOLE) {
+      if constexpr (!KEEP) arrived(k);
+      arrived(v);
+    }
     __syncthreads();  // (a block's second key tile)
     if (first_step < end_step) fetch(0);
     for (int step = first_step; step < end_step; ++step) {
       const int stage = (step - first_step) & 1, q_now = q0;
-      if (tid < 2 * kQueries) rows[stage][tid / kQueries][tid % kQueries] = row_in;
+      if (tid < 2 * kQueries) {
+        // no row: a log-sum of infinity, and so probabilities of zero; a query that sees no key: any finite one
+        const float lse2 = q_now + tid >= sq.len ? -kMinusInf : row_in == kMinusInf ? 0.f : row_in * kLog2e;
+        rows[stage][tid / kQueries][tid % kQueries] = tid < kQueries ? lse2 : row_in;
+      }
       load.settle(stage);
       __syncthreads();
       if (step + 1 < end_step) {
@@ -232,20 +250,41 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
         if (q0 >= sq.len) { q0 = list.first_q; ++head; }
         fetch(stage ^ 1);
       }
-      const unsigned char* q_tile = smem[stage];
-      const unsigned char* g_tile = q_tile + TILE_BYTES;
       // (a wave whose keys none of these queries sees, or without keys)
       if (k_wave < sk.len && (!a.c.causal || q_now + kQueries - 1 + shift >= k_wave)) {
+        const uint32_t q_tile = load.lds + (uint32_t)stage * 2 * TILE_BYTES;
+        int now = lane;
+        if constexpr (KEEP) asm volatile("" : "+v"(now));  // (addresses are computed here: held over the loop they would be spilled)
+        const uint32_t row_at = q_tile + Tile::row_base(now), column_at = q_tile + Tile::column_base(now);
+        // products in pairs: scores and dO V, then dV and dK
+        auto rows_of = [&](int i) { return Tile::rows(row_at + i % 2 * TILE_BYTES, 0, i / 2); };
+        auto columns_of = [&](int i) { return Tile::columns(column_at + (1 - i % 2) * TILE_BYTES, i / 2 / NB * 16, i / 2 % NB); };
         f32x16_t s, dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) s = mma32(Tile::rows(q_tile, 0, st, lane), k[st], s);
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) dp = mma32(Tile::rows(g_tile, 0, st, lane), v[st], dp);
+        u32x4_t f[kAhead];
+        read_ahead<2 * STEPS>(f, rows_of);
+        if constexpr (KEEP) {
+          const uint32_t kept_at = kept_tile + Tile::row_base(now);
+          u32x4_t kf[2] = {Tile::rows(kept_at, 0, 0), Tile::rows(kept_at, 0, 1)};
+          products<2 * STEPS>(f, rows_of, [&](int i, u32x4_t x) {
+            if (i % 2 == 0) {
+              s = mma32(x, kf[i / 2 % 2], s);
+              if (i / 2 + 2 < STEPS) kf[i / 2 % 2] = Tile::rows(kept_at, 0, i / 2 + 2);
+            } else {
+              dp = mma32(x, v[i / 2], dp);
+            }
+          });
+        } else {
+          products<2 * STEPS>(f, rows_of, [&](int i, u32x4_t x) {
+            if (i % 2 == 0) s = mma32(x, k[i / 2], s);
+            else dp = mma32(x, v[i / 2], dp);
+          });
+        }
+        read_ahead<4 * NB>(f, columns_of);
         const float* row = rows[stage][0] + 4 * half;
         if (a.c.causal && q_now + shift < k_wave + 31) {
-          const int first = kj - shift - q_now - 4 * half;  // rows before it do not see the lane's key
+          const int first = k_wave + (now & 31) - shift - q_now - 4 * (now >> 5);  // rows before it do not see the lane's key
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = acc_row(r) >= first ? s[r] : kMinusInf;
         }
@@ -260,15 +299,12 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
             dp[r] = s[r] * (dp[r] - delta[e]);
           }
         }
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const u32x4_t p = acc_operand(s, st), ds = acc_operand(dp, st);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            dv[b] = mma32(Tile::columns(g_tile, 16 * st, b, lane), p, dv[b]);
-            dk[b] = mma32(Tile::columns(q_tile, 16 * st, b, lane), ds, dk[b]);
-          }
-        }
+        const u32x4_t p[2] = {acc_operand(s, 0), acc_operand(s, 1)}, ds[2] = {acc_operand(dp, 0), acc_operand(dp, 1)};
+        products<4 * NB>(f, columns_of, [&](int i, u32x4_t x) {
+          const int b = i / 2 % NB, st = i / 2 / NB;
+          if (i % 2 == 0) dv[b] = mma32(x, p[st], dv[b]);
+          else dk[b] = mma32(x, ds[st], dk[b]);
+        });
       }
     }
     if (list.chunks > 1) {
