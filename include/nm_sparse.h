@@ -536,7 +536,6 @@ int32_t nm_pack_prepare_batched(const nm_layer_desc* descs, int32_t count, void*
  *                are added in a fixed order: results repeat bit for bit); NULL allowed when that size is 0 or dweight is
  *                NULL.  Contents undefined afterwards; concurrent calls need distinct workspaces.
  * Errors: as above, and NM_ERR_WORKSPACE.
- * C % 8 == 0, 16-byte aligned matrices and leading dimensions that are multiples of 8 run with wide accesses.
  */
 int32_t nm_layer_norm(const void* X, int64_t ldx, int32_t x_dtype, const void* R, int64_t ldr, int64_t T, int64_t C,
                       const float* weight, const float* bias, float eps, void* Y, int64_t ldy, int32_t y_dtype, void* S,
@@ -557,7 +556,7 @@ int32_t nm_layer_norm_backward(const void* dY, int64_t lddy, int32_t dy_dtype, c
  *   Y  out  the same with y_token, y_head and y_dtype; may be X itself (same type and strides)
  *   positions  in  [T, axes] contiguous: int32 (positions_f32 == 0) or float
  *   freqs   in   float [rotated / 2]        sections  HOST array of `axes` numbers >= 0 whose sum is rotated / 2
- * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0 or above 2^31, H or D above 2^20, rotated odd, <= 0 or above D, axes outside [1, 4],
+ * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0 or above 2^31, H * D above 2^20, rotated odd, <= 0 or above D, axes outside [1, 4],
  * a sum of sections other than rotated / 2, negative strides, tokens or heads of Y that overlap), NM_ERR_DTYPE, NM_ERR_ALIGN,
  * NM_ERR_DEVICE.
  */
@@ -600,7 +599,7 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (Tq <= 0, Tk < 0, either above 2^30; sequences outside [1, 65535], heads_q no multiple of heads_kv,
  * sequences * heads_q above 2^20, head_size outside [1, 128], max_q, max_k < 0, negative strides, tokens or heads of an output that
  * overlap, scale not positive and finite), NM_ERR_ALIGN, NM_ERR_WORKSPACE, NM_ERR_DEVICE.
- * head_size % 8 == 0, 16-byte aligned tensors and strides that are multiples of 8 run with wide accesses.
+ * Heads of 32, 64 or 128 elements in 16-byte aligned tensors whose strides are multiples of 8 are fastest.
  */
 typedef struct nm_heads {
   nm_bf16* data;  /* inputs are only read */

@@ -601,7 +601,7 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
                   int64_t rotated, int32_t interleaved, int32_t inverse, void* Y, int32_t y_dtype, int64_t y_token,
                   int64_t y_head, void* stream) {
   if (!X || !Y || !positions || !freqs || !sections) return NM_ERR_NULL;
-  if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 1 << 20) return NM_ERR_SHAPE;
+  if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 1 << 20 || H * D > 1 << 20) return NM_ERR_SHAPE;
   if (rotated <= 0 || rotated > D || rotated % 2 || axes < 1 || axes > nm::kMaxRotaryAxes) return NM_ERR_SHAPE;
   if (!strides_ok(T, H, D, x_token, x_head, false) || !strides_ok(T, H, D, y_token, y_head, true)) return NM_ERR_SHAPE;
   nm::RotaryCall c;

@@ -13,6 +13,7 @@
 
 #include "nm_launch.h"
 #include "nm_mma.h"
+#include "nm_rows.h"
 
 #include <type_traits>
 
@@ -114,18 +115,11 @@ struct RowTile {
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 
-// Eight elements of a row, zeros past element D or where `there` is false.  ALIGNED: rows are whole 16-byte pieces.
-template <bool ALIGNED>
+// Eight elements of a row, zeros past element D or where `there` is false.  Any alignment.
 __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, bool there) {
-  u32x4_t v = {0, 0, 0, 0};
-  if constexpr (ALIGNED) {
-    if (there && d < D) v = *reinterpret_cast<const u32x4_t*>(row + d);
-  } else if (there) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (d + e < D) v[e / 2] |= (uint32_t)row[d + e] << (16 * (e & 1));
-  }
-  return v;
+  Raw8<false> r;
+  r.load(row, d, there ? D - d : 0);
+  return r.v[0];
 }
 
 // Two tiles of ROWS rows (of keys and values, or of queries and dO) from memory to LDS, by a block of kThreads lanes.
@@ -134,7 +128,7 @@ __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, b
 // and the last element.
 //   fetch(stage, row0)   starts the loads of a tile (rows row0 ..)
 //   settle(stage)        the tile is in LDS, as far as this wave brought it: a barrier follows
-template <int DP, int ROWS, bool WHOLE, bool ALIGNED>
+template <int DP, int ROWS, bool WHOLE>
 struct TilePair {
   using Tile = RowTile<DP>;
   static constexpr int kBytes = ROWS * Tile::kRowBytes, kPieces = ROWS * Tile::kPieces;
@@ -173,7 +167,7 @@ struct TilePair {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
           const int i = n * kThreads + tid, row = row0 + i / Tile::kPieces;
-          in[t][n] = load_piece<ALIGNED>(base[t] + (int64_t)row * stride[t], i % Tile::kPieces * 8, D,
+          in[t][n] = load_piece(base[t] + (int64_t)row * stride[t], i % Tile::kPieces * 8, D,
                                          row < rows && (kPieces % kThreads == 0 || i < kPieces));
         }
     }
@@ -196,6 +190,9 @@ struct TilePair {
 };
 // WHOLE tiles address their rows by 32-bit offsets
 constexpr int64_t kMostStride = (int64_t)1 << 24;
+inline bool whole_rows(const HeadRows& r) {
+  return ((uintptr_t)r.p & 15) == 0 && (r.token | r.head) % 8 == 0 && r.token <= kMostStride;
+}
 
 // Operands that a loop keeps have arrived.  The compiler, which does not see the asynchronous copies, would wait for them at their
 // first use in the loop, and there for all copies that have just been started, on every round.
@@ -211,8 +208,19 @@ __device__ __forceinline__ u32x4_t acc_operand(const f32x16_t& p, int s) {
                  pack_bf16x2(p[8 * s + 4], p[8 * s + 5]), pack_bf16x2(p[8 * s + 6], p[8 * s + 7])};
 }
 
+// Four elements of a row of D from element d on, of which those from D on are not stored.  Any alignment.
+__device__ __forceinline__ void store4(bf16_t* row, int d, int D, uint32_t lo, uint32_t hi) {
+  if (d + 4 <= D) {
+    *reinterpret_cast<u32x2_any_t*>(row + d) = u32x2_any_t{lo, hi};
+  } else {
+    if (d < D) row[d] = (bf16_t)lo;
+    if (d + 1 < D) row[d + 1] = (bf16_t)(lo >> 16);
+    if (d + 2 < D) row[d + 2] = (bf16_t)hi;
+  }
+}
+
 // One column of a transposed product (DP / 32 accumulators: the elements of one row of the output) to memory, times `by`.
-template <int DP, bool ALIGNED>
+template <int DP>
 __device__ __forceinline__ void store_column(bf16_t* row, const f32x16_t (&acc)[DP / 32], int lane, int D, float by) {
   const int h = lane >> 5;
 #pragma unroll
@@ -220,16 +228,7 @@ __device__ __forceinline__ void store_column(bf16_t* row, const f32x16_t (&acc)[
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int d = 32 * b + 8 * q + 4 * h;
-      const uint32_t lo = pack_bf16x2(acc[b][4 * q] * by, acc[b][4 * q + 1] * by);
-      const uint32_t hi = pack_bf16x2(acc[b][4 * q + 2] * by, acc[b][4 * q + 3] * by);
-      if constexpr (ALIGNED) {
-        if (d < D) *reinterpret_cast<uint2*>(row + d) = uint2{lo, hi};
-      } else {
-        if (d < D) row[d] = (bf16_t)lo;
-        if (d + 1 < D) row[d + 1] = (bf16_t)(lo >> 16);
-        if (d + 2 < D) row[d + 2] = (bf16_t)hi;
-        if (d + 3 < D) row[d + 3] = (bf16_t)(hi >> 16);
-      }
+      store4(row, d, D, pack_bf16x2(acc[b][4 * q] * by, acc[b][4 * q + 1] * by), pack_bf16x2(acc[b][4 * q + 2] * by, acc[b][4 * q + 3] * by));
     }
 }
 
@@ -282,13 +281,12 @@ constexpr int64_t kMostBlocks = (int64_t)1 << 24;
 inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-// calls f(padded head size, WHOLE, ALIGNED) as integral constants
+// calls f(padded head size, WHOLE) as integral constants; whole: what is loaded by tiles has aligned rows of short strides
 template <class F>
-void with_head(int D, bool aligned, bool short_strides, F&& f) {
+void with_head(int D, bool whole, F&& f) {
   auto sized = [&](auto dp) {
-    if (!aligned) f(dp, std::false_type{}, std::false_type{});
-    else if (D == decltype(dp)::value && short_strides) f(dp, std::true_type{}, std::true_type{});
-    else f(dp, std::false_type{}, std::true_type{});
+    if (whole && D == decltype(dp)::value) f(dp, std::true_type{});
+    else f(dp, std::false_type{});
   };
   if (D <= 32) sized(std::integral_constant<int, 32>{});
   else if (D <= 64) sized(std::integral_constant<int, 64>{});
@@ -297,7 +295,6 @@ void with_head(int D, bool aligned, bool short_strides, F&& f) {
 
 #define NM_LDS_ADDRESS(p) ((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(p))
 
-inline bool head_rows_aligned(const HeadRows& r) { return ((uintptr_t)r.p & 15) == 0 && (r.token | r.head) % 8 == 0; }
 
 }  // namespace nm
 

@@ -66,7 +66,7 @@ __device__ __forceinline__ void softmax_step(f32x16_t (&s)[KB], float c, float& 
 constexpr int kKeys = 64;             // per tile
 constexpr int kQueries = kWaves * 32; // per block
 
-template <int DP, bool WHOLE, bool ALIGNED>
+template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;  // causal: query i sees keys up to i + shift
-  TilePair<DP, kKeys, WHOLE, ALIGNED> load;
+  TilePair<DP, kKeys, WHOLE> load;
   load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
   load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
   load.stride[0] = a.c.K.token;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
     u32x4_t q[STEPS];
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) q[st] = load_piece<ALIGNED>(q_row, 16 * st + 8 * half, D, live);
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
 
     // keys that any query of the block, of the wave, and this lane's sees
     const int last_q = (tile + 1) * kQueries < sq.len ? (tile + 1) * kQueries : sq.len;
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     sum = half_sum(sum);
     if (live) {
       bf16_t* o_row = a.c.O.p + (sq.first + qi) * a.c.O.token + head * a.c.O.head;
-      store_column<DP, ALIGNED>(o_row, acc, lane, D, sum == 0.f ? 0.f : 1.f / sum);
+      store_column<DP>(o_row, acc, lane, D, sum == 0.f ? 0.f : 1.f / sum);
       if (a.c.lse != nullptr && half == 0)
         a.c.lse[(int64_t)head * a.c.Tq + sq.first + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
     }
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
 
 // Few queries.  Column n of a row tile is query (32 tile + n) / group of the sequence and head (32 tile + n) % group of the
 // key head's group.  Each wave takes every fourth run of 32 keys of the block's chunk through LDS of its own.
-template <int DP, bool ALIGNED>
+template <int DP>
 __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, RUN = 32, TILE_BYTES = RUN * Tile::kRowBytes;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
     const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
     u32x4_t q[STEPS];
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) q[st] = load_piece<ALIGNED>(q_row, 16 * st + 8 * half, D, live);
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
     int limit = end_key, first_hidden = end_key;
     if (a.c.causal) {
       const int sees = qi + shift + 1, first_sees = row_tile * 32 / a.group + shift + 1;
@@ -223,8 +223,8 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int at = i * 64 + lane, row = k0 + at / Tile::kPieces, d = at % Tile::kPieces * 8;
-        k_in[i] = load_piece<ALIGNED>(Kh + (int64_t)row * a.c.K.token, d, D, row < end_key);
-        v_in[i] = load_piece<ALIGNED>(Vh + (int64_t)row * a.c.V.token, d, D, row < end_key);
+        k_in[i] = load_piece(Kh + (int64_t)row * a.c.K.token, d, D, row < end_key);
+        v_in[i] = load_piece(Vh + (int64_t)row * a.c.V.token, d, D, row < end_key);
       }
     };
     __syncthreads();  // (a further row tile: what the waves joined has been read)
@@ -297,16 +297,7 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].x == kMinusInf ? 0.f : wave_ml[w][c].y * fast_exp2(wave_ml[w][c].x - t);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16_t* out = a.c.O.p + tok * a.c.O.token + hd * a.c.O.head + d;
-        const uint32_t lo = pack_bf16x2(o.x * inv, o.y * inv), hi = pack_bf16x2(o.z * inv, o.w * inv);
-        if constexpr (ALIGNED) {
-          *reinterpret_cast<uint2*>(out) = uint2{lo, hi};
-        } else {
-          out[0] = (bf16_t)lo;
-          if (d + 1 < D) out[1] = (bf16_t)(lo >> 16);
-          if (d + 2 < D) out[2] = (bf16_t)hi;
-          if (d + 3 < D) out[3] = (bf16_t)(hi >> 16);
-        }
+        store4(a.c.O.p + tok * a.c.O.token + hd * a.c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
       } else {
         *reinterpret_cast<float4*>(a.part_o + ((tok * a.c.Hq + hd) * a.n_chunks + chunk) * DP + d) = o;
       }
@@ -391,8 +382,6 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
   a.c = c;
   a.group = c.Hq / c.Hkv;
   a.scale_log2 = c.scale * kLog2e;
-  const bool aligned = c.D % 8 == 0 && head_rows_aligned(c.Q) && head_rows_aligned(c.K) && head_rows_aligned(c.V) &&
-                       head_rows_aligned(c.O);
   const CachePlan plan = cache_plan(c.B, c.Hkv, a.group, c.max_q, c.max_k);
   a.chunk = plan.chunk; a.n_chunks = plan.n_chunks; a.n_row_tiles = plan.n_row_tiles;
   a.n_tiles = (int)((c.max_q + kQueries - 1) / kQueries);
@@ -404,21 +393,21 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) +
                                           round256(columns * padded_head(c.D) * sizeof(float)));
   }
-  auto launch = [&](auto dp, auto whole, auto al) {
+  auto launch = [&](auto dp, auto whole) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool WHOLE = decltype(whole)::value, ALIGNED = decltype(al)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
     if (plan.taken) {
       const int64_t blocks = (int64_t)a.n_chunks * a.n_row_tiles * c.B * c.Hkv;
-      cache_kernel<DP, ALIGNED><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
+      cache_kernel<DP><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
       if (a.n_chunks > 1) {
         const dim3 join((unsigned)((c.max_q * c.Hq + kWaves - 1) / kWaves), (unsigned)c.B);
         cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
       }
     } else {
-      prompt_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
+      prompt_kernel<DP, WHOLE><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
     }
   };
-  with_head(c.D, aligned, c.K.token <= kMostStride && c.V.token <= kMostStride, launch);
+  with_head(c.D, whole_rows(c.K) && whole_rows(c.V), launch);
   return hipGetLastError();
 }
 

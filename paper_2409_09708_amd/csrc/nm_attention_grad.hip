@@ -30,7 +30,7 @@ constexpr int kRows = kWaves * 32;     // queries (keys) that a block keeps
 constexpr int kQueries = 32;           // queries per tile of grad_key_kernel
 constexpr int64_t kKeyBlocks = 2048;    // blocks that grad_key_kernel's work is cut for
 
-template <int DP, bool WHOLE, bool ALIGNED>
+template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
-  TilePair<DP, kKeys, WHOLE, ALIGNED> load;
+  TilePair<DP, kKeys, WHOLE> load;
   load.base[0] = a.c.K.p + sk.first * a.c.K.token + at.kv_head * a.c.K.head;
   load.base[1] = a.c.V.p + sk.first * a.c.V.token + at.kv_head * a.c.V.head;
   load.stride[0] = a.c.K.token;
@@ -66,9 +66,9 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
     float delta = 0.f;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
-      q[st] = load_piece<ALIGNED>(q_row, 16 * st + 8 * half, D, live);
-      g[st] = load_piece<ALIGNED>(do_row, 16 * st + 8 * half, D, live);
-      const u32x4_t o = load_piece<ALIGNED>(o_row, 16 * st + 8 * half, D, live);
+      q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+      g[st] = load_piece(do_row, 16 * st + 8 * half, D, live);
+      const u32x4_t o = load_piece(o_row, 16 * st + 8 * half, D, live);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         delta = fmaf(__uint_as_float(g[st][e] << 16), __uint_as_float(o[e] << 16), delta);
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
         }
       }
     }
-    if (live) store_column<DP, ALIGNED>(a.c.dQ.p + tok * a.c.dQ.token + head * a.c.dQ.head, acc, lane, D, a.c.scale);
+    if (live) store_column<DP>(a.c.dQ.p + tok * a.c.dQ.token + head * a.c.dQ.head, acc, lane, D, a.c.scale);
   }
 }
 
@@ -162,7 +162,7 @@ __device__ __forceinline__ KeySteps key_steps(const GradArgs& a, int tile, int q
   return s;
 }
 
-template <int DP, bool WHOLE, bool ALIGNED>
+template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_key_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kQueries * Tile::kRowBytes;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
-  TilePair<DP, kQueries, WHOLE, ALIGNED> load;
+  TilePair<DP, kQueries, WHOLE> load;
   load.stride[0] = a.c.Q.token;
   load.stride[1] = a.c.dO.token;
   load.rows = sq.len;
@@ -205,9 +205,9 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
     const uint32_t kept_tile = NM_LDS_ADDRESS(kept) + wave * 32 * Tile::kRowBytes;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
-      k[st] = load_piece<ALIGNED>(k_row, 16 * st + 8 * half, D, kj < sk.len);
+      k[st] = load_piece(k_row, 16 * st + 8 * half, D, kj < sk.len);
       if constexpr (KEEP) *reinterpret_cast<u32x4_t*>(own + Tile::place(lane & 31, 2 * st + half)) = k[st];
-      v[st] = load_piece<ALIGNED>(v_row, 16 * st + 8 * half, D, kj < sk.len);
+      v[st] = load_piece(v_row, 16 * st + 8 * half, D, kj < sk.len);
     }
     f32x16_t dk[NB], dv[NB];
 #pragma unroll
@@ -325,8 +325,8 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
 #pragma unroll
           for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.f;
       }
-      store_column<DP, ALIGNED>(a.c.dK.p + tok * a.c.dK.token + at.kv_head * a.c.dK.head, dk, lane, D, a.c.scale);
-      store_column<DP, ALIGNED>(a.c.dV.p + tok * a.c.dV.token + at.kv_head * a.c.dV.head, dv, lane, D, 1.f);
+      store_column<DP>(a.c.dK.p + tok * a.c.dK.token + at.kv_head * a.c.dK.head, dk, lane, D, a.c.scale);
+      store_column<DP>(a.c.dV.p + tok * a.c.dV.token + at.kv_head * a.c.dV.head, dv, lane, D, 1.f);
     }
   }
 }
@@ -416,18 +416,14 @@ hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s) {
   a.n_k_tiles = tiles(c.max_k, c.B, c.Hkv, a.n_chunks);
   a.delta = static_cast<float*>(c.workspace);
   a.part = a.delta + round256((size_t)c.Tq * c.Hq * sizeof(float)) / sizeof(float);
-  const bool aligned = c.D % 8 == 0 && head_rows_aligned(c.Q) && head_rows_aligned(c.K) && head_rows_aligned(c.V) &&
-                       head_rows_aligned(c.O) && head_rows_aligned(c.dO) && head_rows_aligned(c.dQ) &&
-                       head_rows_aligned(c.dK) && head_rows_aligned(c.dV);
-  const bool short_strides = c.K.token <= kMostStride && c.V.token <= kMostStride && c.Q.token <= kMostStride && c.dO.token <= kMostStride;
-  with_head(c.D, aligned, short_strides, [&](auto dp, auto whole, auto al) {
+  with_head(c.D, whole_rows(c.K) && whole_rows(c.V) && whole_rows(c.Q) && whole_rows(c.dO), [&](auto dp, auto whole) {
     constexpr int DP = decltype(dp)::value;
-    constexpr bool WHOLE = decltype(whole)::value, ALIGNED = decltype(al)::value;
+    constexpr bool WHOLE = decltype(whole)::value;
     const int64_t q_blocks = tile_blocks(c.B, c.Hkv, a.group, a.n_q_tiles);
-    grad_query_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)q_blocks), kThreads, 0, s>>>(a);
+    grad_query_kernel<DP, WHOLE><<<dim3((unsigned)q_blocks), kThreads, 0, s>>>(a);
     if (c.Tk == 0) return;
     const int64_t k_blocks = tile_blocks(c.B, c.Hkv, a.n_chunks, a.n_k_tiles);
-    grad_key_kernel<DP, WHOLE, ALIGNED><<<dim3((unsigned)k_blocks), kThreads, 0, s>>>(a);
+    grad_key_kernel<DP, WHOLE><<<dim3((unsigned)k_blocks), kThreads, 0, s>>>(a);
     if (a.n_chunks > 1) {
       constexpr int PER_BLOCK = kThreads / (2 * DP / 4);
       int64_t blocks = (c.max_k * c.Hkv + PER_BLOCK - 1) / PER_BLOCK;

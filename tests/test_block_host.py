@@ -45,14 +45,15 @@ def norm_backward(lib, **kw):
     (dict(dY=None), NULL), (dict(S=None), NULL), (dict(stats=None), NULL), (dict(dX=None), NULL), (dict(dw=None), NULL), (dict(db=None), NULL),
     (dict(T=0), SHAPE), (dict(C=-4), SHAPE), (dict(lddy=63), SHAPE), (dict(lds=63), SHAPE), (dict(lddx=63), SHAPE),
     (dict(dS=FAKE, ldds=1), SHAPE), (dict(yt=2), DTYPE), (dict(st=3), DTYPE), (dict(xt=-1), DTYPE), (dict(stats=FAKE + 4), ALIGN),
-    (dict(dX=FAKE + 2), ALIGN), (dict(dw=FAKE + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(bytes=16), WORKSPACE), (dict(ws=FAKE + 64), WORKSPACE)])
+    (dict(dX=FAKE + 2), ALIGN), (dict(dw=FAKE + 2), ALIGN), (dict(T=999, ws=None), WORKSPACE), (dict(T=999, bytes=16), WORKSPACE),
+    (dict(T=999, ws=FAKE + 64), WORKSPACE)])
 def test_layer_norm_backward_refusals(lib, kw, status):
     assert norm_backward(lib, **kw) == status
 
 
 def test_layer_norm_backward_workspace(lib):
     size = lib.nm_layer_norm_backward_workspace_bytes
-    assert size(1, 768) == 0 and size(0, 768) == 0 and size(8, 0) == 0
+    assert size(4, 768) == 0 and size(0, 768) == 0 and size(8, 0) == 0
     assert size(50432, 768) == size(200000, 768) > 0
     assert size(50432, 768) % (2 * 768 * 4) == 0
 
