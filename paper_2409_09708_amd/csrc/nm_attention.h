@@ -122,17 +122,19 @@ __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, b
   return r.v[0];
 }
 
-// Two tiles of ROWS rows (of keys and values, or of queries and dO) from memory to LDS, by a block of kThreads lanes.
+// Two tiles of ROWS rows (of keys and values, or of queries and dO) from memory to LDS, by LANES lanes: a block of kThreads, or a
+// wave.
 // WHOLE (rows of exactly DP elements, all 16-byte aligned): asynchronous copies straight to LDS, one wave-load a kilobyte; rows past
 // the last one repeat it, so the scores of those have to be hidden.  Otherwise through registers, with zeros past the last row
 // and the last element.
-//   fetch(stage, row0)   starts the loads of a tile (rows row0 ..)
-//   settle(stage)        the tile is in LDS, as far as this wave brought it: a barrier follows
-template <int DP, int ROWS, bool WHOLE>
+//   fetch(stage, row0)   starts the loads of a tile (rows row0 .., one of them there at least)
+//   settle(stage)        the tile is in LDS, as far as this wave brought it, up to LATER copies started after it: a block's
+//                        barrier follows
+template <int DP, int ROWS, bool WHOLE, int LANES>
 struct TilePair {
   using Tile = RowTile<DP>;
   static constexpr int kBytes = ROWS * Tile::kRowBytes, kPieces = ROWS * Tile::kPieces;
-  static constexpr int kLoads = (kPieces + kThreads - 1) / kThreads;
+  static constexpr int kWide = LANES / 64, kLoads = (kPieces + LANES - 1) / LANES;
   const bf16_t* base[2];  // row 0 of the sequence and head
   int64_t stride[2];
   int rows, D;            // of the sequence
@@ -141,23 +143,23 @@ struct TilePair {
   u32x4_t in[WHOLE ? 1 : 2][WHOLE ? 1 : kLoads];
 
   __device__ __forceinline__ void fetch(int stage, int row0) {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x % LANES;
     if constexpr (WHOLE) {
-      const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+      const int wave = kWide == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
       const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (uint32_t)stage * 2 * kBytes);
       const int last = rows - 1 - row0;  // >= 0
-      if (kPieces % kThreads == 0 || wave * 64 < kPieces) {
+      if (kPieces % LANES == 0 || wave * 64 < kPieces) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const uniform_ptr_t from = make_uniform(base[t] + (int64_t)row0 * stride[t]);
           const uint32_t bytes = (uint32_t)stride[t] * 2;
 #pragma unroll
           for (int n = 0; n < kLoads; ++n) {
-            const int i = (n * kWaves + wave) * 64 + lane;
+            const int i = (n * kWide + wave) * 64 + lane;
             int row = i / Tile::kPieces;
             const int piece = (i % Tile::kPieces) ^ Tile::swizzle(row);
             row = row < last ? row : last;
-            dma16(from, (uint32_t)row * bytes + piece * 16, to + t * kBytes + (n * kWaves + wave) * 1024);
+            dma16(from, (uint32_t)row * bytes + piece * 16, to + t * kBytes + (n * kWide + wave) * 1024);
           }
         }
       }
@@ -166,23 +168,24 @@ struct TilePair {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-          const int i = n * kThreads + tid, row = row0 + i / Tile::kPieces;
+          const int i = n * LANES + tid, row = row0 + i / Tile::kPieces;
           in[t][n] = load_piece(base[t] + (int64_t)row * stride[t], i % Tile::kPieces * 8, D,
-                                         row < rows && (kPieces % kThreads == 0 || i < kPieces));
+                                row < rows && (kPieces % LANES == 0 || i < kPieces));
         }
     }
   }
+  template <int LATER = 0>
   __device__ __forceinline__ void settle(int stage) {
     if constexpr (WHOLE) {
-      wait_loads_outstanding<0>();
+      wait_loads_outstanding<LATER>();
     } else {
-      const int tid = threadIdx.x;
+      const int tid = threadIdx.x % LANES;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-          const int i = n * kThreads + tid;
-          if (kPieces % kThreads == 0 || i < kPieces)
+          const int i = n * LANES + tid;
+          if (kPieces % LANES == 0 || i < kPieces)
             *reinterpret_cast<u32x4_t*>(smem + (2 * stage + t) * kBytes + Tile::place(i / Tile::kPieces, i % Tile::kPieces)) = in[t][n];
         }
     }
@@ -239,23 +242,32 @@ __device__ __forceinline__ void hide_rows(f32x16_t& s, int limit) {
   for (int r = 0; r < 16; ++r) s[r] = acc_row(r) < limit ? s[r] : kMinusInf;
 }
 
-// Block -> (sequence, key head, head of its group, tile).  Consecutive blocks go to consecutive XCDs, each with an L2
-// of its own.  Where a head has many tiles, each XCD takes one of every eight of one key head after another, so that at any time
-// an L2 holds the keys of about one head, and the longest tiles of a causal mask come first (the last queries: `last_first`; the
-// first keys); which of the eight alternates in direction, or the first XCDs would get the longer ones every time.  Where a head has few tiles, XCD x takes all tiles of every eighth key head.
+// Block -> (sequence, key head, head of its group, tile).  Consecutive blocks go to consecutive XCDs, each with an L2 of its
+// own.  Where a head has few tiles, XCD x takes all tiles of every eighth key head.  Where it has many, each XCD takes one of
+// every eight: of one key head after another, so that at any time an L2 holds the keys of about one head, or, where tiles
+// differ in length (`longest_first`: causal), the longest of all heads first, since a kernel ends when its last tile does;
+// which of the eight alternates in direction, or the first XCDs would get the longer ones every time.  The last tiles come first
+// where `last_first` (under a causal mask the last queries see the most keys, and the first keys the most queries).
 constexpr int kManyTiles = 16;
 struct TilePlace {
   int seq, kv_head, sub, tile;
 };
-__device__ __forceinline__ bool tile_place(int sequences, int kv_heads, int group, int n_tiles, bool last_first, TilePlace* p) {
+__device__ __forceinline__ bool tile_place(int sequences, int kv_heads, int group, int n_tiles, bool last_first,
+                                           bool longest_first, TilePlace* p) {
   const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
   int unit, t;
   if (n_tiles >= kManyTiles) {
-    const int per_unit = (n_tiles + 7) / 8 * group;
-    unit = slot / per_unit;
-    const int round = slot % per_unit / group;
+    const int units = sequences * kv_heads, rounds = (n_tiles + 7) / 8;
+    int round;
+    if (longest_first) {
+      round = slot / (units * group);
+      unit = slot % (units * group) / group;
+    } else {
+      unit = slot / (rounds * group);
+      round = slot % (rounds * group) / group;
+    }
+    p->sub = slot % group;
     t = round * 8 + (round % 2 ? 7 - xcd : xcd);
-    p->sub = slot % per_unit % group;
     if (t >= n_tiles) return false;
   } else {
     const int per_unit = n_tiles * group;

@@ -72,15 +72,15 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of keys and values
   TilePlace at;
-  if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_tiles, true, &at)) return;
+  if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_tiles, true, a.c.causal, &at)) return;
   const int kv_head = at.kv_head, head = kv_head * a.group + at.sub, seq = at.seq;
-  const int D = a.c.D;
+  const int D = WHOLE ? DP : a.c.D;
   const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
   const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;  // causal: query i sees keys up to i + shift
-  TilePair<DP, kKeys, WHOLE> load;
+  TilePair<DP, kKeys, WHOLE, kThreads> load;
   load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
   load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
   load.stride[0] = a.c.K.token;
@@ -95,10 +95,6 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     const int qi = q_wave + (lane & 31);
     const bool live = qi < sq.len;
     const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
-    u32x4_t q[STEPS];
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-
     // keys that any query of the block, of the wave, and this lane's sees
     const int last_q = (tile + 1) * kQueries < sq.len ? (tile + 1) * kQueries : sq.len;
     int end = sk.len, wave_end = sk.len, first_hidden = sk.len, limit = sk.len;
@@ -119,9 +115,12 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     float ref = kMinusInf, sum = 0.f;
 
     const int n_key_tiles = (end + kKeys - 1) / kKeys;
-    if constexpr (WHOLE) arrived(q);
     __syncthreads();  // (a block's second query tile: the first one's keys are no longer read)
     if (n_key_tiles > 0) load.fetch(0, 0);
+    u32x4_t q[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+    if constexpr (WHOLE) arrived(q);
     for (int kt = 0; kt < n_key_tiles; ++kt) {
       const int k0 = kt * kKeys;
       load.settle(kt & 1);
@@ -131,7 +130,9 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
         const uint32_t k_tile = load.lds + (uint32_t)(kt & 1) * 2 * TILE_BYTES, v_tile = k_tile + TILE_BYTES;
         const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
         constexpr int NS = kKeys / 32 * STEPS, NV = kKeys / 16 * NB;
-        auto keys = [&](int i) { return Tile::rows(k_at, i / STEPS * 32, i % STEPS); };
+        // (products on the same sums wait for each other: the two runs of keys in turn)
+        constexpr int KB = kKeys / 32;
+        auto keys = [&](int i) { return Tile::rows(k_at, i % KB * 32, i / KB); };
         auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
         f32x16_t s[kKeys / 32];
 #pragma unroll
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
           for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
         u32x4_t f[kAhead];
         read_ahead<NS>(f, keys);
-        products<NS>(f, keys, [&](int i, u32x4_t k) { s[i / STEPS] = mma32(k, q[i % STEPS], s[i / STEPS]); });
+        products<NS>(f, keys, [&](int i, u32x4_t k) { s[i % KB] = mma32(k, q[i / KB], s[i % KB]); });
         read_ahead<NV>(f, values);
         if (k0 + kKeys > first_hidden) {
 #pragma unroll
@@ -165,13 +166,13 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
 
 // Few queries.  Column n of a row tile is query (32 tile + n) / group of the sequence and head (32 tile + n) % group of the
 // key head's group.  Each wave takes every fourth run of 32 keys of the block's chunk through LDS of its own.
-template <int DP>
-__global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
+template <int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_kernel(const AttnArgs a) {
   using Tile = RowTile<DP>;
-  constexpr int NB = DP / 32, STEPS = DP / 16, RUN = 32, TILE_BYTES = RUN * Tile::kRowBytes;
-  constexpr int LOADS = RUN * Tile::kPieces / 64;
+  using Load = TilePair<DP, 32, WHOLE, 64>;
+  constexpr int NB = DP / 32, STEPS = DP / 16, RUN = 32, TILE_BYTES = Load::kBytes;
   constexpr int JOIN = 32 * (DP + 4) * 4;  // one wave's output, columns padded against bank conflicts
-  constexpr int OWN = 2 * TILE_BYTES;
+  constexpr int OWN = (WHOLE ? 2 : 1) * 2 * TILE_BYTES;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * (OWN > JOIN ? OWN : JOIN)];
   __shared__ float2 wave_ml[kWaves][32];
   int place = blockIdx.x;
@@ -180,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
   const int row_tile0 = place % a.n_row_tiles;
   place /= a.n_row_tiles;
   const int kv_head = place % a.c.Hkv, seq = place / a.c.Hkv;
-  const int D = a.c.D;
+  const int D = WHOLE ? DP : a.c.D;
   const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
   const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -191,13 +192,16 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
   const int end_key = chunk == a.n_chunks - 1 || first_key + a.chunk > sk.len ? sk.len : first_key + a.chunk;
   const bool alone = a.n_chunks == 1;
   if (!alone && first_key >= sk.len && chunk > 0) return;  // (the first chunk reports where no key is seen)
-  const bf16_t* Kh = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
-  const bf16_t* Vh = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+  Load load;
+  load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
+  load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+  load.stride[0] = a.c.K.token;
+  load.stride[1] = a.c.V.token;
+  load.rows = end_key;
+  load.D = D;
+  load.smem = smem + wave * OWN;
+  load.lds = NM_LDS_ADDRESS(smem) + wave * OWN;
   const int64_t columns = (int64_t)sq.len * a.group;
-  unsigned char* own = smem + wave * OWN;
-  const uint32_t k_at = NM_LDS_ADDRESS(smem) + wave * OWN + Tile::row_base(lane);
-  const uint32_t v_at = NM_LDS_ADDRESS(smem) + wave * OWN + TILE_BYTES + Tile::column_base(lane);
-
   for (int row_tile = row_tile0; (int64_t)row_tile * 32 < columns; row_tile += a.n_row_tiles) {
     const int64_t n = (int64_t)row_tile * 32 + col;
     const bool live = n < columns;
@@ -218,27 +222,28 @@ __global__ void __launch_bounds__(kThreads, 2) cache_kernel(const AttnArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
     float ref = kMinusInf, sum = 0.f;
-    u32x4_t k_in[LOADS], v_in[LOADS];
-    auto fetch = [&](int k0) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int at = i * 64 + lane, row = k0 + at / Tile::kPieces, d = at % Tile::kPieces * 8;
-        k_in[i] = load_piece(Kh + (int64_t)row * a.c.K.token, d, D, row < end_key);
-        v_in[i] = load_piece(Vh + (int64_t)row * a.c.V.token, d, D, row < end_key);
-      }
-    };
     __syncthreads();  // (a further row tile: what the waves joined has been read)
-    int k0 = first_key + wave * RUN;
-    if (k0 < end_key) fetch(k0);
+    int k0 = first_key + wave * RUN, stage = 0;
+    if (k0 < end_key) load.fetch(0, k0);
+    if constexpr (WHOLE) arrived(q);
     for (; k0 < end_key; k0 += kWaves * RUN) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int at = i * 64 + lane, to = Tile::place(at / Tile::kPieces, at % Tile::kPieces);
-        *reinterpret_cast<u32x4_t*>(own + to) = k_in[i];
-        *reinterpret_cast<u32x4_t*>(own + TILE_BYTES + to) = v_in[i];
+      // asynchronous copies go to the other stage while this one is worked on; what comes through registers waits there
+      const bool more = k0 + kWaves * RUN < end_key;
+      if constexpr (WHOLE) {
+        if (more) {
+          load.fetch(stage ^ 1, k0 + kWaves * RUN);
+          load.template settle<2 * Load::kLoads>(stage);
+        } else {
+          load.settle(stage);
+        }
+      } else {
+        load.settle(0);
+        if (more) load.fetch(0, k0 + kWaves * RUN);
       }
-      if (k0 + kWaves * RUN < end_key) fetch(k0 + kWaves * RUN);
       __builtin_amdgcn_wave_barrier();
+      const uint32_t tile = load.lds + (uint32_t)stage * 2 * TILE_BYTES;
+      const uint32_t k_at = tile + Tile::row_base(lane), v_at = tile + TILE_BYTES + Tile::column_base(lane);
+      if constexpr (WHOLE) stage ^= 1;
       constexpr int NV = RUN / 16 * NB;
       auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
       auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
@@ -398,7 +403,7 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
     constexpr bool WHOLE = decltype(whole)::value;
     if (plan.taken) {
       const int64_t blocks = (int64_t)a.n_chunks * a.n_row_tiles * c.B * c.Hkv;
-      cache_kernel<DP><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
+      cache_kernel<DP, WHOLE><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
       if (a.n_chunks > 1) {
         const dim3 join((unsigned)((c.max_q * c.Hq + kWaves - 1) / kWaves), (unsigned)c.B);
         cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);

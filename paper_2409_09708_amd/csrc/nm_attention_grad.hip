@@ -28,7 +28,7 @@ struct GradArgs {
 constexpr int kKeys = 64;              // keys per tile of grad_query_kernel
 constexpr int kRows = kWaves * 32;     // queries (keys) that a block keeps
 constexpr int kQueries = 32;           // queries per tile of grad_key_kernel
-constexpr int64_t kKeyBlocks = 2048;    // blocks that grad_key_kernel's work is cut for
+constexpr int64_t kKeyBlocks = 512;    // blocks that grad_key_kernel's work is cut for
 
 template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs a) {
@@ -36,15 +36,15 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];
   TilePlace at;
-  if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_q_tiles, true, &at)) return;
+  if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_q_tiles, true, a.c.causal, &at)) return;
   const int head = at.kv_head * a.group + at.sub;
-  const int D = a.c.D;
+  const int D = WHOLE ? DP : a.c.D;
   const Span sq = sequence(a.c.offsets_q, nullptr, at.seq, a.c.Tq);
   const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, at.seq, a.c.Tk);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
-  TilePair<DP, kKeys, WHOLE> load;
+  TilePair<DP, kKeys, WHOLE, kThreads> load;
   load.base[0] = a.c.K.p + sk.first * a.c.K.token + at.kv_head * a.c.K.head;
   load.base[1] = a.c.V.p + sk.first * a.c.V.token + at.kv_head * a.c.V.head;
   load.stride[0] = a.c.K.token;
@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
 }
 
 // Key tiles differ in how many queries see them, and shared key heads leave few of them, so the (head, query tile) steps of a key
-// tile are cut into chunks of `chunk` for different blocks; where there is more than one, 32-bit sums of each go to the
+// tile are cut into chunks of up to `chunk` for different blocks; where there is more than one, 32-bit sums of each go to the
 // workspace and grad_key_sum_kernel adds them in order.
 struct KeySteps {
-  int first_q, per_head, steps, chunks;
+  int first_q, per_head, steps, chunks, share;
 };
 __device__ __forceinline__ KeySteps key_steps(const GradArgs& a, int tile, int q_len, int k_len) {
   const int shift = k_len - q_len;
@@ -158,7 +158,8 @@ __device__ __forceinline__ KeySteps key_steps(const GradArgs& a, int tile, int q
   s.steps = s.per_head * a.group;
   s.chunks = (s.steps + a.chunk - 1) / a.chunk;
   if (s.chunks < 1) s.chunks = 1;
-  if (s.chunks > a.n_chunks) s.chunks = a.n_chunks;  // (the last one takes the rest)
+  if (s.chunks > a.n_chunks) s.chunks = a.n_chunks;
+  s.share = (s.steps + s.chunks - 1) / s.chunks;  // steps of a chunk (the last ones can have fewer)
   return s;
 }
 
@@ -173,16 +174,16 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   constexpr bool KEEP = DP == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char kept[KEEP ? kRows * Tile::kRowBytes : 16];
   TilePlace at;
-  if (!tile_place(a.c.B, a.c.Hkv, a.n_chunks, a.n_k_tiles, false, &at)) return;
+  if (!tile_place(a.c.B, a.c.Hkv, a.n_chunks, a.n_k_tiles, false, a.c.causal, &at)) return;
   const int chunk = at.sub;
-  const int D = a.c.D;
+  const int D = WHOLE ? DP : a.c.D;
   const Span sq = sequence(a.c.offsets_q, nullptr, at.seq, a.c.Tq);
   const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, at.seq, a.c.Tk);
   const Span room = sequence(a.c.offsets_k, nullptr, at.seq, a.c.Tk);  // rows past the length get zeros
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
-  TilePair<DP, kQueries, WHOLE> load;
+  TilePair<DP, kQueries, WHOLE, kThreads> load;
   load.stride[0] = a.c.Q.token;
   load.stride[1] = a.c.dO.token;
   load.rows = sq.len;
@@ -193,8 +194,8 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   for (int tile = at.tile; (int64_t)tile * kRows < room.len; tile += a.n_k_tiles) {
     const KeySteps list = key_steps(a, tile, sq.len, sk.len);
     if (chunk >= list.chunks) continue;
-    const int first_step = chunk * a.chunk;
-    const int end_step = chunk == list.chunks - 1 ? list.steps : first_step + a.chunk;
+    const int first_step = chunk * list.share < list.steps ? chunk * list.share : list.steps;
+    const int end_step = first_step + list.share < list.steps ? first_step + list.share : list.steps;
     const int k_wave = tile * kRows + wave * 32;
     const int kj = k_wave + (lane & 31);
     const int64_t tok = sk.first + kj;
