@@ -1066,6 +1066,9 @@ def nm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5, residual=None, t
     bias are float32 [C].  Returns Y (float32 or bfloat16, default float32) -- with a residual (Y, S), S the sum in X's type
     (sum_out, which may be the residual itself), and with train=True the rows' statistics [T, 2] behind them, which
     nm_layer_norm_backward takes."""
+    done = (_CALLS or _native()).layer_norm(X, weight, bias, eps, residual, train, out_dtype, out, sum_out, stream)
+    if done is not NotImplemented:
+        return done
     torch = _torch()
     code = _typed(X, "X")
     T, C, ldx = _rows(X, "X")
@@ -1100,6 +1103,9 @@ def nm_layer_norm_backward(dY, S, stats, weight=None, dS=None, out_dtype=None, o
     """(dX, dweight, dbias) of nm_layer_norm from the gradient dY of its output, what was normalised (X, or the sum S) and its
     statistics; dS (type of dY) is the gradient that reaches the sum by its other use and is added to dX.  dX is float32
     (default) or bfloat16, dweight and dbias float32 [C], or None where params=False."""
+    done = (_CALLS or _native()).layer_norm_backward(dY, S, stats, weight, dS, out_dtype, out, params, workspace, stream)
+    if done is not NotImplemented:
+        return done
     torch = _torch()
     dy_code, s_code = _typed(dY, "dY"), _typed(S, "S")
     T, C, lddy = _rows(dY, "dY")
@@ -1145,6 +1151,9 @@ def nm_rotary(X, positions, freqs, sections=None, interleaved: bool = False, inv
     (pairs per axis, in order; default: all on one axis).  positions are int32 or float32 [T, axes] ([T] for one), freqs
     float32.  Pairs are (i, i + len(freqs)), or (2 i, 2 i + 1) with interleaved=True; inverse=True turns back, which is the
     backward pass.  Y has X's type unless out_dtype says otherwise; out=X turns in place."""
+    done = (_CALLS or _native()).rotary(X, positions, freqs, sections, interleaved, inverse, out_dtype, out, stream)
+    if done is not NotImplemented:
+        return done
     torch = _torch()
     code = _typed(X, "X")
     token, head = _head_strides(X, "X")
@@ -1220,6 +1229,10 @@ def nm_attention(Q, K, V, causal: bool = False, scale=None, offsets_q=None, offs
     offsets_q and offsets_k (int32 [sequences + 1], from 0 to Tq and Tk) say where each begins, lengths_k how many of its keys are in use
     (a cache of fixed capacity); none of them: one sequence.  Causal: a sequence's last query sees all its keys.  max_q and
     max_k are the longest lengths as far as known: the launch is shaped for them."""
+    done = (_CALLS or _native()).attention(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k, lse, out, workspace,
+                                           stream)
+    if done is not NotImplemented:
+        return done
     desc = _attention_desc(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k)
     if out is None:
         out = Q.new_empty(Q.shape)
@@ -1243,6 +1256,11 @@ def nm_attention_backward(dO, Q, K, V, O, lse, causal: bool = False, scale=None,
     """(dQ, dK, dV) of nm_attention, bfloat16 in the shapes of Q, K and V, from dO, the O and lse it returned and the same
     arguments otherwise; gradients of a key head are sums over the query heads that share it.  out: the three tensors to
     write (views of a joint projection's gradient, say)."""
+    if out is None:
+        done = (_CALLS or _native()).attention_backward(dO, Q, K, V, O, lse, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k,
+                                                        workspace, stream)
+        if done is not NotImplemented:
+            return done
     torch = _torch()
     desc = _attention_desc(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k)
     desc.O, desc.dO = _heads(O, "O", Q.shape), _heads(dO, "dO", Q.shape)

@@ -60,26 +60,26 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMinusInf = -__builtin_huge_valf();
 
-// Sequence b of a packed tensor: its first row and length.  Offsets are the caller's; whatever they hold, rows stay inside
-// the tensor.
+// Sequence b of the packed tensors: first rows and lengths, of the keys those in use and the rows that belong to them.  Offsets
+// are the caller's; whatever they hold, rows stay inside the tensors.  Five lanes read the five numbers at once, with one wait.
 struct Span {
   int64_t first;
   int len;
 };
-__device__ __forceinline__ Span sequence(const int32_t* offsets, const int32_t* lengths, int b, int64_t total) {
-  int64_t lo = 0, hi = total;
-  if (offsets != nullptr) {
-    lo = offsets[b];
-    hi = offsets[b + 1];
-    lo = lo < 0 ? 0 : lo > total ? total : lo;
-    hi = hi < lo ? lo : hi > total ? total : hi;
-  }
-  int64_t len = hi - lo;
-  if (lengths != nullptr) {
-    const int64_t n = lengths[b];
-    len = n < 0 ? 0 : n < len ? n : len;
-  }
-  return {lo, (int)len};
+struct Sequence {
+  Span q, k;
+  int room;
+};
+__device__ __forceinline__ Sequence sequence(const AttentionCall& c, int b) {
+  const int lane = threadIdx.x & 63;
+  const int32_t* from = lane < 2 ? c.offsets_q : lane < 4 ? c.offsets_k : c.lengths_k;
+  int v = lane == 1 ? (int)c.Tq : lane == 3 ? (int)c.Tk : lane == 4 ? 0x7FFFFFFF : 0;
+  if (lane < 5 && from != nullptr) v = from[b + (lane < 4 ? lane & 1 : 0)];
+  auto within = [](int x, int lo, int hi) { return x < lo ? lo : x < hi ? x : hi; };
+  const int q0 = within(__builtin_amdgcn_readlane(v, 0), 0, (int)c.Tq), q1 = within(__builtin_amdgcn_readlane(v, 1), q0, (int)c.Tq);
+  const int k0 = within(__builtin_amdgcn_readlane(v, 2), 0, (int)c.Tk), k1 = within(__builtin_amdgcn_readlane(v, 3), k0, (int)c.Tk);
+  const int used = within(__builtin_amdgcn_readlane(v, 4), 0, k1 - k0);
+  return {{q0, q1 - q0}, {k0, used}, k1 - k0};
 }
 
 // A tile of rows of DP bfloat16 in LDS.  The 16-byte pieces of a row are permuted so that both ways of reading it touch every

@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_tiles, true, a.c.causal, &at)) return;
   const int kv_head = at.kv_head, head = kv_head * a.group + at.sub, seq = at.seq;
   const int D = WHOLE ? DP : a.c.D;
-  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const Sequence of = sequence(a.c, seq);
+  const Span sq = of.q, sk = of.k;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;  // causal: query i sees keys up to i + shift
@@ -182,8 +182,8 @@ __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_ke
   place /= a.n_row_tiles;
   const int kv_head = place % a.c.Hkv, seq = place / a.c.Hkv;
   const int D = WHOLE ? DP : a.c.D;
-  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const Sequence of = sequence(a.c, seq);
+  const Span sq = of.q, sk = of.k;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
   const int shift = sk.len - sq.len;
@@ -322,8 +322,8 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) 
   const int lane = threadIdx.x & 63;
   const int64_t n = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);  // query * Hq + head
   const int seq = blockIdx.y;
-  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
+  const Sequence of = sequence(a.c, seq);
+  const Span sq = of.q, sk = of.k;
   const int used = (sk.len + a.chunk - 1) / a.chunk;
   const int chunks = used < 1 ? 1 : used < a.n_chunks ? used : a.n_chunks;
   for (int64_t i = n; i < (int64_t)sq.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {

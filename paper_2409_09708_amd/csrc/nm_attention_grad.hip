@@ -39,8 +39,8 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
   if (!tile_place(a.c.B, a.c.Hkv, a.group, a.n_q_tiles, true, a.c.causal, &at)) return;
   const int head = at.kv_head * a.group + at.sub;
   const int D = WHOLE ? DP : a.c.D;
-  const Span sq = sequence(a.c.offsets_q, nullptr, at.seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, at.seq, a.c.Tk);
+  const Sequence of = sequence(a.c, at.seq);
+  const Span sq = of.q, sk = of.k;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
@@ -177,9 +177,8 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   if (!tile_place(a.c.B, a.c.Hkv, a.n_chunks, a.n_k_tiles, false, a.c.causal, &at)) return;
   const int chunk = at.sub;
   const int D = WHOLE ? DP : a.c.D;
-  const Span sq = sequence(a.c.offsets_q, nullptr, at.seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, at.seq, a.c.Tk);
-  const Span room = sequence(a.c.offsets_k, nullptr, at.seq, a.c.Tk);  // rows past the length get zeros
+  const Sequence of = sequence(a.c, at.seq);
+  const Span sq = of.q, sk = of.k;  // (of.room rows of keys: those past the length get zeros)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5;
   const int shift = sk.len - sq.len;
@@ -191,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   load.smem = smem[0];
   load.lds = NM_LDS_ADDRESS(smem[0]);
 
-  for (int tile = at.tile; (int64_t)tile * kRows < room.len; tile += a.n_k_tiles) {
+  for (int tile = at.tile; (int64_t)tile * kRows < of.room; tile += a.n_k_tiles) {
     const KeySteps list = key_steps(a, tile, sq.len, sk.len);
     if (chunk >= list.chunks) continue;
     const int first_step = chunk * list.share < list.steps ? chunk * list.share : list.steps;
@@ -319,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
             *reinterpret_cast<float4*>(to + DP + 32 * b + acc_row(r)) = float4{dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]};
           }
       }
-    } else if (kj < room.len) {
+    } else if (kj < of.room) {
       if (kj >= sk.len) {  // (it was multiplied as a row of zeros: what came of that, infinities included, is not its gradient)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -337,14 +336,13 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
 template <int DP>
 __global__ void __launch_bounds__(kThreads) grad_key_sum_kernel(const GradArgs a) {
   const int seq = blockIdx.y;
-  const Span sq = sequence(a.c.offsets_q, nullptr, seq, a.c.Tq);
-  const Span sk = sequence(a.c.offsets_k, a.c.lengths_k, seq, a.c.Tk);
-  const Span room = sequence(a.c.offsets_k, nullptr, seq, a.c.Tk);
+  const Sequence of = sequence(a.c, seq);
+  const Span sq = of.q, sk = of.k;
   constexpr int LANES = 2 * DP / 4, PER_BLOCK = kThreads / LANES;  // lanes and rows of one (key, head)
   const int lane = threadIdx.x % LANES;
   const bool values = lane >= DP / 4;
   const int d = lane % (DP / 4) * 4;
-  for (int64_t n = (int64_t)blockIdx.x * PER_BLOCK + threadIdx.x / LANES; n < (int64_t)room.len * a.c.Hkv;
+  for (int64_t n = (int64_t)blockIdx.x * PER_BLOCK + threadIdx.x / LANES; n < (int64_t)of.room * a.c.Hkv;
        n += (int64_t)gridDim.x * PER_BLOCK) {
     const int kj = (int)(n / a.c.Hkv), head = (int)(n % a.c.Hkv);
     const int chunks = key_steps(a, kj / kRows, sq.len, sk.len).chunks;

@@ -24,8 +24,10 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <cmath>
 #include <exception>
 #include <optional>
+#include <vector>
 
 #include "nm_sparse.h"
 
@@ -60,6 +62,14 @@ struct Library {
   decltype(&nm_linear_forward_i8_packed) i8_packed;
   decltype(&nm_linear_forward_i8_packed_prepared) i8_packed_prepared;
   decltype(&nm_i8_workspace_bytes) i8_bytes;
+  decltype(&nm_layer_norm) layer_norm;
+  decltype(&nm_layer_norm_backward) layer_norm_backward;
+  decltype(&nm_layer_norm_backward_workspace_bytes) layer_norm_backward_bytes;
+  decltype(&nm_rotary) rotary;
+  decltype(&nm_attention) attention;
+  decltype(&nm_attention_workspace_bytes) attention_bytes;
+  decltype(&nm_attention_backward) attention_backward;
+  decltype(&nm_attention_backward_workspace_bytes) attention_backward_bytes;
 } lib;
 PyObject* raise_status;    // raises NmError for a status that is not NM_OK
 PyObject* find_workspace;  // the scratch tensor of a device and stream
@@ -545,6 +555,324 @@ PyObject* forward_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// A float or bfloat16 tensor, and its type code.
+bool floating(PyObject* obj, const at::Tensor** t, int32_t* code) {
+  if (plain(obj, at::kBFloat16, t)) *code = NM_OUT_BF16;
+  else if (plain(obj, at::kFloat, t)) *code = NM_OUT_F32;
+  else return false;
+  return true;
+}
+// An optional [rows, cols] matrix of a type.
+bool optional_matrix(PyObject* obj, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor** t, int64_t* ld) {
+  *t = nullptr;
+  *ld = cols;
+  if (obj == Py_None) return true;
+  Matrix m;
+  if (!plain(obj, type, t) || !matrix(**t, &m) || m.rows != rows || m.cols != cols) return false;
+  *ld = m.ld;
+  return true;
+}
+bool flag(PyObject* obj, bool* out) {
+  *out = obj == Py_True;
+  return PyBool_Check(obj);
+}
+at::Tensor fresh_like(at::Device device, at::IntArrayRef sizes, at::ScalarType type) {
+  return at::empty(sizes, at::TensorOptions().dtype(type).device(device));
+}
+
+// layer_norm(X, weight, bias, eps, residual, train, out_dtype, out, sum_out, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *X, *R, *S;
+  Matrix x;
+  int32_t code;
+  const float *w, *b;
+  int64_t ldr, lds;
+  bool train;
+  Output y;
+  void* s;
+  if (n != 10 || lib.layer_norm == nullptr || observed() || !floating(a[0], &X, &code) || !matrix(*X, &x) || !per_feature(a[1], x.cols, &w) ||
+      !per_feature(a[2], x.cols, &b) || !PyFloat_CheckExact(a[3]) || !flag(a[5], &train) ||
+      !optional_matrix(a[4], X->scalar_type(), x.rows, x.cols, &R, &ldr) ||
+      !optional_matrix(a[8], X->scalar_type(), x.rows, x.cols, &S, &lds) || (S != nullptr && R == nullptr) ||
+      !y.read(a[6], a[7], x.rows, x.cols, false) || !stream_of(a[9], &s))
+    return declined();
+  const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+  const at::Device device = X->device();
+  const at::ScalarType type = X->scalar_type();
+  const void *xp = pointer<void>(X), *rp = pointer<void>(R);
+  void* sp = pointer<void>(S);
+  at::Tensor sum, stats;
+  const int32_t st = unlocked([&] {
+    y.make(device);
+    if (rp != nullptr && sp == nullptr) {
+      sum = fresh(device, x.rows, x.cols, type);
+      sp = sum.data_ptr();
+    }
+    if (train) stats = fresh(device, x.rows, 2, at::kFloat);
+    return lib.layer_norm(xp, x.ld, code, rp, ldr, x.rows, x.cols, w, b, eps, y.ptr, y.ld, y.code, sp, lds,
+                          train ? static_cast<float*>(stats.data_ptr()) : nullptr, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* out = y.take();
+  if (rp == nullptr && !train) return out;
+  PyObject* total = nullptr;
+  if (rp != nullptr) {
+    if (a[8] != Py_None) {
+      Py_INCREF(a[8]);
+      total = a[8];
+    } else {
+      total = THPVariable_Wrap(std::move(sum));
+    }
+  }
+  if (!train) return Py_BuildValue("(NN)", out, total);
+  PyObject* kept = THPVariable_Wrap(std::move(stats));
+  return rp != nullptr ? Py_BuildValue("(NNN)", out, total, kept) : Py_BuildValue("(NN)", out, kept);
+  END_HANDLE_TH_ERRORS
+}
+
+// layer_norm_backward(dY, S, stats, weight, dS, out_dtype, out, params, workspace, stream)
+PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *dY, *S, *stats, *dS;
+  Matrix dy, x;
+  int32_t y_code, s_code;
+  const float* w;
+  int64_t ldds;
+  bool params;
+  Output d;
+  void* s;
+  if (n != 10 || lib.layer_norm_backward == nullptr || lib.layer_norm_backward_bytes == nullptr || observed() ||
+      !floating(a[0], &dY, &y_code) || !matrix(*dY, &dy) || !floating(a[1], &S, &s_code) || !matrix(*S, &x) || x.rows != dy.rows ||
+      x.cols != dy.cols || !plain(a[2], at::kFloat, &stats) || !whole(*stats) || stats->size(0) != dy.rows || stats->size(1) != 2 ||
+      !per_feature(a[3], dy.cols, &w) || !optional_matrix(a[4], dY->scalar_type(), dy.rows, dy.cols, &dS, &ldds) ||
+      !d.read(a[5], a[6], dy.rows, dy.cols, false) || !flag(a[7], &params) || !stream_of(a[9], &s))
+    return declined();
+  Workspace ws;
+  const size_t need = params && a[8] == Py_None ? lib.layer_norm_backward_bytes(dy.rows, dy.cols) : 0;
+  if (const Take t = need != 0 ? scratch_workspace(need, a[0], a[9], s, &ws) : given_workspace(a[8], &ws); t != TAKEN)
+    return t == DECLINED ? declined() : nullptr;
+  const at::Device device = dY->device();
+  const void *dyp = pointer<void>(dY), *xp = pointer<void>(S), *dsp = pointer<void>(dS);
+  const float* sp = pointer<float>(stats);
+  at::Tensor dw, db;
+  const int32_t st = unlocked([&] {
+    d.make(device);
+    if (params) {
+      dw = fresh_like(device, {dy.cols}, at::kFloat);
+      db = fresh_like(device, {dy.cols}, at::kFloat);
+    }
+    return lib.layer_norm_backward(dyp, dy.ld, y_code, xp, x.ld, s_code, sp, w, dsp, ldds, dy.rows, dy.cols, d.ptr, d.ld, d.code,
+                                   params ? static_cast<float*>(dw.data_ptr()) : nullptr,
+                                   params ? static_cast<float*>(db.data_ptr()) : nullptr, ws.ptr, ws.bytes, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* dx = d.take();
+  if (!params) return Py_BuildValue("(NOO)", dx, Py_None, Py_None);
+  PyObject* dwp = THPVariable_Wrap(std::move(dw));
+  PyObject* dbp = THPVariable_Wrap(std::move(db));
+  return Py_BuildValue("(NNN)", dx, dwp, dbp);
+  END_HANDLE_TH_ERRORS
+}
+
+// [tokens, heads, elements] whose heads are contiguous
+bool heads_of(const at::Tensor& t) { return t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1); }
+
+// rotary(X, positions, freqs, sections, interleaved, inverse, out_dtype, out, stream)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *X, *positions, *freqs, *out = nullptr;
+  int32_t code, y_code, sections[4], axes = 1;
+  bool interleaved, inverse, whole_numbers;
+  void* s;
+  if (n != 9 || lib.rotary == nullptr || observed() || !floating(a[0], &X, &code) || !heads_of(*X) ||
+      !((whole_numbers = plain(a[1], at::kInt, &positions)) || plain(a[1], at::kFloat, &positions)) || !positions->is_contiguous() ||
+      !plain(a[2], at::kFloat, &freqs) || freqs->dim() != 1 || !freqs->is_contiguous() || !flag(a[4], &interleaved) || !flag(a[5], &inverse) ||
+      !stream_of(a[8], &s))
+    return declined();
+  const int64_t T = X->size(0), H = X->size(1), D = X->size(2), pairs = freqs->size(0);
+  if (a[3] != Py_None) {
+    if (!PyTuple_CheckExact(a[3]) || PyTuple_GET_SIZE(a[3]) < 1 || PyTuple_GET_SIZE(a[3]) > 4) return declined();
+    axes = (int32_t)PyTuple_GET_SIZE(a[3]);
+    for (int32_t i = 0; i < axes; ++i) {
+      int64_t v;
+      if (!integer(PyTuple_GET_ITEM(a[3], i), 0, 1 << 30, &v)) return declined();
+      sections[i] = (int32_t)v;
+    }
+  } else {
+    if (pairs > 1 << 30) return declined();
+    sections[0] = (int32_t)pairs;
+  }
+  if (positions->dim() == 2 ? positions->size(0) != T || positions->size(1) != axes
+                            : positions->dim() != 1 || axes != 1 || positions->size(0) != T)
+    return declined();
+  at::ScalarType type = X->scalar_type();
+  at::Tensor made;
+  if (a[7] != Py_None) {
+    if (!floating(a[7], &out, &y_code) || !heads_of(*out) || out->size(0) != T || out->size(1) != H || out->size(2) != D) return declined();
+  } else {
+    if (a[6] != Py_None) {
+      if (!THPDtype_Check(a[6])) return declined();
+      type = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
+    }
+    if (type != at::kFloat && type != at::kBFloat16) return declined();
+    y_code = type == at::kFloat ? NM_OUT_F32 : NM_OUT_BF16;
+  }
+  const at::Device device = X->device();
+  const int64_t x_token = X->stride(0), x_head = X->stride(1);
+  int64_t y_token = out ? out->stride(0) : H * D, y_head = out ? out->stride(1) : D;
+  const void *xp = pointer<void>(X), *pp = pointer<void>(positions);
+  const float* fp = pointer<float>(freqs);
+  void* yp = pointer<void>(out);
+  const int32_t st = unlocked([&] {
+    if (yp == nullptr) {
+      made = fresh_like(device, {T, H, D}, type);
+      yp = made.data_ptr();
+    }
+    return lib.rotary(xp, code, T, H, D, x_token, x_head, pp, !whole_numbers, fp, sections, axes, 2 * pairs, interleaved, inverse, yp,
+                      y_code, y_token, y_head, s);
+  });
+  if (out != nullptr) {
+    Py_INCREF(a[7]);
+    return result(st, a[7]);
+  }
+  return result(st, THPVariable_Wrap(std::move(made)));
+  END_HANDLE_TH_ERRORS
+}
+
+bool read_heads(PyObject* obj, nm_heads* h, const at::Tensor** t) {
+  if (!plain(obj, at::kBFloat16, t) || !heads_of(**t)) return false;
+  *h = nm_heads{pointer<uint16_t>(*t), (*t)->stride(0), (*t)->stride(1)};
+  return true;
+}
+bool same_sizes(const at::Tensor& a, const at::Tensor& b) { return a.sizes() == b.sizes(); }
+// offsets and lengths: an optional int32 [count]
+bool per_sequence(PyObject* obj, int64_t count, const int32_t** out) {
+  const at::Tensor* t = nullptr;
+  if (obj != Py_None && (!plain(obj, at::kInt, &t) || t->dim() != 1 || t->size(0) != count || !t->is_contiguous())) return false;
+  *out = pointer<int32_t>(t);
+  return true;
+}
+bool most(PyObject* obj, int64_t otherwise, int64_t* out) {
+  *out = otherwise;
+  return obj == Py_None || integer(obj, 0, 1ll << 40, out);
+}
+// what both attention calls have in common: Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k from a on
+bool read_attention(PyObject* const* a, nm_attention_desc* d, const at::Tensor** Q, const at::Tensor** K) {
+  const at::Tensor* V;
+  bool causal;
+  if (!read_heads(a[0], &d->Q, Q) || !read_heads(a[1], &d->K, K) || !read_heads(a[2], &d->V, &V) || !same_sizes(**K, *V) ||
+      (*Q)->size(2) != (*K)->size(2) || !flag(a[3], &causal))
+    return false;
+  if (a[4] == Py_None) d->scale = (float)(1.0 / std::sqrt((double)(*Q)->size(2)));
+  else if (PyFloat_CheckExact(a[4])) d->scale = (float)PyFloat_AS_DOUBLE(a[4]);
+  else return false;
+  const at::Tensor* first = nullptr;
+  int64_t sequences = 1;
+  if (a[5] != Py_None) {
+    if (a[6] == Py_None || !plain(a[5], at::kInt, &first) || first->dim() != 1 || first->size(0) < 2 || first->size(0) > 1 << 30) return false;
+    sequences = first->size(0) - 1;
+  } else if (a[6] != Py_None) {
+    return false;
+  }
+  if (!per_sequence(a[5], sequences + 1, &d->offsets_q) || !per_sequence(a[6], sequences + 1, &d->offsets_k) ||
+      !per_sequence(a[7], sequences, &d->lengths_k))
+    return false;
+  d->Tq = (*Q)->size(0);
+  d->Tk = (*K)->size(0);
+  if (!most(a[8], (d->Tq + sequences - 1) / sequences, &d->max_q) || !most(a[9], (d->Tk + sequences - 1) / sequences, &d->max_k)) return false;
+  constexpr int64_t limit = 1 << 30;
+  if ((*Q)->size(1) > limit || (*K)->size(1) > limit || (*Q)->size(2) > limit) return false;
+  d->sequences = (int32_t)sequences;
+  d->heads_q = (int32_t)(*Q)->size(1);
+  d->heads_kv = (int32_t)(*K)->size(1);
+  d->head_size = (int32_t)(*Q)->size(2);
+  d->causal = causal;
+  return true;
+}
+nm_heads contiguous_heads(const at::Tensor& t) {
+  return nm_heads{static_cast<uint16_t*>(t.data_ptr()), t.size(1) * t.size(2), t.size(2)};
+}
+
+// attention(Q, K, V, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k, lse, out, workspace, stream)
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_attention_desc d = {};
+  const at::Tensor *Q, *K, *O = nullptr;
+  bool lse;
+  void* s;
+  if (n != 14 || lib.attention == nullptr || lib.attention_bytes == nullptr || observed() || !read_attention(a, &d, &Q, &K) ||
+      !flag(a[10], &lse) || (a[11] != Py_None && (!read_heads(a[11], &d.O, &O) || !same_sizes(*O, *Q))) || !stream_of(a[13], &s))
+    return declined();
+  Workspace ws;
+  const size_t need = a[12] == Py_None ? lib.attention_bytes(d.Tq, d.sequences, d.heads_q, d.heads_kv, d.head_size, d.max_q,
+                                                             d.max_k < d.Tk ? d.max_k : d.Tk) : 0;
+  if (const Take t = need != 0 ? scratch_workspace(need, a[0], a[13], s, &ws) : given_workspace(a[12], &ws); t != TAKEN)
+    return t == DECLINED ? declined() : nullptr;
+  const at::Device device = Q->device();
+  const std::vector<int64_t> sizes = Q->sizes().vec();
+  at::Tensor made, sums;
+  const int32_t st = unlocked([&] {
+    if (O == nullptr) {
+      made = fresh_like(device, sizes, at::kBFloat16);
+      d.O = contiguous_heads(made);
+    }
+    if (lse) {
+      sums = fresh(device, d.heads_q, d.Tq, at::kFloat);
+      d.lse = static_cast<float*>(sums.data_ptr());
+    }
+    return lib.attention(&d, ws.ptr, ws.bytes, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* out;
+  if (O != nullptr) {
+    Py_INCREF(a[11]);
+    out = a[11];
+  } else {
+    out = THPVariable_Wrap(std::move(made));
+  }
+  return lse ? Py_BuildValue("(NN)", out, THPVariable_Wrap(std::move(sums))) : out;
+  END_HANDLE_TH_ERRORS
+}
+
+// attention_backward(dO, Q, K, V, O, lse, causal, scale, offsets_q, offsets_k, lengths_k, max_q, max_k, workspace, stream)
+PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_attention_desc d = {};
+  const at::Tensor *dO, *Q, *K, *O, *lse;
+  void* s;
+  if (n != 15) return declined();
+  PyObject* const shared[10] = {a[1], a[2], a[3], a[6], a[7], a[8], a[9], a[10], a[11], a[12]};
+  if (lib.attention_backward == nullptr || lib.attention_backward_bytes == nullptr || observed() || !read_attention(shared, &d, &Q, &K) ||
+      !read_heads(a[0], &d.dO, &dO) || !same_sizes(*dO, *Q) || !read_heads(a[4], &d.O, &O) || !same_sizes(*O, *Q) ||
+      !plain(a[5], at::kFloat, &lse) || !whole(*lse) || lse->size(0) != d.heads_q || lse->size(1) != d.Tq || !stream_of(a[14], &s))
+    return declined();
+  d.lse = pointer<float>(lse);
+  Workspace ws;
+  const size_t need = a[13] == Py_None ? lib.attention_backward_bytes(d.Tq, d.Tk, d.sequences, d.heads_q, d.heads_kv, d.head_size, d.max_q,
+                                                                     d.max_k, d.causal) : 0;
+  if (const Take t = need != 0 ? scratch_workspace(need, a[1], a[14], s, &ws) : given_workspace(a[13], &ws); t != TAKEN)
+    return t == DECLINED ? declined() : nullptr;
+  const at::Device device = Q->device();
+  const std::vector<int64_t> q_sizes = Q->sizes().vec(), k_sizes = K->sizes().vec();
+  at::Tensor dQ, dK, dV;
+  const int32_t st = unlocked([&] {
+    dQ = fresh_like(device, q_sizes, at::kBFloat16);
+    dK = fresh_like(device, k_sizes, at::kBFloat16);
+    dV = fresh_like(device, k_sizes, at::kBFloat16);
+    d.dQ = contiguous_heads(dQ);
+    d.dK = contiguous_heads(dK);
+    d.dV = contiguous_heads(dV);
+    return lib.attention_backward(&d, ws.ptr, ws.bytes, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* q = THPVariable_Wrap(std::move(dQ));
+  PyObject* k = THPVariable_Wrap(std::move(dK));
+  PyObject* v = THPVariable_Wrap(std::move(dV));
+  return Py_BuildValue("(NNN)", q, k, v);
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses by name, raise_status, find_workspace[, where that keeps its tensors])
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *table, *raise, *find, *kept = nullptr;
@@ -565,7 +893,12 @@ PyObject* bind(PyObject*, PyObject* args) {
       {"nm_linear_backward_weight_scratch", &l.backward_weight_scratch, true},
       {"nm_backward_weight_scratch_bytes", &l.backward_weight_scratch_bytes, true}, {"nm_linear_forward_i8", &l.i8, true},
       {"nm_linear_forward_i8_prepared", &l.i8_prepared, true}, {"nm_linear_forward_i8_packed", &l.i8_packed, true},
-      {"nm_linear_forward_i8_packed_prepared", &l.i8_packed_prepared, true}, {"nm_i8_workspace_bytes", &l.i8_bytes, true}};
+      {"nm_linear_forward_i8_packed_prepared", &l.i8_packed_prepared, true}, {"nm_i8_workspace_bytes", &l.i8_bytes, true},
+      {"nm_layer_norm", &l.layer_norm, true}, {"nm_layer_norm_backward", &l.layer_norm_backward, true},
+      {"nm_layer_norm_backward_workspace_bytes", &l.layer_norm_backward_bytes, true}, {"nm_rotary", &l.rotary, true},
+      {"nm_attention", &l.attention, true}, {"nm_attention_workspace_bytes", &l.attention_bytes, true},
+      {"nm_attention_backward", &l.attention_backward, true},
+      {"nm_attention_backward_workspace_bytes", &l.attention_backward_bytes, true}};
   for (auto& e : slots) {
     PyObject* address = PyDict_GetItemString(table, e.name);
     if (address == nullptr && e.optional) continue;
@@ -596,6 +929,11 @@ PyMethodDef methods[] = {
     {"backward_input", (PyCFunction)(void (*)())backward_input, METH_FASTCALL, nullptr},
     {"backward_weight", (PyCFunction)(void (*)())backward_weight, METH_FASTCALL, nullptr},
     {"forward_i8", (PyCFunction)(void (*)())forward_i8, METH_FASTCALL, nullptr},
+    {"layer_norm", (PyCFunction)(void (*)())layer_norm, METH_FASTCALL, nullptr},
+    {"layer_norm_backward", (PyCFunction)(void (*)())layer_norm_backward, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
+    {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
+    {"attention_backward", (PyCFunction)(void (*)())attention_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nm_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
