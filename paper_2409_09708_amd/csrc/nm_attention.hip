@@ -164,8 +164,53 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
   }
 }
 
+// Number `n` of all chunks of all sequences, in order: the sequence and its chunk.  A sequence has as many chunks as its keys
+// need (one at least, at most n_chunks, the last of which takes the rest); their counts are added up 64 sequences at a time.
+__device__ __forceinline__ bool find_chunk(const AttnArgs& a, int64_t n, int* seq, int* chunk) {
+  if (a.n_chunks == 1) {
+    *seq = (int)n;
+    *chunk = 0;
+    return n < a.c.B;
+  }
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+    const int b = b0 + lane;
+    int count = 0;
+    if (b < a.c.B) {
+      int64_t lo = 0, hi = a.c.Tk;
+      if (a.c.offsets_k != nullptr) {
+        lo = a.c.offsets_k[b];
+        hi = a.c.offsets_k[b + 1];
+      }
+      int64_t len = hi - lo;
+      if (a.c.lengths_k != nullptr && a.c.lengths_k[b] < len) len = a.c.lengths_k[b];
+      const int64_t need = (len + a.chunk - 1) / a.chunk;  // (of offsets that lie: some number; the keys are checked later)
+      count = (int)(need < 1 ? 1 : need < a.n_chunks ? need : a.n_chunks);
+    }
+    int upto = count;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int before = __shfl_up(upto, m, 64);
+      if (lane >= m) upto += before;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63);
+    if (n < total) {
+      const int at = __ffsll((unsigned long long)__ballot(upto > n)) - 1;
+      *seq = b0 + at;
+      *chunk = (int)n - (__shfl(upto, at, 64) - __shfl(count, at, 64));
+      *seq = __builtin_amdgcn_readfirstlane(*seq);
+      *chunk = __builtin_amdgcn_readfirstlane(*chunk);
+      return true;
+    }
+    n -= total;
+  }
+  return false;
+}
+
 // Few queries.  Column n of a row tile is query (32 tile + n) / group of the sequence and head (32 tile + n) % group of the
-// key head's group.  Each wave takes every fourth run of 32 keys of the block's chunk through LDS of its own.
+// key head's group.  As many blocks as the chip holds take the chunks, row tiles and key heads in turn (a grid with a block for
+// every chunk that there might be had most of them empty where lengths differ, and each of those held a compute unit's LDS:
+// 24 caches of up to 16k 223 us, 73 so).  Each wave takes every fourth run of 32 keys of the chunk through LDS of its own.
 template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_kernel(const AttnArgs a) {
   using Tile = RowTile<DP>;
@@ -175,201 +220,211 @@ __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_ke
   constexpr int OWN = (WHOLE ? 2 : 1) * 2 * TILE_BYTES;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * (OWN > JOIN ? OWN : JOIN)];
   __shared__ float2 wave_ml[kWaves][32];
-  int place = blockIdx.x;
-  const int chunk = place % a.n_chunks;
-  place /= a.n_chunks;
-  const int row_tile0 = place % a.n_row_tiles;
-  place /= a.n_row_tiles;
-  const int kv_head = place % a.c.Hkv, seq = place / a.c.Hkv;
   const int D = WHOLE ? DP : a.c.D;
-  const Sequence of = sequence(a.c, seq);
-  const Span sq = of.q, sk = of.k;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
-  const int shift = sk.len - sq.len;
-  // the chunks of this sequence: as many as its keys need, the last block of a too short grid takes what is left
-  const int first_key = chunk * a.chunk;
-  const int end_key = chunk == a.n_chunks - 1 || first_key + a.chunk > sk.len ? sk.len : first_key + a.chunk;
   const bool alone = a.n_chunks == 1;
-  if (!alone && first_key >= sk.len && chunk > 0) return;  // (the first chunk reports where no key is seen)
-  Load load;
-  load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
-  load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
-  load.stride[0] = a.c.K.token;
-  load.stride[1] = a.c.V.token;
-  load.rows = end_key;
-  load.D = D;
-  load.smem = smem + wave * OWN;
-  load.lds = NM_LDS_ADDRESS(smem) + wave * OWN;
-  const int64_t columns = (int64_t)sq.len * a.group;
-  for (int row_tile = row_tile0; (int64_t)row_tile * 32 < columns; row_tile += a.n_row_tiles) {
-    const int64_t n = (int64_t)row_tile * 32 + col;
-    const bool live = n < columns;
-    const int qi = (int)(n / a.group), head = kv_head * a.group + (int)(n % a.group);
-    const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
-    u32x4_t q[STEPS];
+  const int per_chunk = a.n_row_tiles * a.c.Hkv;
+  for (int64_t item = blockIdx.x; ; item += gridDim.x) {
+    int seq, chunk;
+    if (!find_chunk(a, item / per_chunk, &seq, &chunk)) return;
+    const int kv_head = (int)(item % per_chunk) % a.c.Hkv, row_tile0 = (int)(item % per_chunk) / a.c.Hkv;
+    const Sequence of = sequence(a.c, seq);
+    const Span sq = of.q, sk = of.k;
+    const int shift = sk.len - sq.len;
+    const int first_key = chunk * a.chunk;
+    const int end_key = chunk == a.n_chunks - 1 || first_key + a.chunk > sk.len ? sk.len : first_key + a.chunk;
+    Load load;
+    load.base[0] = a.c.K.p + sk.first * a.c.K.token + kv_head * a.c.K.head;
+    load.base[1] = a.c.V.p + sk.first * a.c.V.token + kv_head * a.c.V.head;
+    load.stride[0] = a.c.K.token;
+    load.stride[1] = a.c.V.token;
+    load.rows = end_key;
+    load.D = D;
+    load.smem = smem + wave * OWN;
+    load.lds = NM_LDS_ADDRESS(smem) + wave * OWN;
+    const int64_t columns = (int64_t)sq.len * a.group;
+    for (int row_tile = row_tile0; (int64_t)row_tile * 32 < columns; row_tile += a.n_row_tiles) {
+      const int64_t n = (int64_t)row_tile * 32 + col;
+      const bool live = n < columns;
+      const int qi = (int)(n / a.group), head = kv_head * a.group + (int)(n % a.group);
+      const bf16_t* q_row = a.c.Q.p + (sq.first + qi) * a.c.Q.token + head * a.c.Q.head;
+      u32x4_t q[STEPS];
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-    int limit = end_key, first_hidden = end_key;
-    if (a.c.causal) {
-      const int sees = qi + shift + 1, first_sees = row_tile * 32 / a.group + shift + 1;
-      limit = sees < end_key ? sees : end_key;
-      first_hidden = first_sees < end_key ? first_sees : end_key;
-    }
-    f32x16_t acc[NB];
+      for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+      int limit = end_key, first_hidden = end_key, end = end_key;  // keys that this lane, all lanes, any lane sees
+      if (a.c.causal) {
+        auto upto = [&](int64_t column) { const int n = (int)(column / a.group) + shift + 1; return n < end_key ? n : end_key; };
+        limit = upto(n);
+        first_hidden = upto((int64_t)row_tile * 32);
+        end = upto((int64_t)row_tile * 32 + 31 < columns ? (int64_t)row_tile * 32 + 31 : columns - 1);
+      }
+      f32x16_t acc[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
-    float ref = kMinusInf, sum = 0.f;
-    __syncthreads();  // (a further row tile: what the waves joined has been read)
-    int k0 = first_key + wave * RUN, stage = 0;
-    if (k0 < end_key) load.fetch(0, k0);
-    if constexpr (WHOLE) arrived(q);
-    for (; k0 < end_key; k0 += kWaves * RUN) {
-      // asynchronous copies go to the other stage while this one is worked on; what comes through registers waits there
-      const bool more = k0 + kWaves * RUN < end_key;
-      if constexpr (WHOLE) {
-        if (more) {
-          load.fetch(stage ^ 1, k0 + kWaves * RUN);
-          load.template settle<2 * Load::kLoads>(stage);
+        for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+      float ref = kMinusInf, sum = 0.f;
+      __syncthreads();  // (a further row tile: what the waves joined has been read)
+      int k0 = first_key + wave * RUN, stage = 0;
+      if (k0 < end) load.fetch(0, k0);
+      if constexpr (WHOLE) arrived(q);
+      for (; k0 < end; k0 += kWaves * RUN) {
+        // asynchronous copies go to the other stage while this one is worked on; what comes through registers waits there
+        const bool more = k0 + kWaves * RUN < end;
+        if constexpr (WHOLE) {
+          if (more) {
+            load.fetch(stage ^ 1, k0 + kWaves * RUN);
+            load.template settle<2 * Load::kLoads>(stage);
+          } else {
+            load.settle(stage);
+          }
         } else {
-          load.settle(stage);
+          load.settle(0);
+          if (more) load.fetch(0, k0 + kWaves * RUN);
         }
-      } else {
-        load.settle(0);
-        if (more) load.fetch(0, k0 + kWaves * RUN);
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t tile = load.lds + (uint32_t)stage * 2 * TILE_BYTES;
+        const uint32_t k_at = tile + Tile::row_base(lane), v_at = tile + TILE_BYTES + Tile::column_base(lane);
+        if constexpr (WHOLE) stage ^= 1;
+        constexpr int NV = RUN / 16 * NB;
+        auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
+        auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
+        f32x16_t s[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+        u32x4_t f[kAhead];
+        read_ahead<STEPS>(f, keys);
+        products<STEPS>(f, keys, [&](int i, u32x4_t k) { s[0] = mma32(k, q[i], s[0]); });
+        read_ahead<NV>(f, values);
+        if (k0 + RUN > first_hidden) hide_rows(s[0], limit - k0 - 4 * half);
+        softmax_step(s, a.scale_log2, ref, sum, acc);
+        const u32x4_t p[2] = {acc_operand(s[0], 0), acc_operand(s[0], 1)};
+        products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, p[i / NB], acc[i % NB]); });
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_wave_barrier();
-      const uint32_t tile = load.lds + (uint32_t)stage * 2 * TILE_BYTES;
-      const uint32_t k_at = tile + Tile::row_base(lane), v_at = tile + TILE_BYTES + Tile::column_base(lane);
-      if constexpr (WHOLE) stage ^= 1;
-      constexpr int NV = RUN / 16 * NB;
-      auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
-      auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
-      f32x16_t s[1];
+      // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
+      sum = half_sum(sum);
+      if (half == 0) wave_ml[wave][col] = float2{ref, sum};
+      __syncthreads();
+      float top = kMinusInf, total = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
-      u32x4_t f[kAhead];
-      read_ahead<STEPS>(f, keys);
-      products<STEPS>(f, keys, [&](int i, u32x4_t k) { s[0] = mma32(k, q[i], s[0]); });
-      read_ahead<NV>(f, values);
-      if (k0 + RUN > first_hidden) hide_rows(s[0], limit - k0 - 4 * half);
-      softmax_step(s, a.scale_log2, ref, sum, acc);
-      const u32x4_t p[2] = {acc_operand(s[0], 0), acc_operand(s[0], 1)};
-      products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, p[i / NB], acc[i % NB]); });
-      __builtin_amdgcn_wave_barrier();
-    }
-    // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
-    sum = half_sum(sum);
-    if (half == 0) wave_ml[wave][col] = float2{ref, sum};
-    __syncthreads();
-    float top = kMinusInf, total = 0.f;
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_ml[w][col].x);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_ml[w][col].x);
+      for (int w = 0; w < kWaves; ++w)
+        total += wave_ml[w][col].x == kMinusInf ? 0.f : wave_ml[w][col].y * fast_exp2(wave_ml[w][col].x - top);
+      const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - top);
+      float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      total += wave_ml[w][col].x == kMinusInf ? 0.f : wave_ml[w][col].y * fast_exp2(wave_ml[w][col].x - top);
-    const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - top);
-    float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4*>(joined + col * (DP + 4) + 32 * b + acc_row(r) + 4 * half) =
+              float4{acc[b][r] * by, acc[b][r + 1] * by, acc[b][r + 2] * by, acc[b][r + 3] * by};
+      __syncthreads();
+      // lane -> (column, four elements)
+      constexpr int PER_COL = DP / 4;
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<float4*>(joined + col * (DP + 4) + 32 * b + acc_row(r) + 4 * half) =
-            float4{acc[b][r] * by, acc[b][r + 1] * by, acc[b][r + 2] * by, acc[b][r + 3] * by};
-    __syncthreads();
-    // lane -> (column, four elements)
-    constexpr int PER_COL = DP / 4;
+      for (int i = 0; i < 32 * PER_COL / kThreads; ++i) {
+        const int at = i * kThreads + tid, c = at / PER_COL, d = at % PER_COL * 4;
+        const int64_t cn = (int64_t)row_tile * 32 + c;
+        if (cn >= columns || d >= D) continue;
+        const float* from = reinterpret_cast<const float*>(smem) + c * (DP + 4) + d;
+        float4 o = *reinterpret_cast<const float4*>(from);
 #pragma unroll
-    for (int i = 0; i < 32 * PER_COL / kThreads; ++i) {
-      const int at = i * kThreads + tid, c = at / PER_COL, d = at % PER_COL * 4;
-      const int64_t cn = (int64_t)row_tile * 32 + c;
-      if (cn >= columns || d >= D) continue;
-      const float* from = reinterpret_cast<const float*>(smem) + c * (DP + 4) + d;
-      float4 o = *reinterpret_cast<const float4*>(from);
+        for (int w = 1; w < kWaves; ++w) {
+          const float4 x = *reinterpret_cast<const float4*>(from + w * 32 * (DP + 4));
+          o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        }
+        const int64_t tok = sq.first + cn / a.group;
+        const int hd = kv_head * a.group + (int)(cn % a.group);
+        if (alone) {
+          float t = kMinusInf, l = 0.f;
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(from + w * 32 * (DP + 4));
-        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+          for (int w = 0; w < kWaves; ++w) t = fmaxf(t, wave_ml[w][c].x);
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].x == kMinusInf ? 0.f : wave_ml[w][c].y * fast_exp2(wave_ml[w][c].x - t);
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          store4(a.c.O.p + tok * a.c.O.token + hd * a.c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        } else {
+          *reinterpret_cast<float4*>(a.part_o + ((tok * a.c.Hq + hd) * a.n_chunks + chunk) * DP + d) = o;
+        }
       }
-      const int64_t tok = sq.first + cn / a.group;
-      const int hd = kv_head * a.group + (int)(cn % a.group);
-      if (alone) {
-        float t = kMinusInf, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) t = fmaxf(t, wave_ml[w][c].x);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].x == kMinusInf ? 0.f : wave_ml[w][c].y * fast_exp2(wave_ml[w][c].x - t);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        store4(a.c.O.p + tok * a.c.O.token + hd * a.c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-      } else {
-        *reinterpret_cast<float4*>(a.part_o + ((tok * a.c.Hq + hd) * a.n_chunks + chunk) * DP + d) = o;
+      if (wave == 0 && half == 0 && live) {
+        const int64_t tok = sq.first + qi;
+        if (!alone) a.part_ml[(tok * a.c.Hq + head) * a.n_chunks + chunk] = float2{top, total};
+        else if (a.c.lse != nullptr)
+          a.c.lse[(int64_t)head * a.c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
       }
-    }
-    if (wave == 0 && half == 0 && live) {
-      const int64_t tok = sq.first + qi;
-      if (!alone) a.part_ml[(tok * a.c.Hq + head) * a.n_chunks + chunk] = float2{top, total};
-      else if (a.c.lse != nullptr)
-        a.c.lse[(int64_t)head * a.c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
     }
   }
 }
 
-// Joins the chunks of a column: a wave per (query, head), lanes along its elements.
+// Joins the chunks of a column: a wave per (query, head).  DP / 4 lanes take four elements each of every (256 / DP)-th chunk, so
+// that several chunks' loads are under way; the shares are added in a fixed order.
 template <int DP>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);  // query * Hq + head
+  constexpr int LANES = DP / 4, GROUPS = 64 / LANES;
+  const int lane = threadIdx.x & 63, part = lane / LANES, d = lane % LANES * 4;
   const int seq = blockIdx.y;
   const Sequence of = sequence(a.c, seq);
-  const Span sq = of.q, sk = of.k;
-  const int used = (sk.len + a.chunk - 1) / a.chunk;
+  const int used = (of.k.len + a.chunk - 1) / a.chunk;
   const int chunks = used < 1 ? 1 : used < a.n_chunks ? used : a.n_chunks;
-  for (int64_t i = n; i < (int64_t)sq.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
-    const int64_t tok = sq.first + i / a.c.Hq;
+  for (int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); i < (int64_t)of.q.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
+    const int64_t tok = of.q.first + i / a.c.Hq;
     const int head = (int)(i % a.c.Hq);
     const int64_t at = (tok * a.c.Hq + head) * a.n_chunks;
     float top = kMinusInf;
     for (int k = lane; k < chunks; k += 64) top = fmaxf(top, a.part_ml[at + k].x);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    float total = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int k = 0; k < chunks; ++k) {
+    float total = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = part; k < chunks; k += GROUPS) {
       const float2 ml = a.part_ml[at + k];
       const float by = ml.x == kMinusInf ? 0.f : fast_exp2(ml.x - top);
-      total += ml.y * by;
-      const float* o = a.part_o + (at + k) * DP;
-      if (lane < a.c.D) o0 = fmaf(o[lane], by, o0);
-      if (DP > 64 && lane + 64 < a.c.D) o1 = fmaf(o[lane + 64], by, o1);
+      total = fmaf(ml.y, by, total);
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.part_o + (at + k) * DP + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = d + e < a.c.D ? fmaf(x[e], by, o[e]) : 0.f;
+    }
+#pragma unroll
+    for (int m = LANES; m < 64; m <<= 1) {
+      total += __shfl_xor(total, m, 64);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m, 64);
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    bf16_t* out = a.c.O.p + tok * a.c.O.token + head * a.c.O.head;
-    if (lane < a.c.D) out[lane] = (bf16_t)f32_to_bf16_rne(o0 * inv);
-    if (DP > 64 && lane + 64 < a.c.D) out[lane + 64] = (bf16_t)f32_to_bf16_rne(o1 * inv);
+    if (part == 0)
+      store4(a.c.O.p + tok * a.c.O.token + head * a.c.O.head, d, a.c.D, pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
     if (a.c.lse != nullptr && lane == 0)
       a.c.lse[(int64_t)head * a.c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
   }
 }
 
 // How a call is cut: few queries per key head take the cache kernel.
-constexpr int64_t kFewColumns = 128;
+// The cache kernel serves up to kFewColumns (query, head) pairs to a key head -- more would pass over the keys once for every 32 --
+// and any number of them while its blocks (32 columns each, waves on different keys) are not more than fit the chip at once, where a
+// prompt's 128-query blocks leave most of it idle and walk over the keys four times as long: one image, 12 heads, 7.0 us against 8.3.
+constexpr int64_t kFewColumns = 128, kFewBlocks = 512, kCacheBlocks = 3072, kCutSequences = 512;
 struct CachePlan {
   bool taken;
   int chunk, n_chunks, n_row_tiles;
 };
 CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
   CachePlan p = {};
-  p.taken = max_q * group <= kFewColumns;
+  const int64_t row_tiles = (max_q * group + 31) / 32, blocks = (int64_t)B * Hkv * row_tiles;
+  p.taken = max_q * group <= kFewColumns || blocks <= kFewBlocks;
   if (!p.taken) return p;
-  p.n_row_tiles = (int)((max_q * group + 31) / 32);
-  // chunks so that there are about eight blocks to a compute unit (sequences differ in length), of 256 keys at least
-  const int64_t blocks = (int64_t)B * Hkv * p.n_row_tiles, target = 2048;
-  int64_t chunk = (max_k * blocks + target - 1) / target;
+  p.n_row_tiles = (int)(row_tiles > 0 ? row_tiles : 1);
+  // chunks of at least 256 keys, about kCacheBlocks of them if all sequences were of the longest length; none of them where there
+  // are sequences enough to go round (finding a chunk means adding up all of theirs)
+  int64_t chunk = (max_k * blocks + kCacheBlocks - 1) / kCacheBlocks;
   chunk = (chunk < 256 ? 256 : chunk + 127) / 128 * 128;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((max_k + chunk - 1) / chunk);
-  if (p.n_chunks < 1) p.n_chunks = 1;
+  if (p.n_chunks < 1 || B > kCutSequences) p.n_chunks = 1;
   return p;
 }
 
@@ -387,6 +442,8 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
   a.c = c;
   a.group = c.Hq / c.Hkv;
   a.scale_log2 = c.scale * kLog2e;
+  int cus = 0;
+  if (hipError_t e = compute_units(&cus); e != hipSuccess) return e;
   const CachePlan plan = cache_plan(c.B, c.Hkv, a.group, c.max_q, c.max_k);
   a.chunk = plan.chunk; a.n_chunks = plan.n_chunks; a.n_row_tiles = plan.n_row_tiles;
   a.n_tiles = (int)((c.max_q + kQueries - 1) / kQueries);
@@ -402,10 +459,12 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool WHOLE = decltype(whole)::value;
     if (plan.taken) {
-      const int64_t blocks = (int64_t)a.n_chunks * a.n_row_tiles * c.B * c.Hkv;
-      cache_kernel<DP, WHOLE><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
+      // (one, two or four blocks to a compute unit, as registers and LDS allow)
+      const int64_t items = (int64_t)plan.n_chunks * plan.n_row_tiles * c.B * c.Hkv, room = (int64_t)cus * (DP == 128 ? (WHOLE ? 1 : 2) : DP == 64 ? 2 : 4);
+      cache_kernel<DP, WHOLE><<<dim3((unsigned)(items < room ? items : room)), kThreads, 0, s>>>(a);
       if (a.n_chunks > 1) {
-        const dim3 join((unsigned)((c.max_q * c.Hq + kWaves - 1) / kWaves), (unsigned)c.B);
+        const int64_t waves = c.max_q * c.Hq, most = (waves + kWaves - 1) / kWaves;
+        const dim3 join((unsigned)(most < 1 ? 1 : most), (unsigned)c.B);
         cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
       }
     } else {
