@@ -63,6 +63,10 @@ __device__ __forceinline__ void softmax_step(f32x16_t (&s)[KB], float c, float& 
     }
 }
 
+// What a part's sums, taken against `ref`, count for against the maximum of all parts.  (-infinity: none of its scores was above
+// that; its sums are zeros, or NaN where a score was, which stays.)
+__device__ __forceinline__ float part_weight(float ref, float top) { return ref == kMinusInf ? 1.f : fast_exp2(ref - top); }
+
 constexpr int kKeys = 64;             // per tile
 constexpr int kQueries = kWaves * 32; // per block
 
@@ -312,8 +316,8 @@ __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_ke
       for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_ml[w][col].x);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
-        total += wave_ml[w][col].x == kMinusInf ? 0.f : wave_ml[w][col].y * fast_exp2(wave_ml[w][col].x - top);
-      const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - top);
+        total += wave_ml[w][col].y * part_weight(wave_ml[w][col].x, top);
+      const float by = part_weight(ref, top);
       float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_ke
 #pragma unroll
           for (int w = 0; w < kWaves; ++w) t = fmaxf(t, wave_ml[w][c].x);
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].x == kMinusInf ? 0.f : wave_ml[w][c].y * fast_exp2(wave_ml[w][c].x - t);
+          for (int w = 0; w < kWaves; ++w) l += wave_ml[w][c].y * part_weight(wave_ml[w][c].x, t);
           const float inv = l == 0.f ? 0.f : 1.f / l;
           store4(a.c.O.p + tok * a.c.O.token + hd * a.c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         } else {
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) 
 #pragma unroll 4
     for (int k = part; k < chunks; k += GROUPS) {
       const float2 ml = a.part_ml[at + k];
-      const float by = ml.x == kMinusInf ? 0.f : fast_exp2(ml.x - top);
+      const float by = part_weight(ml.x, top);
       total = fmaf(ml.y, by, total);
       const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.part_o + (at + k) * DP + d);
 #pragma unroll

@@ -374,7 +374,7 @@ struct KeyPlan {
   int chunk, n_chunks;
 };
 KeyPlan key_plan(int64_t Tk, int B, int Hkv, int group, int64_t max_q, int64_t max_k, bool causal) {
-  const int64_t most = (max_q + kQueries - 1) / kQueries * group;  // steps of a key tile
+  const int64_t most = max_k > 0 ? (max_q + kQueries - 1) / kQueries * group : 0;  // steps of a key tile
   const int64_t all_tiles = Tk / kRows + B, tiles = all_tiles < (int64_t)B * ((max_k + kRows - 1) / kRows) ? all_tiles : (int64_t)B * ((max_k + kRows - 1) / kRows);
   const int64_t total = tiles * Hkv * (causal ? (most + 1) / 2 : most);
   int64_t chunk = (total + kKeyBlocks - 1) / kKeyBlocks;

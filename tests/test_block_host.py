@@ -128,6 +128,7 @@ def test_attention_workspace(lib):
     back = lib.nm_attention_backward_workspace_bytes
     assert back(100, 100, 1, 4, 2, 64, 100, 100, 0) == 1792 and back(0, 100, 1, 4, 2, 64, 100, 100, 0) == 0
     assert back(8192, 8192, 1, 16, 4, 128, 8192, 8192, 1) > 8192 * 16 * 4
+    assert back(65536, 65536, 65535, 1, 1, 64, 8192, 0, 0) == 65536 * 4   # no keys: nothing to cut
     assert attention(lib, True, ws=None, bytes=0) == WORKSPACE
 
 

@@ -163,6 +163,20 @@ def test_keys_of_minus_infinity_do_not_count():
         assert float(none.abs().max()) == 0 and bool((lse == -float("inf")).all())
 
 
+@pytest.mark.parametrize("Lq,Lk,H", [(2, 3000, 2), (150, 150, 2), (2500, 130, 8)])
+def test_nan_stays_in_its_row(Lq, Lk, H):
+    """A query that holds a NaN has an output and a log-sum of NaN; the other queries have their own."""
+    import paper_2409_09708_amd as nm
+    Q, K, V, _ = tensors(25, Lq, Lk, H, H, 64)
+    o, bo, l, bl = ref.attention(Q, K, V, False, 0.125, [(0, Lq)], [(0, Lk)])
+    Q[1, 0, 5] = float("nan")
+    got, lse = nm.nm_attention(Q, K, V, lse=True)
+    assert bool(got[1, 0].isnan().all()) and bool(lse[0, 1].isnan())
+    got[1, 0], lse[0, 1] = o[1, 0], l[0, 1]
+    ref.close(got, o, bo)
+    ref.close(lse, l, bl)
+
+
 def test_offsets_past_32_bits():
     """A cache of over 2^31 elements, its last sequence behind them."""
     import paper_2409_09708_amd as nm
