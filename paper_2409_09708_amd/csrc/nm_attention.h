@@ -222,6 +222,59 @@ __device__ __forceinline__ void store4(bf16_t* row, int d, int D, uint32_t lo, u
   }
 }
 
+// A wave's 32 rows of DP elements, between memory and operands.  The operand form: lane l has, of row l % 32, the 16-byte pieces
+// 2 m + l / 32.  Loads and stores of just those would move 32 bytes of each of 32 rows; lanes 16 apart exchange pieces, so that an
+// instruction moves 64 bytes of each of 16: then v[i] is of row row(i, lane), piece piece(i, lane).  256 images of 12 heads: 90 us, 96
+// with pieces of 8 bytes stored from the accumulators; gradients of 64: 83 and 92.  (A second exchange, for whole lines, gave no more.)
+template <int DP>
+struct WaveRows {
+  static constexpr int N = DP / 16;
+  static __device__ __forceinline__ int row(int i, int lane) { return 16 * (i & 1) + (lane & 15); }
+  static __device__ __forceinline__ int piece(int i, int lane) { return 4 * (i >> 1) + 2 * (lane >> 4 & 1) + (lane >> 5); }
+  // From one form to the other.  (Even registers' odd groups of 16 lanes change places with odd registers' even ones.)
+  static __device__ __forceinline__ void exchange(u32x4_t (&v)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; n += 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const auto s = __builtin_amdgcn_permlane16_swap(v[n][e], v[n + 1][e], false, false);
+        v[n][e] = s[0];
+        v[n + 1][e] = s[1];
+      }
+  }
+  // Of the `rows` rows from `from` on, `stride` elements apart; zeros past them.  In the form of memory.
+  static __device__ __forceinline__ void load(u32x4_t (&v)[N], const bf16_t* from, int64_t stride, int rows, int lane) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row(i, lane);
+      v[i] = u32x4_t{0, 0, 0, 0};
+      if (r < rows) v[i] = *reinterpret_cast<const u32x4_t*>(from + r * stride + piece(i, lane) * 8);
+    }
+  }
+  // A transposed product (DP / 32 accumulators: a lane's column is a row of the output) times `by`, to the first `rows` rows.
+  static __device__ __forceinline__ void store(bf16_t* to, int64_t stride, int rows, const f32x16_t (&acc)[DP / 32], int lane, float by) {
+    u32x4_t v[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {  // (the lane has half of each piece, its partner 32 lanes away the other)
+      const f32x16_t& x = acc[n / 2];
+      const int r = n % 2 * 8;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const auto s = __builtin_amdgcn_permlane32_swap(pack_bf16x2(x[r + 2 * e] * by, x[r + 2 * e + 1] * by),
+                                                        pack_bf16x2(x[r + 4 + 2 * e] * by, x[r + 5 + 2 * e] * by), false, false);
+        v[n][e] = s[0];
+        v[n][2 + e] = s[1];
+      }
+    }
+    exchange(v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row(i, lane);
+      if (r < rows) *reinterpret_cast<u32x4_t*>(to + r * stride + piece(i, lane) * 8) = v[i];
+    }
+  }
+};
+
 // One column of a transposed product (DP / 32 accumulators: the elements of one row of the output) to memory, times `by`.
 template <int DP>
 __device__ __forceinline__ void store_column(bf16_t* row, const f32x16_t (&acc)[DP / 32], int lane, int D, float by) {

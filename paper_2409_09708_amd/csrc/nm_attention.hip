@@ -159,9 +159,11 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
       }
     }
     sum = half_sum(sum);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    bf16_t* o_rows = a.c.O.p + (sq.first + q_wave) * a.c.O.token + head * a.c.O.head;
+    if constexpr (WHOLE) WaveRows<DP>::store(o_rows, a.c.O.token, sq.len - q_wave, acc, lane, inv);
     if (live) {
-      bf16_t* o_row = a.c.O.p + (sq.first + qi) * a.c.O.token + head * a.c.O.head;
-      store_column<DP>(o_row, acc, lane, D, sum == 0.f ? 0.f : 1.f / sum);
+      if constexpr (!WHOLE) store_column<DP>(o_rows + (lane & 31) * a.c.O.token, acc, lane, D, inv);
       if (a.c.lse != nullptr && half == 0)
         a.c.lse[(int64_t)head * a.c.Tq + sq.first + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
     }
@@ -459,10 +461,11 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) +
                                           round256(columns * padded_head(c.D) * sizeof(float)));
   }
-  auto launch = [&](auto dp, auto whole) {
-    constexpr int DP = decltype(dp)::value;
-    constexpr bool WHOLE = decltype(whole)::value;
-    if (plan.taken) {
+  const bool whole_keys = whole_rows(c.K) && whole_rows(c.V);
+  if (plan.taken) {
+    with_head(c.D, whole_keys, [&](auto dp, auto whole) {
+      constexpr int DP = decltype(dp)::value;
+      constexpr bool WHOLE = decltype(whole)::value;
       // (one, two or four blocks to a compute unit, as registers and LDS allow)
       const int64_t items = (int64_t)plan.n_chunks * plan.n_row_tiles * c.B * c.Hkv, room = (int64_t)cus * (DP == 128 ? (WHOLE ? 1 : 2) : DP == 64 ? 2 : 4);
       cache_kernel<DP, WHOLE><<<dim3((unsigned)(items < room ? items : room)), kThreads, 0, s>>>(a);
@@ -471,11 +474,13 @@ hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {
         const dim3 join((unsigned)(most < 1 ? 1 : most), (unsigned)c.B);
         cache_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
       }
-    } else {
-      prompt_kernel<DP, WHOLE><<<dim3((unsigned)tile_blocks(c.B, c.Hkv, a.group, a.n_tiles)), kThreads, 0, s>>>(a);
-    }
-  };
-  with_head(c.D, whole_rows(c.K) && whole_rows(c.V), launch);
+    });
+  } else {
+    with_head(c.D, whole_keys && whole_rows(c.Q) && whole_rows(c.O), [&](auto dp, auto whole) {
+      const int64_t blocks = tile_blocks(c.B, c.Hkv, a.group, a.n_tiles);
+      prompt_kernel<decltype(dp)::value, decltype(whole)::value><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a);
+    });
+  }
   return hipGetLastError();
 }
 

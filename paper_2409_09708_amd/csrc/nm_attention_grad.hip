@@ -11,6 +11,9 @@
 // are 32-bit floats; p and dS are rounded to bfloat16 as operands of the products that take them.
 #include "nm_attention.h"
 
+#include <algorithm>
+#include <iterator>
+
 namespace nm {
 
 namespace {
@@ -33,6 +36,7 @@ constexpr int64_t kKeyBlocks = 512;    // blocks that grad_key_kernel's work is 
 template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
+  using Rows = WaveRows<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kKeys * Tile::kRowBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];
   TilePlace at;
@@ -59,20 +63,35 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
     const int qi = q_wave + (lane & 31);
     const bool live = qi < sq.len;
     const int64_t tok = sq.first + qi;
-    const bf16_t* q_row = a.c.Q.p + tok * a.c.Q.token + head * a.c.Q.head;
-    const bf16_t* do_row = a.c.dO.p + tok * a.c.dO.token + head * a.c.dO.head;
-    const bf16_t* o_row = a.c.O.p + tok * a.c.O.token + head * a.c.O.head;
+    const bf16_t* q_rows = a.c.Q.p + (sq.first + q_wave) * a.c.Q.token + head * a.c.Q.head;
+    const bf16_t* do_rows = a.c.dO.p + (sq.first + q_wave) * a.c.dO.token + head * a.c.dO.head;
+    const bf16_t* o_rows = a.c.O.p + (sq.first + q_wave) * a.c.O.token + head * a.c.O.head;
     u32x4_t q[STEPS], g[STEPS];
     float delta = 0.f;
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-      g[st] = load_piece(do_row, 16 * st + 8 * half, D, live);
-      const u32x4_t o = load_piece(o_row, 16 * st + 8 * half, D, live);
+    auto add = [&](u32x4_t x, u32x4_t o) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        delta = fmaf(__uint_as_float(g[st][e] << 16), __uint_as_float(o[e] << 16), delta);
-        delta = fmaf(__uint_as_float(g[st][e] & 0xFFFF0000u), __uint_as_float(o[e] & 0xFFFF0000u), delta);
+        delta = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(o[e] << 16), delta);
+        delta = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(o[e] & 0xFFFF0000u), delta);
+      }
+    };
+    if constexpr (WHOLE) {
+      u32x4_t o[STEPS];
+      Rows::load(g, do_rows, a.c.dO.token, sq.len - q_wave, lane);
+      Rows::load(o, o_rows, a.c.O.token, sq.len - q_wave, lane);
+      Rows::load(q, q_rows, a.c.Q.token, sq.len - q_wave, lane);
+      Rows::exchange(g);
+      Rows::exchange(o);
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) add(g[st], o[st]);
+      Rows::exchange(q);
+    } else {
+      const int row = lane & 31;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        q[st] = load_piece(q_rows + row * a.c.Q.token, 16 * st + 8 * half, D, live);
+        g[st] = load_piece(do_rows + row * a.c.dO.token, 16 * st + 8 * half, D, live);
+        add(g[st], load_piece(o_rows + row * a.c.O.token, 16 * st + 8 * half, D, live));
       }
     }
     delta = half_sum(delta);
@@ -139,7 +158,9 @@ __global__ void __launch_bounds__(kThreads, 2) grad_query_kernel(const GradArgs 
         }
       }
     }
-    if (live) store_column<DP>(a.c.dQ.p + tok * a.c.dQ.token + head * a.c.dQ.head, acc, lane, D, a.c.scale);
+    bf16_t* dq_rows = a.c.dQ.p + (sq.first + q_wave) * a.c.dQ.token + head * a.c.dQ.head;
+    if constexpr (WHOLE) Rows::store(dq_rows, a.c.dQ.token, sq.len - q_wave, acc, lane, a.c.scale);
+    else if (live) store_column<DP>(dq_rows + (lane & 31) * a.c.dQ.token, acc, lane, D, a.c.scale);
   }
 }
 
@@ -166,6 +187,7 @@ __device__ __forceinline__ KeySteps key_steps(const GradArgs& a, int tile, int q
 template <int DP, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_key_kernel(const GradArgs a) {
   using Tile = RowTile<DP>;
+  using Rows = WaveRows<DP>;
   constexpr int NB = DP / 32, STEPS = DP / 16, TILE_BYTES = kQueries * Tile::kRowBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * TILE_BYTES];  // two stages of queries and dO
   __shared__ __attribute__((aligned(16))) float rows[2][2][kQueries];               // ... and of lse (base 2) and D
@@ -198,16 +220,29 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
     const int k_wave = tile * kRows + wave * 32;
     const int kj = k_wave + (lane & 31);
     const int64_t tok = sk.first + kj;
-    const bf16_t* k_row = a.c.K.p + tok * a.c.K.token + at.kv_head * a.c.K.head;
-    const bf16_t* v_row = a.c.V.p + tok * a.c.V.token + at.kv_head * a.c.V.head;
+    const bf16_t* k_rows = a.c.K.p + (sk.first + k_wave) * a.c.K.token + at.kv_head * a.c.K.head;
+    const bf16_t* v_rows = a.c.V.p + (sk.first + k_wave) * a.c.V.token + at.kv_head * a.c.V.head;
     u32x4_t k[STEPS], v[STEPS];
     unsigned char* own = kept + wave * 32 * Tile::kRowBytes;
     const uint32_t kept_tile = NM_LDS_ADDRESS(kept) + wave * 32 * Tile::kRowBytes;
+    if constexpr (WHOLE) {
+      Rows::load(k, k_rows, a.c.K.token, sk.len - k_wave, lane);
+      Rows::load(v, v_rows, a.c.V.token, sk.len - k_wave, lane);
+      if constexpr (KEEP) {
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      k[st] = load_piece(k_row, 16 * st + 8 * half, D, kj < sk.len);
-      if constexpr (KEEP) *reinterpret_cast<u32x4_t*>(own + Tile::place(lane & 31, 2 * st + half)) = k[st];
-      v[st] = load_piece(v_row, 16 * st + 8 * half, D, kj < sk.len);
+        for (int i = 0; i < STEPS; ++i) *reinterpret_cast<u32x4_t*>(own + Tile::place(Rows::row(i, lane), Rows::piece(i, lane))) = k[i];
+      } else {
+        Rows::exchange(k);
+      }
+      Rows::exchange(v);
+    } else {
+      const int row = lane & 31;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        k[st] = load_piece(k_rows + row * a.c.K.token, 16 * st + 8 * half, D, kj < sk.len);
+        if constexpr (KEEP) *reinterpret_cast<u32x4_t*>(own + Tile::place(row, 2 * st + half)) = k[st];
+        v[st] = load_piece(v_rows + row * a.c.V.token, 16 * st + 8 * half, D, kj < sk.len);
+      }
     }
     f32x16_t dk[NB], dv[NB];
 #pragma unroll
@@ -318,15 +353,22 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
             *reinterpret_cast<float4*>(to + DP + 32 * b + acc_row(r)) = float4{dv[b][r], dv[b][r + 1], dv[b][r + 2], dv[b][r + 3]};
           }
       }
-    } else if (kj < of.room) {
+    } else {
       if (kj >= sk.len) {  // (it was multiplied as a row of zeros: what came of that, infinities included, is not its gradient)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.f;
       }
-      store_column<DP>(a.c.dK.p + tok * a.c.dK.token + at.kv_head * a.c.dK.head, dk, lane, D, a.c.scale);
-      store_column<DP>(a.c.dV.p + tok * a.c.dV.token + at.kv_head * a.c.dV.head, dv, lane, D, 1.f);
+      bf16_t* dk_rows = a.c.dK.p + (sk.first + k_wave) * a.c.dK.token + at.kv_head * a.c.dK.head;
+      bf16_t* dv_rows = a.c.dV.p + (sk.first + k_wave) * a.c.dV.token + at.kv_head * a.c.dV.head;
+      if constexpr (WHOLE) {
+        Rows::store(dk_rows, a.c.dK.token, of.room - k_wave, dk, lane, a.c.scale);
+        Rows::store(dv_rows, a.c.dV.token, of.room - k_wave, dv, lane, 1.f);
+      } else if (kj < of.room) {
+        store_column<DP>(dk_rows + (lane & 31) * a.c.dK.token, dk, lane, D, a.c.scale);
+        store_column<DP>(dv_rows + (lane & 31) * a.c.dV.token, dv, lane, D, 1.f);
+      }
     }
   }
 }
@@ -415,7 +457,8 @@ hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s) {
   a.n_k_tiles = tiles(c.max_k, c.B, c.Hkv, a.n_chunks);
   a.delta = static_cast<float*>(c.workspace);
   a.part = a.delta + round256((size_t)c.Tq * c.Hq * sizeof(float)) / sizeof(float);
-  with_head(c.D, whole_rows(c.K) && whole_rows(c.V) && whole_rows(c.Q) && whole_rows(c.dO), [&](auto dp, auto whole) {
+  const HeadRows* all[] = {&c.Q, &c.K, &c.V, &c.O, &c.dO, &c.dQ, &c.dK, &c.dV};
+  with_head(c.D, std::all_of(std::begin(all), std::end(all), [](const HeadRows* r) { return whole_rows(*r); }), [&](auto dp, auto whole) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool WHOLE = decltype(whole)::value;
     const int64_t q_blocks = tile_blocks(c.B, c.Hkv, a.group, a.n_q_tiles);

@@ -163,6 +163,17 @@ def test_keys_of_minus_infinity_do_not_count():
         assert float(none.abs().max()) == 0 and bool((lse == -float("inf")).all())
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [32, 40, 64, 100, 128])
+def test_many_sequences(D, causal):
+    """More query tiles than blocks: some with no queries, no keys, fewer keys than queries, and more tiles than the hint says."""
+    lens = [(0, 5), (1, 1), (130, 0), (300, 300), (127, 64), (0, 0), (64, 200), (257, 31), (128, 128), (3, 65), (200, 129)] * 9
+    Tq, Tk = sum(q for q, _ in lens), sum(k for _, k in lens)
+    Q, K, V, dO = tensors(27, Tq, Tk, 8, 4, D)
+    for hint in (300, 150):
+        check(Q, K, V, dO, causal, q_lens=[q for q, _ in lens], k_lens=[k for _, k in lens], backward=hint == 300, max_q=hint, max_k=300)
+
+
 @pytest.mark.parametrize("Lq,Lk,H", [(2, 3000, 2), (150, 150, 2), (2500, 130, 8)])
 def test_nan_stays_in_its_row(Lq, Lk, H):
     """A query that holds a NaN has an output and a log-sum of NaN; the other queries have their own."""
