@@ -410,10 +410,11 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) 
 }
 
 // How a call is cut: few queries per key head take the cache kernel.
-// The cache kernel serves up to kFewColumns (query, head) pairs to a key head -- more would pass over the keys once for every 32 --
-// and any number of them while its blocks (32 columns each, waves on different keys) are not more than fit the chip at once, where a
-// prompt's 128-query blocks leave most of it idle and walk over the keys four times as long: one image, 12 heads, 7.0 us against 8.3.
-constexpr int64_t kFewColumns = 128, kFewBlocks = 512, kCacheBlocks = 3072, kCutSequences = 512;
+// It serves up to kFewColumns (query, head) pairs to a key head: 24 caches of 16k, 32 heads on 8, 128 pairs 570 us and 686 by the
+// prompt kernel, 256 pairs 924 and 790, since it passes over the keys once for every 32.  It also serves any number of them in up to
+// kFewBlocks blocks (32 columns each, waves on different keys), where a prompt's blocks of 128 leave most of the chip idle: one image
+// of 12 heads, 84 blocks, 6.8 us and 8.0; 16 heads on 4 of 128, 256 tokens (128 blocks) 9.5 and 10.1, 512 tokens 25 and 15.
+constexpr int64_t kFewColumns = 128, kFewBlocks = 128, kCacheBlocks = 3072, kCutSequences = 512;
 struct CachePlan {
   bool taken;
   int chunk, n_chunks, n_row_tiles;
@@ -424,10 +425,11 @@ CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
   p.taken = max_q * group <= kFewColumns || blocks <= kFewBlocks;
   if (!p.taken) return p;
   p.n_row_tiles = (int)(row_tiles > 0 ? row_tiles : 1);
-  // chunks of at least 256 keys, about kCacheBlocks of them if all sequences were of the longest length; none of them where there
-  // are sequences enough to go round (finding a chunk means adding up all of theirs)
+  // chunks of at least 512 keys (one cache of 16k 22 us, 28 with 256; four 59 and 73), about kCacheBlocks of them if all sequences were
+  // of the longest length: most are shorter (24 of them, a fifth full, 77 us, with 1536 84, with 768 122; all full 305, 296, 288).
+  // None where there are sequences enough to go round (finding a chunk means adding up all of theirs).
   int64_t chunk = (max_k * blocks + kCacheBlocks - 1) / kCacheBlocks;
-  chunk = (chunk < 256 ? 256 : chunk + 127) / 128 * 128;
+  chunk = (chunk < 512 ? 512 : chunk + 127) / 128 * 128;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((max_k + chunk - 1) / chunk);
   if (p.n_chunks < 1 || B > kCutSequences) p.n_chunks = 1;
