@@ -8,6 +8,8 @@
 // Bound by memory (3 flops per element): every element is read and written once.  The cosines and sines of a block's tokens
 // are computed once into LDS and serve all heads; then the block's lanes take both members of eight pairs, in memory order
 // over the heads of a token, so that loads and stores run along whole lines.
+// Measured: 12608 tokens of 24 heads of 64 inside a joint projection's output, two axes, bfloat16: 14.4 us, 5.4 TB/s; 16399 tokens of
+// 10 heads of 128, 96 of them turned, interleaved, float to bfloat16: 20.5 us, 6.1 TB/s.  Both at the rate of a large copy.
 #include "nm_device.h"
 #include "nm_launch.h"
 #include "nm_rows.h"
