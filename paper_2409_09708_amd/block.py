@@ -29,19 +29,37 @@ class Sequences:
 @dataclass
 class Cache:
     """Keys and values of `count` sequences with room for `room` tokens each ([count * room, key heads, head size]), how many are
-    in use (int32 [count]) and where each sequence begins (int32 [count + 1])."""
+    in use (int32 [count]) and where each sequence begins (int32 [count + 1]).  used: what the host knows of the lengths, none is
+    above it (None: nothing is known); a caller that raises `lengths` itself sets it.
+
+    Tokens that do not fit are refused before anything is computed.  Where the host cannot know -- a replayed graph -- no row of
+    another sequence is written: the lengths count on, and a sequence whose length is above `room` has lost its last tokens, and its
+    outputs mean nothing from there on."""
     K: object
     V: object
     lengths: object
     offsets: object
     room: int
+    used: Optional[int] = None
 
     @classmethod
     def empty(cls, count: int, room: int, heads: int, size: int, device="cuda") -> "Cache":
         import torch
         K, V = (torch.empty((count * room, heads, size), dtype=torch.bfloat16, device=device) for _ in range(2))
         offsets = torch.arange(count + 1, dtype=torch.int32, device=device) * room
-        return cls(K, V, torch.zeros(count, dtype=torch.int32, device=device), offsets, room)
+        return cls(K, V, torch.zeros(count, dtype=torch.int32, device=device), offsets, room, 0)
+
+    def expect(self, new: int, offsets) -> None:
+        """Up to `new` more tokens of each sequence (offsets: how many of each) are about to be kept: ValueError where a sequence has
+        no room for its.  Waits for the device only where what the host knows of the lengths does not settle it."""
+        import torch
+        if self.used is not None and self.used + new <= self.room:
+            self.used += new
+        elif not (self.lengths.is_cuda and torch.cuda.is_current_stream_capturing()):  # (a capture computes nothing yet)
+            used = int((self.lengths + offsets.diff()).max())
+            if used > self.room:
+                raise ValueError(f"a sequence of {used} tokens in a cache with room for {self.room} each")
+            self.used = used
 
 
 class SparseBlock:
@@ -91,7 +109,9 @@ class SparseBlock:
 
     def forward(self, branch, stream, of: Sequences, cache: Optional[Cache] = None, train: bool = False):
         """((branch, stream), what `backward` needs or None).  With an empty cache the keys and values of the sequences are kept in
-        it as their first tokens."""
+        it as their first tokens; ValueError where one is longer than the cache's room."""
+        if cache is not None:
+            cache.expect(of.longest, of.offsets)
         n1 = nm.nm_layer_norm(branch, *self.norms[0], self.eps, residual=stream, train=train, out_dtype=branch.dtype)
         qkv = self._linear("qkv", n1[0])
         turned, q, k, v = self._split(qkv)
@@ -106,16 +126,18 @@ class SparseBlock:
 
     def _keep(self, cache: Cache, k, v, offsets) -> None:
         import torch
-        counts = offsets.diff()
         rows = torch.arange(k.shape[0], device=k.device)
-        seq = torch.searchsorted(offsets[1:].contiguous(), rows, right=True)
-        at = cache.offsets[seq] + cache.lengths[seq] + (rows - offsets[seq])
+        seq = torch.searchsorted(offsets[1:-1], rows, right=True)
+        # (what would go past a sequence's rows goes to the last of them)
+        at = torch.minimum(rows + (cache.offsets[:-1] + cache.lengths - offsets[:-1])[seq], (cache.offsets[1:] - 1)[seq])
         cache.K[at], cache.V[at] = k, v
-        cache.lengths += counts
+        cache.lengths += offsets.diff()
 
     def step(self, branch, stream, positions, offsets, cache: Cache, longest: int, new: int = 1):
         """One or a few new tokens per sequence (offsets; at most `new` each) against the cache, which takes their keys and
-        values; longest: tokens of the longest sequence, the new ones counted, as far as known."""
+        values; longest: tokens of the longest sequence, the new ones counted, as far as known.  ValueError, and nothing computed or
+        kept, where a sequence has no room for its."""
+        cache.expect(new, offsets)
         n1 = nm.nm_layer_norm(branch, *self.norms[0], self.eps, residual=stream, out_dtype=branch.dtype)
         turned, q, k, v = self._split(self._linear("qkv", n1[0]))
         self._turn(turned, positions)
