@@ -23,6 +23,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_ptr;
 typedef __attribute__((address_space(3))) const u32x4_t* lds_u32x4_ptr;
+typedef __attribute__((address_space(3))) u32x4_t* lds_u32x4_out_ptr;
 
 __device__ __forceinline__ f32x16_t mma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
@@ -125,11 +126,13 @@ __device__ __forceinline__ u32x4_t load_piece(const bf16_t* row, int d, int D, b
 // Two tiles of ROWS rows (of keys and values, or of queries and dO) from memory to LDS, by LANES lanes: a block of kThreads, or a
 // wave.
 // WHOLE (rows of exactly DP elements, all 16-byte aligned): asynchronous copies straight to LDS, one wave-load a kilobyte; rows past
-// the last one repeat it, so the scores of those have to be hidden.  Otherwise through registers, with zeros past the last row
-// and the last element.
-//   fetch(stage, row0)   starts the loads of a tile (rows row0 .., one of them there at least)
-//   settle(stage)        the tile is in LDS, as far as this wave brought it, up to LATER copies started after it: a block's
-//                        barrier follows
+// the last one repeat it, so the scores of those have to be hidden, and they must not be summed (clear_past).  Otherwise through
+// registers, with zeros past the last row and the last element.
+//   fetch(stage, row0)       starts the loads of a tile (rows row0 .., one of them there at least)
+//   settle(stage)            the tile is in LDS, as far as this wave brought it, up to LATER copies started after it: a block's
+//                            barrier follows
+//   clear_past(stage, row0)  between the two, where the second tile's rows are summed: zeros for those past the last one, again as far
+//                            as this wave brought them.  (Their weight is zero, and zero times an infinity in the last row is NaN.)
 template <int DP, int ROWS, bool WHOLE, int LANES>
 struct TilePair {
   using Tile = RowTile<DP>;
@@ -188,6 +191,21 @@ struct TilePair {
           if (kPieces % LANES == 0 || i < kPieces)
             *reinterpret_cast<u32x4_t*>(smem + (2 * stage + t) * kBytes + Tile::place(i / Tile::kPieces, i % Tile::kPieces)) = in[t][n];
         }
+    }
+  }
+  __device__ __forceinline__ void clear_past(int stage, int row0) {
+    if constexpr (WHOLE) {
+      const int there = rows - row0;
+      if (there >= ROWS) return;
+      int tid = threadIdx.x % LANES;
+      uint32_t zero = 0;
+      asm volatile("" : "+v"(tid), "+v"(zero));  // (computed here, in a sequence's last tile: held over the loop it would cost registers)
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        const int i = n * LANES + tid;  // the piece that this lane's copy brought
+        if (i / Tile::kPieces >= there && (kPieces % LANES == 0 || i < kPieces))
+          *(lds_u32x4_out_ptr)(uintptr_t)(lds + (2 * stage + 1) * kBytes + i * 16) = u32x4_t{zero, zero, zero, zero};
+      }
     }
   }
 };

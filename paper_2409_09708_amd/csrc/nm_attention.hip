@@ -134,8 +134,13 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(const AttnArgs a) {
     for (int kt = 0; kt < n_key_tiles; ++kt) {
       const int k0 = kt * kKeys;
       load.settle(kt & 1);
-      __syncthreads();
-      if (kt + 1 < n_key_tiles) load.fetch((kt + 1) & 1, k0 + kKeys);
+      if (kt + 1 < n_key_tiles) {
+        __syncthreads();
+        load.fetch((kt + 1) & 1, k0 + kKeys);
+      } else {
+        load.clear_past(kt & 1, k0);
+        __syncthreads();
+      }
       if (k0 < wave_end) {
         const uint32_t k_tile = load.lds + (uint32_t)(kt & 1) * 2 * TILE_BYTES, v_tile = k_tile + TILE_BYTES;
         const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
@@ -290,6 +295,7 @@ __global__ void __launch_bounds__(kThreads, WHOLE && DP == 128 ? 1 : 2) cache_ke
             load.template settle<2 * Load::kLoads>(stage);
           } else {
             load.settle(stage);
+            load.clear_past(stage, k0);
           }
         } else {
           load.settle(0);

@@ -285,11 +285,13 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
     for (int step = first_step; step < end_step; ++step) {
       const int stage = (step - first_step) & 1, q_now = q0;
       if (tid < 2 * kQueries) {
-        // no row: a log-sum of infinity, and so probabilities of zero; a query that sees no key: any finite one
-        const float lse2 = q_now + tid >= sq.len ? -kMinusInf : row_in == kMinusInf ? 0.f : row_in * kLog2e;
-        rows[stage][tid / kQueries][tid % kQueries] = tid < kQueries ? lse2 : row_in;
+        // no row: a log-sum of infinity, and so probabilities of zero, and a D of zero; a query that sees no key: any finite log-sum
+        const bool there = q_now + tid % kQueries < sq.len;
+        const float lse2 = !there ? -kMinusInf : row_in == kMinusInf ? 0.f : row_in * kLog2e;
+        rows[stage][tid / kQueries][tid % kQueries] = tid < kQueries ? lse2 : there ? row_in : 0.f;
       }
       load.settle(stage);
+      load.clear_past(stage, q_now);
       __syncthreads();
       if (step + 1 < end_step) {
         q0 -= kQueries;
