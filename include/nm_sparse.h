@@ -584,7 +584,8 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
  *   lse         out float [heads_q, Tq], or NULL
  *   workspace   scratch of nm_attention_workspace_bytes() bytes, 256-byte aligned (few queries against many keys: the keys are
  *               cut into chunks for different blocks, whose results a second launch joins); NULL allowed when that size is 0.
- *               Contents undefined afterwards; concurrent calls need distinct workspaces.
+ *               The size for some max_k does for any smaller one as well, Tk being what it may.  Contents undefined afterwards;
+ *               concurrent calls need distinct workspaces.
  * Scores, their maximum, sums and outputs are 32-bit floats; exp(s_j - ..) is rounded to bfloat16 as operand of the product with
  * the values.  Values that a query does not see inside its sequence are multiplied by zero, so they have to be finite.
  *
@@ -593,8 +594,9 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
  *   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i p_ij dO_i, the latter two summed over the
  *   query heads that share the key head; keys past lengths_k get zeros.
  *   workspace   nm_attention_backward_workspace_bytes() bytes, 256-byte aligned: D, and where few key tiles are there for many
- *               queries, 32-bit sums of runs of queries, which a further launch adds in order.  Contents undefined afterwards;
- *               concurrent calls need distinct workspaces.
+ *               queries, 32-bit sums of runs of queries, which a further launch adds in order.  The size is that of a call with just
+ *               these arguments: fewer keys can be cut further.  Contents undefined afterwards; concurrent calls need distinct
+ *               workspaces.
  * Every sum is taken in a fixed order: results repeat bit for bit.
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (Tq <= 0, Tk < 0, either above 2^30; sequences outside [1, 65535], heads_q no multiple of heads_kv,
  * sequences * heads_q above 2^20, head_size outside [1, 128], max_q, max_k < 0, negative strides, tokens or heads of an output that

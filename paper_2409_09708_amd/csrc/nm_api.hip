@@ -624,9 +624,10 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
 }
 
 namespace {
+constexpr int64_t kMostTokens = (int64_t)1 << 30;
 bool attention_sizes_ok(int64_t Tq, int64_t sequences, int64_t heads_q, int64_t heads_kv, int64_t head_size, int64_t max_q,
                         int64_t max_k) {
-  return Tq > 0 && Tq <= (int64_t)1 << 30 && sequences >= 1 && sequences <= 65535 && heads_q >= 1 && heads_kv >= 1 &&
+  return Tq > 0 && Tq <= kMostTokens && sequences >= 1 && sequences <= 65535 && heads_q >= 1 && heads_kv >= 1 &&
          heads_q % heads_kv == 0 && sequences * heads_q <= 1 << 20 && head_size >= 1 && head_size <= 128 && max_q >= 0 && max_k >= 0;
 }
 
@@ -637,7 +638,7 @@ int32_t attention_check(const nm_attention_desc* d, bool backward, nm::Attention
   if (backward && (!d->dO.data || !d->dQ.data || (keys && (!d->dK.data || !d->dV.data)) || !d->lse)) return NM_ERR_NULL;
   if ((!d->offsets_q || !d->offsets_k) && d->sequences != 1) return d->sequences < 1 ? NM_ERR_SHAPE : NM_ERR_NULL;
   if (!attention_sizes_ok(d->Tq, d->sequences, d->heads_q, d->heads_kv, d->head_size, d->max_q, d->max_k)) return NM_ERR_SHAPE;
-  if (d->Tk < 0 || d->Tk > (int64_t)1 << 30) return NM_ERR_SHAPE;
+  if (d->Tk < 0 || d->Tk > kMostTokens) return NM_ERR_SHAPE;
   if (!(d->scale > 0.f) || d->scale > 3.0e38f) return NM_ERR_SHAPE;
   auto take = [&](const nm_heads& h, nm::HeadRows* r, int64_t T, int64_t H, bool output) {
     *r = nm::HeadRows{h.data, h.token, h.head};
@@ -668,7 +669,8 @@ int32_t attention_check(const nm_attention_desc* d, bool backward, nm::Attention
 size_t nm_attention_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size,
                                     int64_t max_q, int64_t max_k) {
   if (!attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, max_k)) return 0;
-  return nm::attention_workspace_bytes(Tq, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq, max_k);
+  // (the call cuts max_k to its number of keys, which this does not know)
+  return nm::attention_workspace_most(Tq, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq, max_k < kMostTokens ? max_k : kMostTokens);
 }
 
 int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
@@ -682,7 +684,7 @@ int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t work
 
 size_t nm_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int32_t sequences, int32_t heads_q, int32_t heads_kv,
                                              int32_t head_size, int64_t max_q, int64_t max_k, int32_t causal) {
-  if (!attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, max_k) || Tk < 0 || Tk > (int64_t)1 << 30) return 0;
+  if (!attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, max_k) || Tk < 0 || Tk > kMostTokens) return 0;
   return nm::attention_grad_workspace_bytes(Tq, Tk, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq,
                                             max_k < Tk ? max_k : Tk, causal != 0);
 }

@@ -426,10 +426,11 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(const AttnArgs a) 
 // prompt kernel, 256 pairs 924 and 790, since it passes over the keys once for every 32.  It also serves any number of them in up to
 // kFewBlocks blocks (32 columns each, waves on different keys), where a prompt's blocks of 128 leave most of the chip idle: one image
 // of 12 heads, 84 blocks, 6.8 us and 8.0; 16 heads on 4 of 128, 256 tokens (128 blocks) 9.5 and 10.1, 512 tokens 25 and 15.
-constexpr int64_t kFewColumns = 128, kFewBlocks = 128, kCacheBlocks = 3072, kCutSequences = 512;
+constexpr int64_t kFewColumns = 128, kFewBlocks = 128, kLeastChunk = 512, kCacheBlocks = 3072, kCutSequences = 512;
 struct CachePlan {
   bool taken;
   int chunk, n_chunks, n_row_tiles;
+  int64_t most_chunks;  // n_chunks of any number of keys up to max_k: n_chunks itself falls where chunks are rounded up to 128 keys
 };
 CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
   CachePlan p = {};
@@ -441,20 +442,34 @@ CachePlan cache_plan(int B, int Hkv, int group, int64_t max_q, int64_t max_k) {
   // of the longest length: most are shorter (24 of them, a fifth full, 77 us, with 1536 84, with 768 122; all full 305, 296, 288).
   // None where there are sequences enough to go round (finding a chunk means adding up all of theirs).
   int64_t chunk = (max_k * blocks + kCacheBlocks - 1) / kCacheBlocks;
-  chunk = (chunk < 512 ? 512 : chunk + 127) / 128 * 128;
+  chunk = (chunk < kLeastChunk ? kLeastChunk : chunk + 127) / 128 * 128;
   p.chunk = (int)chunk;
   p.n_chunks = (int)((max_k + chunk - 1) / chunk);
+  // (a chunk has kLeastChunk keys or more, and no fewer than max_k * blocks / kCacheBlocks)
+  const int64_t by_least = (max_k + kLeastChunk - 1) / kLeastChunk, by_blocks = blocks > 0 ? (kCacheBlocks + blocks - 1) / blocks : by_least;
+  p.most_chunks = by_least < by_blocks ? by_least : by_blocks;
   if (p.n_chunks < 1 || B > kCutSequences) p.n_chunks = 1;
+  if (p.most_chunks < 1 || B > kCutSequences) p.most_chunks = 1;
   return p;
 }
 
 }  // namespace
 
+namespace {
+size_t chunks_bytes(int64_t Tq, int Hq, int D, int64_t n_chunks) {
+  if (n_chunks <= 1) return 0;
+  const size_t columns = (size_t)Tq * Hq * n_chunks;
+  return round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2);
+}
+}  // namespace
+
 size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k) {
   const CachePlan p = cache_plan(B, Hkv, Hq / Hkv, max_q, max_k);
-  if (!p.taken || p.n_chunks == 1) return 0;
-  const size_t columns = (size_t)Tq * Hq * p.n_chunks;
-  return round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2);
+  return chunks_bytes(Tq, Hq, D, p.taken ? p.n_chunks : 1);
+}
+size_t attention_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k) {
+  const CachePlan p = cache_plan(B, Hkv, Hq / Hkv, max_q, max_k);
+  return chunks_bytes(Tq, Hq, D, p.taken ? p.most_chunks : 1);
 }
 
 hipError_t launch_attention(const AttentionCall& c, hipStream_t s) {

@@ -297,6 +297,7 @@ struct AttentionCall {
   void* workspace;
 };
 size_t attention_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k);
+size_t attention_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k);  // ... of any max_k up to this
 hipError_t launch_attention(const AttentionCall& c, hipStream_t s);
 size_t attention_grad_workspace_bytes(int64_t Tq, int64_t Tk, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k,
                                       bool causal);
