@@ -8,8 +8,12 @@
 //   dw = sum over rows of dy n,  db = sum over rows of dy.
 //
 // All sums, statistics and the normalised values are 32-bit floats; a value is rounded once, when it is stored as
-// bfloat16.  The mean is taken first and the variance from the differences to it (the row lies in registers, so the
-// second sum costs no memory traffic), which keeps rows with a large common offset exact.
+// bfloat16.  The mean m of one sum is off by the roundings of that sum, for rows with a large common offset by more than their
+// spread.  So with the squares of the differences to it goes their sum (the row lies in registers: no memory traffic):
+//
+//   e = mean(s - m),  mu = m + e,  variance = mean((s - m)^2) - e^2,  y = ((s - m) - e) rstd w + b
+//
+// where s - m is exact once m is close.  (Rows of 768 times 10000.1, eps 1e-6: y was -0.7, and is 0 to 10^-5.)
 //
 // Bound by memory at any width: 8 flops per element forward, 14 backward, against 4 to 16 bytes.  A row is held by
 // LANES lanes (16 for the narrowest, a wave, or a block of four waves), 8 consecutive elements (one 16-byte piece of
@@ -70,9 +74,34 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
   return v;
 }
 
+// Two sums at once; `slots` of at least 8 floats.
+template <int LANES>
+__device__ __forceinline__ void row_sums(float& u, float& v, float* slots) {
+#pragma unroll
+  for (int m = 1; m < (LANES < 64 ? LANES : 64); m <<= 1) {
+    u += __shfl_xor(u, m, 64);
+    v += __shfl_xor(v, m, 64);
+  }
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) *reinterpret_cast<float2*>(slots + 2 * (threadIdx.x >> 6)) = float2{u, v};
+    __syncthreads();
+    u = (slots[0] + slots[2]) + (slots[4] + slots[6]);
+    v = (slots[1] + slots[3]) + (slots[5] + slots[7]);
+  }
+}
+
+// What the differences to a first mean, their sum and that of their squares, say of a row of 1 / inv elements.
+struct RowStats {
+  float e, mean, rstd;
+};
+__device__ __forceinline__ RowStats row_stats(float first, float sum, float sq, float inv, float eps) {
+  const float e = sum * inv, var = sq * inv - e * e;
+  return {e, first + e, rsqrtf((var < 0.f ? 0.f : var) + eps)};  // (a NaN stays one)
+}
+
 template <bool XF32, int LANES, int CH>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
-  __shared__ float slots[8];
+  __shared__ __attribute__((aligned(8))) float slots[12];
   const int lane = threadIdx.x % LANES;
   const int64_t row = flat_lane_256() / LANES;
   const bool live = row < a.T;
@@ -99,16 +128,22 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
       for (int e = 0; e < 8; ++e) sum += x[c][e];
     }
   }
-  const float mean = row_sum<LANES>(sum, slots) / (float)C;  // (one rounding: rows of one value have no variance)
-  float sq = 0.f;
+  const float inv = 1.f / (float)C, first = row_sum<LANES>(sum, slots + 8) / (float)C;
+  float off = 0.f, sq = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int n = C - (c * LANES + lane) * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) sq = fmaf(x[c][e] - mean, x[c][e] - mean, sq);
+    for (int e = 0; e < 8; ++e) {
+      x[c][e] -= first;
+      if (e < n) {
+        off += x[c][e];
+        sq = fmaf(x[c][e], x[c][e], sq);
+      }
+    }
   }
-  const float rstd = rsqrtf(row_sum<LANES>(sq, slots + 4) / (float)C + a.eps);
+  row_sums<LANES>(off, sq, slots);
+  const RowStats st = row_stats(first, off, sq, inv, a.eps);
   if (!live) return;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -116,7 +151,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
     if (at < C) {
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = (x[c][e] - mean) * rstd;
+      for (int e = 0; e < 8; ++e) y[e] = (x[c][e] - st.e) * st.rstd;
       Raw8<true> p;
       if (a.w != nullptr) {
         p.load(a.w, at, C - at);
@@ -131,13 +166,13 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a) {
       store8(a.Y, row * a.ldy + at, C - at, y, a.y_bf16);
     }
   }
-  if (a.stats != nullptr && lane == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = float2{mean, rstd};
+  if (a.stats != nullptr && lane == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = float2{st.mean, st.rstd};
 }
 
 // Rows of any length: one block each, read once for every sum.
 template <bool XF32>
 __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(const NormArgs a) {
-  __shared__ float slots[8];
+  __shared__ __attribute__((aligned(8))) float slots[12];
   const int64_t row = flat_lane_256() / kNormThreads;
   if (row >= a.T) return;
   auto value = [&](int64_t at) {
@@ -146,19 +181,21 @@ __global__ void __launch_bounds__(kNormThreads) norm_long_kernel(const NormArgs 
   };
   float sum = 0.f;
   for (int64_t at = threadIdx.x; at < a.C; at += kNormThreads) sum += value(at);
-  const float mean = row_sum<kNormThreads>(sum, slots) / (float)a.C;
-  float sq = 0.f;
+  const float inv = 1.f / (float)a.C, first = row_sum<kNormThreads>(sum, slots + 8) / (float)a.C;
+  float off = 0.f, sq = 0.f;
   for (int64_t at = threadIdx.x; at < a.C; at += kNormThreads) {
-    const float d = value(at) - mean;
+    const float d = value(at) - first;
+    off += d;
     sq = fmaf(d, d, sq);
   }
-  const float rstd = rsqrtf(row_sum<kNormThreads>(sq, slots + 4) / (float)a.C + a.eps);
+  row_sums<kNormThreads>(off, sq, slots);
+  const RowStats st = row_stats(first, off, sq, inv, a.eps);
   for (int64_t at = threadIdx.x; at < a.C; at += kNormThreads) {
     const float s = value(at);
     if (a.R != nullptr && a.S != nullptr) store1(a.S, row * a.lds + at, s, !XF32);
-    store1(a.Y, row * a.ldy + at, fmaf((s - mean) * rstd, a.w ? a.w[at] : 1.f, a.b ? a.b[at] : 0.f), a.y_bf16);
+    store1(a.Y, row * a.ldy + at, fmaf((s - first - st.e) * st.rstd, a.w ? a.w[at] : 1.f, a.b ? a.b[at] : 0.f), a.y_bf16);
   }
-  if (a.stats != nullptr && threadIdx.x == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = float2{mean, rstd};
+  if (a.stats != nullptr && threadIdx.x == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = float2{st.mean, st.rstd};
 }
 
 // A block walks over rows, LANES lanes to each, and keeps its share of dw and db in registers; at the end the row groups of
