@@ -518,7 +518,7 @@ int32_t nm_pack_prepare_batched(const nm_layer_desc* descs, int32_t count, void*
  *   S       out  [T, C], ld lds, type of X: the sum, rounded once; NULL to skip; not used without R.  (Y is that of the sum
  *                before it was rounded.)  May be the same matrix as R or as X (a residual stream kept in place).
  *   stats   out  float [T, 2], 8-byte aligned: (mean, rstd) of each row, for the backward pass; NULL to skip
- * All arithmetic is in 32-bit floats, the variance from the differences to the mean.
+ * All arithmetic is in 32-bit floats, the variance from the differences to the mean, which is corrected by theirs.
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0, T above 2^31, C above 2^24, T * C above
  * 2^40, a leading dimension smaller than its row, eps < 0 or NaN),
  * NM_ERR_DTYPE, NM_ERR_ALIGN (element alignment), NM_ERR_DEVICE.
@@ -597,7 +597,8 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
  *               queries, 32-bit sums of runs of queries, which a further launch adds in order.  The size is that of a call with just
  *               these arguments: fewer keys can be cut further.  Contents undefined afterwards; concurrent calls need distinct
  *               workspaces.
- * Every sum is taken in a fixed order: results repeat bit for bit.
+ * Every sum is taken in a fixed order: results repeat bit for bit.  What a pair of a query and a key inside one sequence that does not
+ * see each other holds is multiplied by zero here too: keys, queries and dO have to be finite as well.
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (Tq <= 0, Tk < 0, either above 2^30; sequences outside [1, 65535], heads_q no multiple of heads_kv,
  * sequences * heads_q above 2^20, head_size outside [1, 128], max_q, max_k < 0, negative strides, tokens or heads of an output that
  * overlap, scale not positive and finite), NM_ERR_ALIGN, NM_ERR_WORKSPACE, NM_ERR_DEVICE.

@@ -12,11 +12,11 @@
 // group) pairs that share a key head, its waves walk over different keys, and keys are cut into chunks for different blocks;
 // what they leave (output, maximum, sum) a second launch joins in order.
 //
-// Measured: two causal prompts of 8191 and 342, 16 heads on 4 of 128: 273 us, 1000 TFLOP/s of useful products, bound by issue: a tile
+// Measured: two causal prompts of 8191 and 342, 16 heads on 4 of 128: 278 us, 990 TFLOP/s of useful products, bound by issue: a tile
 // of 64 keys is 32 matrix instructions and 150 others to a wave, two waves a SIMD.  256 images of 197 tokens, 12 heads of 64: 310 MB in
-// 90 us, where loads, stores and products, of four tiles to a block, are 55, 25 and 75 alone (no deeper staging, nor blocks that
-// take several tiles with the next one's loads under way, overlaps them better).  24 caches of 1 to 16384 keys, 32 heads on 8 of 128:
-// 337 MB in 71 us, 4.7 TB/s, and 5 for the join: bound by memory, and by how evenly chunks of unknown lengths go round.
+// 92 to 97 us by the card, where loads, stores and products, of four tiles to a block, are 55, 25 and 75 alone (no deeper staging, nor
+// blocks that take several tiles with the next one's loads under way, overlaps them better).  24 caches of 1 to 16384 keys, 32 heads on
+// 8 of 128: 337 MB in 71 us, 4.7 TB/s, and 5 for the join: bound by memory, and by how evenly chunks of unknown lengths go round.
 #include "nm_attention.h"
 
 namespace nm {

@@ -10,9 +10,10 @@
 // heads.  That recomputes the scores and dP once more, 7 products instead of 5, and needs no atomics.  Scores, probabilities and sums
 // are 32-bit floats; p and dS are rounded to bfloat16 as operands of the products that take them.
 //
-// Measured: packed causal texts of 4093, 848 and 1393 tokens, 16 heads on 4 of 128: 396 us, of which the queries' kernel has 145, the
-// keys' 250 and the joined sums 26 under a profiler; of 199 GFLOP that makes 500 TFLOP/s, 700 of the products there are.  Bound by
-// registers: two waves a SIMD, 256 registers each, are too few to keep the matrix cores fed through the exponentials.  64 images of 197 tokens, 12 heads of 64: 35 and 47 us, 155 MB.
+// Measured: packed causal texts of 4093, 848 and 1393 tokens, 16 heads on 4 of 128: 399 us, of which the queries' kernel has 142, the
+// keys' 232 and the joined sums 25; of 199 GFLOP that makes 500 TFLOP/s, 700 of the products there are.  Bound by registers: two
+// waves a SIMD, 256 registers each, are too few to keep the matrix cores fed through the exponentials, and the keys' kernel spills 38
+// of its own.  64 images of 197 tokens, 12 heads of 64: 34 and 45 us, 155 MB.
 #include "nm_attention.h"
 
 #include <algorithm>
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && !WHOLE ? 1 : 2) grad_ke
   __shared__ __attribute__((aligned(16))) float rows[2][2][kQueries];               // ... and of lse (base 2) and D
   // Heads of 128 elements: the keys' operands stay in LDS, each wave's its own, since 64 registers of keys and values beside 160 of
   // sums leave too few for two waves a SIMD (65 were spilled; the packed texts above took 638 us, 420 with the keys in LDS, as things
-  // were then).
+  // were then; 38 still are).
   constexpr bool KEEP = DP == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char kept[KEEP ? kRows * Tile::kRowBytes : 16];
   TilePlace at;

@@ -19,9 +19,10 @@
 // LANES lanes (16 for the narrowest, a wave, or a block of four waves), 8 consecutive elements (one 16-byte piece of
 // bfloat16) per lane and step, so that a wave's load covers whole 128-byte lines, at any width and alignment.  Rows above
 // 8192 elements are read again for each sum.
-// Measured: 200704 x 128, float in with the sum kept, 361 MB in 63 us, 5.7 TB/s, what a large copy reaches; backward 50432 x 768 of
-// bfloat16, 310 MB in 60 us and 5 for the sums of dw and db; 4099 x 5003 of float, rows 5008 apart, 246 MB in 68 and 8; one row 3 us, a
-// launch.
+// Measured: 200704 x 128, float in with the sum kept, 361 MB in 65 us, 5.6 TB/s, what a large copy reaches; backward 50432 x 768 of
+// bfloat16, 310 MB in 60 us and 5 for the sums of dw and db; 4099 x 5003 of float, rows 5008 apart, 246 MB in 67 and 8 (a row of a block
+// pays a barrier for each of its two sums); one row 3 us, a launch.  The second sum of the forward pass costs 8192 x 2048 of bfloat16 in
+// and out 16.0 us where 15.3 were without; elsewhere at most one part in a hundred.
 #include "nm_device.h"
 #include "nm_launch.h"
 #include "nm_rows.h"
@@ -432,10 +433,11 @@ void with_form(const RowForm& r, F&& f) {
   else f(Int<256>{}, Int<4>{});
 }
 
-// Blocks that walk the rows of the backward pass: as many as a compute unit's registers hold (rows of up to a wave's lanes: three,
-// of a block's: two), each with 2 C partial sums that are written and read once more; fewer where there are fewer rows.
-// 50432 x 768, bfloat16: 73 us with 256 blocks, 60 with 768, 70 with 1024; 4099 x 5003, float: 87, 77 and 74, and 5, 11 and 13
-// more for the sums.
+// Blocks that walk the rows of the backward pass, each with 2 C partial sums that are written and read once more; fewer where there
+// are fewer rows.  Rows of a wave: what a compute unit's registers hold of them in bfloat16, three; rows of a block: two.  The whole
+// call with 256, 512, 768 and 1024 blocks: 50432 x 768 of bfloat16 76, 65, 64 and 75 us; 4099 x 5003 of float 93, 75, 87 and 86.  By the
+// width alone, since the workspace's size knows no types: of rows of a wave with float on a side two fit, and 768 are too many
+// there (50432 x 768 of float 118, 121, 134 and 124; float rows with gradients in bfloat16 90, 90, 105 and 95).
 constexpr int64_t kWaveRowBlocks = 768, kBlockRowBlocks = 512;
 int64_t grad_blocks(int64_t T, const RowForm& r) {
   const int64_t per_block = r.lanes ? kNormThreads / r.lanes : 4, all = (T + per_block - 1) / per_block;
