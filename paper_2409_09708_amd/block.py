@@ -45,7 +45,7 @@ class Cache:
     @classmethod
     def empty(cls, count: int, room: int, heads: int, size: int, device="cuda") -> "Cache":
         import torch
-        K, V = (torch.empty((count * room, heads, size), dtype=torch.bfloat16, device=device) for _ in range(2))
+        K, V = (torch.zeros((count * room, heads, size), dtype=torch.bfloat16, device=device) for _ in range(2))
         offsets = torch.arange(count + 1, dtype=torch.int32, device=device) * room
         return cls(K, V, torch.zeros(count, dtype=torch.int32, device=device), offsets, room, 0)
 
