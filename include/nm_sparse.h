@@ -80,7 +80,7 @@ enum {
   NM_ERR_EXHAUSTED = 8  /* nm_sample_config ran out of random numbers before a configuration fell into the interval */
 };
 
-enum { NM_OUT_F32 = 0, NM_OUT_BF16 = 1, NM_OUT_I32 = 2 /* int8 calls only: the raw integer sums */ };
+enum { NM_OUT_F32 = 0, NM_OUT_BF16 = 1, NM_OUT_I32 = 2 /* int8 calls only: the raw integer sums */, NM_E4M3 = 3 /* pages of a cache only */ };
 
 /* Text for a status code (static storage, never NULL). */
 const char* nm_status_string(int32_t status);
@@ -626,6 +626,124 @@ int32_t nm_attention(const nm_attention_desc* desc, void* workspace, size_t work
 size_t nm_attention_backward_workspace_bytes(int64_t Tq, int64_t Tk, int32_t sequences, int32_t heads_q, int32_t heads_kv,
                                              int32_t head_size, int64_t max_q, int64_t max_k, int32_t causal);
 int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * nm_head_norm -- norm of queries and keys: each head of each token over its own D elements, and its rotary turn in the same pass
+ *   c = x - mean(x) where centred != 0 (layer norm), else x (root mean square),  rstd = 1 / sqrt(mean(c^2) + eps),  n = c rstd
+ *   y = turn(n w),  turn as nm_rotary has it with the angle positions[t, x] freqs[i] taken in 64 bits
+ *   X       in   [T, H, D], elements of a head contiguous, strides in elements between tokens and heads (the heads of q and k inside a
+ *                joint projection's output); float or bfloat16
+ *   weight  in   float [D] for all heads (heads = H), or [2, D]: the first `heads` heads (queries) take the first row, the others
+ *                (keys) the second.  NULL: 1
+ *   positions    in  [T, axes] contiguous, int32 or float (positions_f32), with freqs, sections (HOST), axes, rotated, interleaved as
+ *                nm_rotary takes them.  NULL: no turn, and those are not used
+ *   Y       out  [T, H, D]; may be X itself (same type and strides)
+ * nm_head_norm_backward -- with d = turn^-1(dy) and g = d w:
+ *   dx = rstd (g (- mean(g) where centred) - n mean(g n)),  dweight = sum over tokens and the heads of a row of d n
+ *   X, dY   in   what was normed, and the gradient of the output;  Y  out  dX; may be X or dY itself (same type and strides)
+ *   dweight out  float, in weight's shape; NULL to skip it.  Needs a weight
+ *   workspace    nm_head_norm_backward_workspace_bytes(T, H, heads, D, rotated) bytes (rotated 0: no turn), 256-byte aligned: sums of runs
+ *                of tokens, which are added in a fixed order, so that results repeat bit for bit; NULL allowed when that size is 0 or
+ *                dweight is NULL.  Contents undefined afterwards; concurrent calls need distinct workspaces.
+ * Statistics and sums are 32-bit floats; a value is rounded once, when it is stored.  Outputs must not overlap inputs otherwise.
+ * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0, T above 2^31, D above 512, H * D above 2^20, heads outside [1, H], eps < 0 or NaN, a
+ * turn that nm_rotary refuses, negative strides, tokens or heads of Y that overlap), NM_ERR_DTYPE, NM_ERR_ALIGN, NM_ERR_WORKSPACE,
+ * NM_ERR_DEVICE.
+ */
+typedef struct nm_typed_heads {
+  void* data;  /* inputs are only read */
+  int64_t token, head;
+  int32_t dtype, reserved;
+} nm_typed_heads;
+typedef struct nm_head_norm_desc {
+  nm_typed_heads X, Y;
+  nm_typed_heads dY;        /* nm_head_norm_backward only */
+  const float* weight;
+  float* dweight;           /* nm_head_norm_backward only */
+  const void* positions;
+  const float* freqs;
+  const int32_t* sections;  /* HOST */
+  int64_t T, H, heads, D, rotated;
+  int32_t axes, positions_f32, interleaved, centred;
+  float eps;
+  int32_t reserved;
+} nm_head_norm_desc;
+int32_t nm_head_norm(const nm_head_norm_desc* desc, void* stream);
+size_t nm_head_norm_backward_workspace_bytes(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t rotated);
+int32_t nm_head_norm_backward(const nm_head_norm_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A cache of keys and values in pages.  Token j of sequence b is slot j % page_size of page table[b, j / page_size]; a sequence's
+ * memory is handed out a page at a time, in any order, and pages may be shared between sequences as long as none of them is written.
+ *   K, V     [pages, page_size, heads, head_size], elements of a head contiguous, any strides in elements otherwise (both the same)
+ *   dtype    NM_OUT_BF16: as they are.  NM_E4M3: 8-bit codes (four bits of exponent, three of mantissa, 448 the largest) times a
+ *            power of two for each head of a token: the value is code * 2^(byte - 127), which bfloat16 holds exactly.
+ *   K_scales, V_scales  [pages, page_size, heads] bytes with strides of their own (both the same); NM_E4M3 only
+ *   table    int32 [sequences, table_width] contiguous.  An entry outside 0 .. pages - 1 is a page that is not there: it is not
+ *            written, read back as zeros, and its keys are not seen.
+ *   lengths  int32 [sequences]: tokens of each sequence, new ones counted.  (Above the table's room they are taken as the room.)
+ *
+ * nm_cache_write -- new tokens, packed one sequence after another, become the last ones of their sequences: token i of the n new ones
+ *   of sequence b is its token lengths[b] - n + i.  One that falls outside the table, or on a page that is not there, is dropped.
+ *   NM_E4M3: with e the smallest exponent that has max |x| <= 448 2^e over the finite elements of a row (between -100 and 119), each
+ *   element becomes the code nearest to x 2^-e (to an even one where two are as near); infinities and NaN become NaN.  A row read back is off
+ *   by at most 2^-4 of each element, or 2^-10 2^e of one below 2^-6 2^e.
+ *   K, V     in  [T, heads, head_size] bfloat16, any strides between tokens and heads
+ *   offsets  int32 [sequences + 1]: sequence b's new tokens are offsets[b] .. offsets[b + 1] - 1, from 0 to T, not decreasing.  A token
+ *            that no sequence holds is not kept.  NULL: T / sequences of each
+ * nm_cache_read -- tokens back from the cache: rows offsets[b] .. offsets[b + 1] - 1 of K and V become tokens first[b], first[b] + 1, ..
+ *   of sequence b (first NULL: 0).  Rows behind a sequence's last token, and rows that no sequence holds, are left as they were.
+ * No two new tokens of a call may go to the same slot.  Errors: NM_ERR_NULL, NM_ERR_SHAPE (T <= 0 or above 2^30; no offsets and T no multiple
+ * of sequences; pages, page_size, table_width, sequences, heads <= 0; page_size above 2^20, table_width * page_size above 2^30,
+ * sequences above 65535, sequences * heads above 2^20, head_size outside [1, 128]; negative strides; elements that are written and overlap),
+ * NM_ERR_DTYPE, NM_ERR_ALIGN, NM_ERR_DEVICE.
+ */
+typedef struct nm_pages {
+  void* K;
+  void* V;
+  uint8_t* K_scales;
+  uint8_t* V_scales;
+  int64_t page, token, head;
+  int64_t scale_page, scale_token, scale_head;
+  const int32_t* table;
+  const int32_t* lengths;
+  int64_t pages;
+  int32_t page_size, table_width, sequences, heads, head_size, dtype;
+} nm_pages;
+int32_t nm_cache_write(const nm_pages* pages, const nm_heads* K, const nm_heads* V, const int32_t* offsets, int64_t T, void* stream);
+int32_t nm_cache_read(const nm_pages* pages, const nm_heads* K, const nm_heads* V, const int32_t* offsets, const int32_t* first, int64_t T,
+                      void* stream);
+
+/*
+ * nm_attention_paged -- nm_attention of new tokens, one or a chunk of them per sequence, over a cache in pages, which holds their own
+ * keys and values already.  Query i of the Lq queries of sequence b stands at p = lengths[b] - Lq + i and sees the keys
+ *   j <= p  with  j > p - window (window 0: all of them)  or  j < sinks.
+ * A query that sees no key gets o = 0 and lse = -infinity.
+ *   Q, O       [Tq, heads_q, head_size] bfloat16, strides as for nm_attention; query head h reads key head h / (heads_q / heads)
+ *   offsets_q  int32 [sequences + 1], as for nm_attention.  NULL: Tq / sequences queries of each
+ *   max_q, max_k  the longest lengths, as far as the caller knows: the launch is shaped for them.  Longer ones are computed too
+ *   lse        out float [heads_q, Tq], or NULL
+ *   workspace  scratch of nm_attention_paged_workspace_bytes() bytes, 256-byte aligned; it does for any max_k, window and sinks.  NULL
+ *              allowed where keys are few (max_k up to 512, or that size is 0).  Contents undefined afterwards; concurrent calls need
+ *              distinct workspaces.
+ * Arithmetic as nm_attention's; 8-bit keys and values enter as the exact bfloat16 numbers that they stand for.  Keys that no query of its
+ * sequence sees -- behind the end, between sinks and window, on pages that are not there -- are not read, whatever they hold; what one query
+ * of a sequence sees and another does not is multiplied by zero for that one, so it has to be finite.
+ * Errors: those of nm_attention and of the pages, Tq * heads_q above 2^30, window or sinks negative (NM_ERR_SHAPE).
+ * Pages of heads of 32, 64 or 128 elements whose rows are 16-byte aligned are fastest; the heads of a page one after another (strides
+ * page > head > token) a little more so.
+ */
+typedef struct nm_paged_desc {
+  nm_pages pages;
+  nm_heads Q, O;
+  float* lse;
+  const int32_t* offsets_q;
+  int64_t Tq, max_q, max_k;
+  int32_t heads_q, window, sinks;
+  float scale;
+} nm_paged_desc;
+size_t nm_attention_paged_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size, int64_t max_q);
+int32_t nm_attention_paged(const nm_paged_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aids -- no part of the layer and of no passage of the paper: the two rates the kernels above are

@@ -21,7 +21,7 @@ _CALLS = None
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 
 NM_OK = 0
-NM_OUT_F32, NM_OUT_BF16, NM_OUT_I32 = 0, 1, 2
+NM_OUT_F32, NM_OUT_BF16, NM_OUT_I32, NM_E4M3 = 0, 1, 2, 3
 
 EXPORTS = (
     "nm_status_string", "nm_last_hip_error", "nm_values_bytes", "nm_index_bytes", "nm_mask_bytes",
@@ -39,6 +39,8 @@ EXPORTS = (
     "nm_prepared_batched_scratch_bytes", "nm_linear_forward_prepared_batched_scratch", "nm_prune_scored", "nm_i8_workspace_bytes", "nm_linear_forward_i8", "nm_i8_prepare", "nm_linear_forward_i8_prepared",
     "nm_layer_norm", "nm_layer_norm_backward_workspace_bytes", "nm_layer_norm_backward", "nm_rotary",
     "nm_attention_workspace_bytes", "nm_attention", "nm_attention_backward_workspace_bytes", "nm_attention_backward",
+    "nm_head_norm", "nm_head_norm_backward_workspace_bytes", "nm_head_norm_backward", "nm_cache_write", "nm_cache_read",
+    "nm_attention_paged_workspace_bytes", "nm_attention_paged",
 )
 
 
@@ -96,6 +98,33 @@ class AttentionDesc(ctypes.Structure):
         ("Tq", c_int64), ("Tk", c_int64), ("max_q", c_int64), ("max_k", c_int64),
         ("sequences", c_int32), ("heads_q", c_int32), ("heads_kv", c_int32), ("head_size", c_int32),
         ("causal", c_int32), ("scale", ctypes.c_float)]
+
+
+class TypedHeads(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("token", c_int64), ("head", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("X", TypedHeads), ("Y", TypedHeads), ("dY", TypedHeads), ("weight", c_void_p), ("dweight", c_void_p),
+                ("positions", c_void_p), ("freqs", c_void_p), ("sections", c_void_p),
+                ("T", c_int64), ("H", c_int64), ("heads", c_int64), ("D", c_int64), ("rotated", c_int64),
+                ("axes", c_int32), ("positions_f32", c_int32), ("interleaved", c_int32), ("centred", c_int32),
+                ("eps", ctypes.c_float), ("reserved", c_int32)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("K", c_void_p), ("V", c_void_p), ("K_scales", c_void_p), ("V_scales", c_void_p),
+                ("page", c_int64), ("token", c_int64), ("head", c_int64),
+                ("scale_page", c_int64), ("scale_token", c_int64), ("scale_head", c_int64),
+                ("table", c_void_p), ("lengths", c_void_p), ("pages", c_int64),
+                ("page_size", c_int32), ("table_width", c_int32), ("sequences", c_int32), ("heads", c_int32),
+                ("head_size", c_int32), ("dtype", c_int32)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [("pages", Pages), ("Q", Heads), ("O", Heads), ("lse", c_void_p), ("offsets_q", c_void_p),
+                ("Tq", c_int64), ("max_q", c_int64), ("max_k", c_int64),
+                ("heads_q", c_int32), ("window", c_int32), ("sinks", c_int32), ("scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -262,6 +291,21 @@ def load_library() -> ctypes.CDLL:
                                                           c_int32]
     lib.nm_attention_backward.restype = c_int32
     lib.nm_attention_backward.argtypes = lib.nm_attention.argtypes
+    lib.nm_head_norm.restype = c_int32
+    lib.nm_head_norm.argtypes = [ctypes.POINTER(HeadNormDesc), c_void_p]
+    lib.nm_head_norm_backward_workspace_bytes.restype = c_size_t
+    lib.nm_head_norm_backward_workspace_bytes.argtypes = [c_int64] * 5
+    lib.nm_head_norm_backward.restype = c_int32
+    lib.nm_head_norm_backward.argtypes = [ctypes.POINTER(HeadNormDesc), c_void_p, c_size_t, c_void_p]
+    lib.nm_cache_write.restype = c_int32
+    lib.nm_cache_write.argtypes = [ctypes.POINTER(Pages), ctypes.POINTER(Heads), ctypes.POINTER(Heads), c_void_p, c_int64, c_void_p]
+    lib.nm_cache_read.restype = c_int32
+    lib.nm_cache_read.argtypes = [ctypes.POINTER(Pages), ctypes.POINTER(Heads), ctypes.POINTER(Heads), c_void_p, c_void_p, c_int64,
+                                  c_void_p]
+    lib.nm_attention_paged_workspace_bytes.restype = c_size_t
+    lib.nm_attention_paged_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32, c_int32, c_int64]
+    lib.nm_attention_paged.restype = c_int32
+    lib.nm_attention_paged.argtypes = [ctypes.POINTER(PagedDesc), c_void_p, c_size_t, c_void_p]
     _LIB = lib
     return lib
 
@@ -1276,3 +1320,203 @@ def nm_attention_backward(dO, Q, K, V, O, lse, causal: bool = False, scale=None,
             desc.Tq, desc.Tk, desc.sequences, desc.heads_q, desc.heads_kv, desc.head_size, desc.max_q, desc.max_k, desc.causal), Q.device, stream)
     _check(lib.nm_attention_backward(ctypes.byref(desc), *_scratch(workspace), _stream_handle(stream)))
     return dQ, dK, dV
+
+
+def _turn(positions, freqs, sections, T: int):
+    """(pointers of positions and freqs, whether positions are float, sections, pairs) of a rotary turn, or of none."""
+    torch = _torch()
+    if positions is None:
+        if freqs is not None or sections is not None:
+            raise ValueError("freqs and sections need positions")
+        return None, None, False, (), 0
+    if freqs is None:
+        raise ValueError("positions need freqs")
+    _need(freqs, torch.float32, "freqs")
+    if len(freqs.shape) != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be contiguous [pairs]")
+    sections = (freqs.shape[0],) if sections is None else tuple(sections)
+    if positions.dtype != torch.int32:
+        _need(positions, torch.float32, "positions")
+    elif not positions.is_cuda:
+        raise ValueError("positions must be a device tensor")
+    if tuple(positions.shape) not in ((T, len(sections)),) + (((T,),) if len(sections) == 1 else ()) or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous [T, axes]")
+    return positions.data_ptr(), freqs.data_ptr(), positions.dtype == torch.float32, sections, freqs.shape[0]
+
+
+def _typed_heads(t, what: str, shape=None) -> TypedHeads:
+    code = _typed(t, what)
+    token, head = _head_strides(t, what, shape)
+    return TypedHeads(t.data_ptr(), token, head, code, 0)
+
+
+def _head_norm_desc(X, weight, heads, eps, centred, positions, freqs, sections, interleaved) -> HeadNormDesc:
+    d = HeadNormDesc()
+    d.X = _typed_heads(X, "X")
+    d.T, d.H, d.D = X.shape
+    d.heads = d.H if heads is None else heads
+    if weight is not None:
+        _need(weight, _torch().float32, "weight")
+        shapes = ((2, d.D),) if d.heads < d.H else ((d.D,), (1, d.D))
+        if tuple(weight.shape) not in shapes or not weight.is_contiguous():
+            raise ValueError(f"weight must be contiguous {list(shapes[0])}")
+        d.weight = weight.data_ptr()
+    d.positions, d.freqs, d.positions_f32, sections, pairs = _turn(positions, freqs, sections, d.T)
+    d.axes, d.rotated = len(sections), 2 * pairs
+    if sections:
+        d.kept = _ints(sections)  # (the descriptor holds a pointer only)
+        d.sections = ctypes.addressof(d.kept)
+    d.interleaved, d.centred, d.eps = int(interleaved), int(centred), eps
+    return d
+
+
+def nm_head_norm(X, weight=None, heads=None, eps: float = 1e-6, centred: bool = False, positions=None, freqs=None, sections=None,
+                 interleaved: bool = False, out_dtype=None, out=None, stream=None):
+    """Norm of queries and keys: each head of X [T, H, D] (float32 or bfloat16; any strides between tokens and heads) over its own
+    elements, by its root mean square or, centred, as a layer norm; times weight (float32 [D], or [2, D]: a row for the first `heads`
+    heads, the queries, and one for the others), and turned by the rotary positions where they are given (positions, freqs, sections and
+    interleaved as nm_rotary takes them).  Y has X's type unless out_dtype says otherwise; out=X norms in place."""
+    done = (_CALLS or _native()).head_norm(X, weight, heads, eps, centred, positions, freqs, sections, interleaved, out_dtype, out, stream)
+    if done is not NotImplemented:
+        return done
+    d = _head_norm_desc(X, weight, heads, eps, centred, positions, freqs, sections, interleaved)
+    if out is None:
+        out = X.new_empty(tuple(X.shape), dtype=X.dtype if out_dtype is None else out_dtype)
+    d.Y = _typed_heads(out, "out", X.shape)
+    _check(load_library().nm_head_norm(ctypes.byref(d), _stream_handle(stream)))
+    return out
+
+
+def nm_head_norm_backward(dY, X, weight=None, heads=None, eps: float = 1e-6, centred: bool = False, positions=None, freqs=None,
+                          sections=None, interleaved: bool = False, out_dtype=None, out=None, params: bool = True, workspace=None,
+                          stream=None):
+    """(dX, dweight) of nm_head_norm from the gradient dY of its output, what it normed and the same arguments otherwise.  dX has X's
+    type unless out_dtype says otherwise (out: the tensor to write, dY or X themselves too), dweight is float32 in weight's shape, None
+    without a weight or with params=False."""
+    done = (_CALLS or _native()).head_norm_backward(dY, X, weight, heads, eps, centred, positions, freqs, sections, interleaved, out_dtype,
+                                                    out, params, workspace, stream)
+    if done is not NotImplemented:
+        return done
+    d = _head_norm_desc(X, weight, heads, eps, centred, positions, freqs, sections, interleaved)
+    d.dY = _typed_heads(dY, "dY", X.shape)
+    if out is None:
+        out = X.new_empty(tuple(X.shape), dtype=X.dtype if out_dtype is None else out_dtype)
+    d.Y = _typed_heads(out, "out", X.shape)
+    lib = load_library()
+    dweight = None
+    if params and weight is not None:
+        dweight = weight.new_empty(tuple(weight.shape))
+        d.dweight = dweight.data_ptr()
+        if workspace is None:
+            need = lib.nm_head_norm_backward_workspace_bytes(d.T, d.H, d.heads, d.D, d.rotated)
+            if need:
+                workspace = _own_scratch(need, stream)
+    _check(lib.nm_head_norm_backward(ctypes.byref(d), *_scratch(workspace), _stream_handle(stream)))
+    return out, dweight
+
+
+def _pages(K_pages, V_pages, page_table, lengths, K_scales, V_scales) -> Pages:
+    torch = _torch()
+    codes = K_pages.dtype == torch.float8_e4m3fn
+    p = Pages()
+    for what, t in (("K_pages", K_pages), ("V_pages", V_pages)):
+        _need(t, torch.float8_e4m3fn if codes else torch.bfloat16, what)
+    if len(K_pages.shape) != 4 or V_pages.shape != K_pages.shape or V_pages.stride() != K_pages.stride():
+        raise ValueError("K_pages and V_pages must be [pages, page size, heads, elements], of one shape and with the same strides")
+    p.pages, p.page_size, p.heads, p.head_size = K_pages.shape
+    p.page, p.token, p.head, step = K_pages.stride()
+    if step != 1 and p.head_size > 1:
+        raise ValueError("pages must have contiguous heads")
+    p.K, p.V, p.dtype = K_pages.data_ptr(), V_pages.data_ptr(), NM_E4M3 if codes else NM_OUT_BF16
+    if codes:
+        if K_scales is None or V_scales is None:
+            raise ValueError("pages in 8 bits need K_scales and V_scales")
+        for what, t in (("K_scales", K_scales), ("V_scales", V_scales)):
+            _need(t, torch.uint8, what)
+        if K_scales.shape != K_pages.shape[:3] or V_scales.shape != K_scales.shape or V_scales.stride() != K_scales.stride():
+            raise ValueError("K_scales and V_scales must be [pages, page size, heads], with the same strides")
+        p.scale_page, p.scale_token, p.scale_head = K_scales.stride()
+        p.K_scales, p.V_scales = K_scales.data_ptr(), V_scales.data_ptr()
+    elif K_scales is not None or V_scales is not None:
+        raise ValueError("pages of bfloat16 have no scales")
+    _need(page_table, torch.int32, "page_table")
+    if len(page_table.shape) != 2 or not page_table.is_contiguous():
+        raise ValueError("page_table must be contiguous [sequences, pages of a sequence]")
+    p.sequences, p.table_width = page_table.shape
+    p.table, p.lengths = page_table.data_ptr(), _per_sequence(lengths, p.sequences, "lengths")
+    return p
+
+
+def nm_cache_write(K, V, K_pages, V_pages, page_table, lengths, offsets=None, K_scales=None, V_scales=None, stream=None) -> None:
+    """New keys and values (bfloat16 [T, heads, D], any strides between tokens and heads; sequence b's are rows offsets[b] ..
+    offsets[b + 1] - 1, without offsets each sequence has as many) become the last tokens of their sequences in the cache: token j of
+    sequence b is slot j % page size of page page_table[b, j // page size], and lengths (int32 [sequences]) count the new ones.
+    Pages are [pages, page size, heads, D], any strides between the first three: bfloat16, or float8_e4m3fn with K_scales and V_scales
+    (uint8 [pages, page size, heads]; the value is code * 2 ** (byte - 127)).  What falls outside the table or on a page that is not
+    there (an entry below 0, say) is dropped."""
+    done = (_CALLS or _native()).cache_write(K, V, K_pages, V_pages, page_table, lengths, offsets, K_scales, V_scales, stream)
+    if done is not NotImplemented:
+        return done
+    p = _pages(K_pages, V_pages, page_table, lengths, K_scales, V_scales)
+    shape = (K.shape[0], p.heads, p.head_size)
+    k, v = _heads(K, "K", shape), _heads(V, "V", shape)
+    _check(load_library().nm_cache_write(ctypes.byref(p), ctypes.byref(k), ctypes.byref(v), _per_sequence(offsets, p.sequences + 1, "offsets"),
+                                         shape[0], _stream_handle(stream)))
+
+
+def nm_cache_read(K_pages, V_pages, page_table, lengths, offsets=None, tokens=None, first=None, K_scales=None, V_scales=None, out=None,
+                  stream=None):
+    """(K, V), bfloat16 [tokens, heads, D], from a cache as nm_cache_write has it: rows offsets[b] .. offsets[b + 1] - 1 are tokens
+    first[b] .. (from 0 on without `first`) of sequence b, up to its last; other rows are left as they were (out: the two tensors to
+    write, any strides between tokens and heads).  Pages that are not there give zeros."""
+    done = (_CALLS or _native()).cache_read(K_pages, V_pages, page_table, lengths, offsets, tokens, first, K_scales, V_scales, out, stream)
+    if done is not NotImplemented:
+        return done
+    p = _pages(K_pages, V_pages, page_table, lengths, K_scales, V_scales)
+    if out is None:
+        if tokens is None:
+            raise ValueError("tokens (the rows of the outputs) or out must be given")
+        out = tuple(K_pages.new_empty((tokens, p.heads, p.head_size), dtype=_torch().bfloat16) for _ in range(2))
+    K, V = out
+    shape = (K.shape[0] if tokens is None else tokens, p.heads, p.head_size)
+    k, v = _heads(K, "K", shape), _heads(V, "V", shape)
+    _check(load_library().nm_cache_read(ctypes.byref(p), ctypes.byref(k), ctypes.byref(v), _per_sequence(offsets, p.sequences + 1, "offsets"),
+                                        _per_sequence(first, p.sequences, "first"), shape[0], _stream_handle(stream)))
+    return K, V
+
+
+def nm_attention_paged(Q, K_pages, V_pages, page_table, lengths, scale=None, offsets_q=None, window: int = 0, sinks: int = 0, K_scales=None,
+                       V_scales=None, max_q=None, max_k=None, lse: bool = False, out=None, workspace=None, stream=None):
+    """Softmax attention of new tokens, one or a chunk of them per sequence, over a cache as nm_cache_write has it, which holds their
+    own keys and values already: O (bfloat16, Q's shape [Tq, heads, D]), or (O, lse) with lse=True, lse float32 [heads, Tq].  A token sees
+    the keys up to its own: all of them, or with a window the last `window` of them and the first `sinks` of the sequence.  offsets_q
+    (int32 [sequences + 1]) says where each sequence's queries begin; without it each has as many.  max_q and max_k are the longest
+    lengths as far as known: the launch is shaped for them."""
+    done = (_CALLS or _native()).attention_paged(Q, K_pages, V_pages, page_table, lengths, scale, offsets_q, window, sinks, K_scales,
+                                                 V_scales, max_q, max_k, lse, out, workspace, stream)
+    if done is not NotImplemented:
+        return done
+    d = PagedDesc()
+    d.Q = _heads(Q, "Q")
+    d.pages = p = _pages(K_pages, V_pages, page_table, lengths, K_scales, V_scales)
+    d.Tq, d.heads_q, D = Q.shape
+    if D != p.head_size:
+        raise ValueError("Q and the pages must have heads of one size")
+    d.offsets_q = _per_sequence(offsets_q, p.sequences + 1, "offsets_q")
+    d.max_q = max_q if max_q is not None else -(-d.Tq // max(p.sequences, 1))
+    d.max_k = max_k if max_k is not None else p.table_width * p.page_size
+    d.window, d.sinks, d.scale = window, sinks, D ** -0.5 if scale is None else scale
+    if out is None:
+        out = Q.new_empty(Q.shape)
+    d.O = _heads(out, "out", Q.shape)
+    sums = None
+    if lse:
+        sums = Q.new_empty((d.heads_q, d.Tq), dtype=_torch().float32)
+        d.lse = sums.data_ptr()
+    lib = load_library()
+    if workspace is None:
+        need = lib.nm_attention_paged_workspace_bytes(d.Tq, p.sequences, d.heads_q, p.heads, p.head_size, d.max_q)
+        if need:
+            workspace = _own_scratch(need, stream)
+    _check(lib.nm_attention_paged(ctypes.byref(d), *_scratch(workspace), _stream_handle(stream)))
+    return (out, sums) if lse else out

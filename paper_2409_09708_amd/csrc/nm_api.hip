@@ -551,6 +551,17 @@ inline bool strides_ok(int64_t T, int64_t H, int64_t D, int64_t token, int64_t h
   // the heads of a token side by side (or those of all tokens, head after head)
   return (head >= D && token >= (H - 1) * head + D) || (token >= D && head >= (T - 1) * token + D);
 }
+// The rotary turn of a call: the pairs of each axis.
+int32_t rotary_check(const int32_t* sections, int32_t axes, int64_t rotated, int64_t D, int (&section_end)[nm::kMaxRotaryAxes]) {
+  if (rotated <= 0 || rotated > D || rotated % 2 || axes < 1 || axes > nm::kMaxRotaryAxes) return NM_ERR_SHAPE;
+  int64_t end = 0;
+  for (int x = 0; x < nm::kMaxRotaryAxes; ++x) {
+    if (x < axes && (sections[x] < 0 || sections[x] > rotated / 2)) return NM_ERR_SHAPE;
+    end += x < axes ? sections[x] : 0;
+    section_end[x] = x < axes - 1 ? (int)end : (int)(rotated / 2);
+  }
+  return end == rotated / 2 ? NM_OK : NM_ERR_SHAPE;
+}
 }  // namespace
 
 int32_t nm_layer_norm(const void* X, int64_t ldx, int32_t x_dtype, const void* R, int64_t ldr, int64_t T, int64_t C,
@@ -602,16 +613,9 @@ int32_t nm_rotary(const void* X, int32_t x_dtype, int64_t T, int64_t H, int64_t 
                   int64_t y_head, void* stream) {
   if (!X || !Y || !positions || !freqs || !sections) return NM_ERR_NULL;
   if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 1 << 20 || H * D > 1 << 20) return NM_ERR_SHAPE;
-  if (rotated <= 0 || rotated > D || rotated % 2 || axes < 1 || axes > nm::kMaxRotaryAxes) return NM_ERR_SHAPE;
-  if (!strides_ok(T, H, D, x_token, x_head, false) || !strides_ok(T, H, D, y_token, y_head, true)) return NM_ERR_SHAPE;
   nm::RotaryCall c;
-  int64_t end = 0;
-  for (int x = 0; x < nm::kMaxRotaryAxes; ++x) {
-    if (x < axes && (sections[x] < 0 || sections[x] > rotated / 2)) return NM_ERR_SHAPE;
-    end += x < axes ? sections[x] : 0;
-    c.section_end[x] = x < axes - 1 ? (int)end : (int)(rotated / 2);
-  }
-  if (end != rotated / 2) return NM_ERR_SHAPE;
+  if (int32_t st = rotary_check(sections, axes, rotated, D, c.section_end)) return st;
+  if (!strides_ok(T, H, D, x_token, x_head, false) || !strides_ok(T, H, D, y_token, y_head, true)) return NM_ERR_SHAPE;
   if (!type_ok(x_dtype) || !type_ok(y_dtype)) return NM_ERR_DTYPE;
   if (!type_aligned(X, x_dtype) || !type_aligned(Y, y_dtype) || !aligned(positions, 4) || !aligned(freqs, 4)) return NM_ERR_ALIGN;
   c.X = X; c.Y = Y; c.positions = positions; c.freqs = freqs;
@@ -697,6 +701,183 @@ int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, si
     return NM_ERR_WORKSPACE;
   c.workspace = workspace;
   return device_status(nm::launch_attention_grad(c, (hipStream_t)stream));
+}
+
+namespace {
+int32_t head_norm_check(const nm_head_norm_desc* d, bool backward, nm::HeadNormCall* c) {
+  if (!d || !d->X.data || !d->Y.data || (backward && !d->dY.data)) return NM_ERR_NULL;
+  const bool turned = d->positions != nullptr;
+  if (turned && (!d->freqs || !d->sections)) return NM_ERR_NULL;
+  if (backward && d->dweight && !d->weight) return NM_ERR_NULL;
+  const int64_t T = d->T, H = d->H, D = d->D;
+  if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 512 || H * D > 1 << 20) return NM_ERR_SHAPE;
+  if (d->heads < 1 || d->heads > H || !(d->eps >= 0.f)) return NM_ERR_SHAPE;
+  *c = nm::HeadNormCall{};
+  if (turned)
+    if (int32_t st = rotary_check(d->sections, d->axes, d->rotated, D, c->section_end)) return st;
+  if (!strides_ok(T, H, D, d->X.token, d->X.head, false) || !strides_ok(T, H, D, d->Y.token, d->Y.head, true) ||
+      (backward && !strides_ok(T, H, D, d->dY.token, d->dY.head, false)))
+    return NM_ERR_SHAPE;
+  if (!type_ok(d->X.dtype) || !type_ok(d->Y.dtype) || (backward && !type_ok(d->dY.dtype))) return NM_ERR_DTYPE;
+  if (!type_aligned(d->X.data, d->X.dtype) || !type_aligned(d->Y.data, d->Y.dtype) || (backward && !type_aligned(d->dY.data, d->dY.dtype)))
+    return NM_ERR_ALIGN;
+  for (const void* p : {(const void*)d->weight, (const void*)d->dweight, d->positions, (const void*)d->freqs})
+    if (!aligned(p, 4)) return NM_ERR_ALIGN;
+  c->X = d->X.data; c->Y = d->Y.data; c->w = d->weight;
+  c->T = T; c->H = H; c->D = D; c->heads = d->heads;
+  c->x_token = d->X.token; c->x_head = d->X.head; c->y_token = d->Y.token; c->y_head = d->Y.head;
+  c->eps = d->eps; c->centred = d->centred != 0;
+  c->x_f32 = d->X.dtype == NM_OUT_F32; c->y_f32 = d->Y.dtype == NM_OUT_F32;
+  if (turned) {
+    c->R = d->rotated; c->axes = d->axes; c->positions = d->positions; c->freqs = d->freqs;
+    c->positions_f32 = d->positions_f32 != 0; c->interleaved = d->interleaved != 0;
+  }
+  if (backward) {
+    c->dY = d->dY.data; c->dy_token = d->dY.token; c->dy_head = d->dY.head; c->dy_f32 = d->dY.dtype == NM_OUT_F32;
+    c->dw = d->dweight;
+  }
+  return NM_OK;
+}
+}  // namespace
+
+int32_t nm_head_norm(const nm_head_norm_desc* desc, void* stream) {
+  nm::HeadNormCall c;
+  if (int32_t st = head_norm_check(desc, false, &c)) return st;
+  return device_status(nm::launch_head_norm(c, (hipStream_t)stream));
+}
+
+size_t nm_head_norm_backward_workspace_bytes(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t rotated) {
+  if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 512 || H * D > 1 << 20 || heads < 1 || heads > H) return 0;
+  if (rotated < 0 || rotated > D || rotated % 2) return 0;
+  return nm::head_norm_grad_workspace_bytes(T, H, D, rotated, heads < H ? 2 : 1);
+}
+
+int32_t nm_head_norm_backward(const nm_head_norm_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
+  nm::HeadNormCall c;
+  if (int32_t st = head_norm_check(desc, true, &c)) return st;
+  if (c.dw && !workspace_ok(workspace, workspace_bytes, nm::head_norm_grad_workspace_bytes(c.T, c.H, c.D, c.R, c.heads < c.H ? 2 : 1)))
+    return NM_ERR_WORKSPACE;
+  c.workspace = workspace;
+  return device_status(nm::launch_head_norm_grad(c, (hipStream_t)stream));
+}
+
+namespace {
+constexpr int64_t kMostPageTokens = (int64_t)1 << 30;
+// whether elements of three nested strides, `extent` of them in a row, are all different places
+bool apart(int64_t extent, int64_t s0, int64_t n0, int64_t s1, int64_t n1, int64_t s2, int64_t n2) {
+  int64_t s[3] = {s0, s1, s2}, n[3] = {n0, n1, n2};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2 - i; ++j)
+      if (s[j] > s[j + 1]) {
+        const int64_t t = s[j], m = n[j];
+        s[j] = s[j + 1]; n[j] = n[j + 1];
+        s[j + 1] = t; n[j + 1] = m;
+      }
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] == 1) continue;
+    if (s[i] < extent) return false;
+    extent += s[i] * (n[i] - 1);
+  }
+  return true;
+}
+
+int32_t pages_check(const nm_pages* d, bool written, nm::PagesCall* c) {
+  if (!d || !d->K || !d->V || !d->table || !d->lengths) return NM_ERR_NULL;
+  if (d->dtype != NM_OUT_BF16 && d->dtype != NM_E4M3) return NM_ERR_DTYPE;
+  const bool codes = d->dtype == NM_E4M3;
+  if (codes && (!d->K_scales || !d->V_scales)) return NM_ERR_NULL;
+  if (d->pages < 1 || d->pages > 0x7FFFFFFF || d->page_size < 1 || d->page_size > 1 << 20 || d->table_width < 1 ||
+      (int64_t)d->table_width * d->page_size > kMostPageTokens)
+    return NM_ERR_SHAPE;
+  if (d->sequences < 1 || d->sequences > 65535 || d->heads < 1 || (int64_t)d->sequences * d->heads > 1 << 20 || d->head_size < 1 ||
+      d->head_size > 128)
+    return NM_ERR_SHAPE;
+  const int64_t most = (int64_t)1 << 40;
+  for (int64_t s : {d->page, d->token, d->head, d->scale_page, d->scale_token, d->scale_head})
+    if (s < 0 || s > most) return NM_ERR_SHAPE;
+  if (written && (!apart(d->head_size, d->page, d->pages, d->token, d->page_size, d->head, d->heads) ||
+                  (codes && !apart(1, d->scale_page, d->pages, d->scale_token, d->page_size, d->scale_head, d->heads))))
+    return NM_ERR_SHAPE;
+  if (!aligned(d->K, codes ? 1 : 2) || !aligned(d->V, codes ? 1 : 2) || !aligned(d->table, 4) || !aligned(d->lengths, 4)) return NM_ERR_ALIGN;
+  c->K = d->K; c->V = d->V; c->K_scales = d->K_scales; c->V_scales = d->V_scales;
+  c->page = d->page; c->token = d->token; c->head = d->head;
+  c->scale_page = d->scale_page; c->scale_token = d->scale_token; c->scale_head = d->scale_head;
+  c->table = d->table; c->lengths = d->lengths; c->pages = d->pages;
+  c->page_size = d->page_size; c->width = d->table_width; c->B = d->sequences; c->H = d->heads; c->D = d->head_size;
+  c->e4m3 = codes;
+  return NM_OK;
+}
+
+// packed tokens beside a cache: K and V, their offsets
+int32_t packed_check(const nm_pages& d, const nm_heads* K, const nm_heads* V, const int32_t* offsets, int64_t T, bool output, nm::HeadRows* k,
+                     nm::HeadRows* v) {
+  if (!K || !V || !K->data || !V->data) return NM_ERR_NULL;
+  if (T <= 0 || T > kMostTokens || (!offsets && T % d.sequences)) return NM_ERR_SHAPE;
+  if (!strides_ok(T, d.heads, d.head_size, K->token, K->head, output) || !strides_ok(T, d.heads, d.head_size, V->token, V->head, output))
+    return NM_ERR_SHAPE;
+  if (!aligned(K->data, 2) || !aligned(V->data, 2) || !aligned(offsets, 4)) return NM_ERR_ALIGN;
+  *k = nm::HeadRows{K->data, K->token, K->head};
+  *v = nm::HeadRows{V->data, V->token, V->head};
+  return NM_OK;
+}
+}  // namespace
+
+int32_t nm_cache_write(const nm_pages* pages, const nm_heads* K, const nm_heads* V, const int32_t* offsets, int64_t T, void* stream) {
+  nm::CacheWriteCall c = {};
+  if (int32_t st = pages_check(pages, true, &c.p)) return st;
+  if (int32_t st = packed_check(*pages, K, V, offsets, T, false, &c.K, &c.V)) return st;
+  c.offsets = offsets;
+  c.T = T;
+  return device_status(nm::launch_cache_write(c, (hipStream_t)stream));
+}
+
+int32_t nm_cache_read(const nm_pages* pages, const nm_heads* K, const nm_heads* V, const int32_t* offsets, const int32_t* first, int64_t T,
+                      void* stream) {
+  nm::CacheReadCall c = {};
+  if (int32_t st = pages_check(pages, false, &c.p)) return st;
+  if (int32_t st = packed_check(*pages, K, V, offsets, T, true, &c.K, &c.V)) return st;
+  if (!aligned(first, 4)) return NM_ERR_ALIGN;
+  c.offsets = offsets;
+  c.first = first;
+  c.T = T;
+  return device_status(nm::launch_cache_read(c, (hipStream_t)stream));
+}
+
+namespace {
+bool paged_sizes_ok(int64_t Tq, int64_t sequences, int64_t heads_q, int64_t heads_kv, int64_t head_size, int64_t max_q) {
+  return attention_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q, 0) && Tq * heads_q <= kMostTokens;
+}
+}  // namespace
+
+size_t nm_attention_paged_workspace_bytes(int64_t Tq, int32_t sequences, int32_t heads_q, int32_t heads_kv, int32_t head_size, int64_t max_q) {
+  if (!paged_sizes_ok(Tq, sequences, heads_q, heads_kv, head_size, max_q)) return 0;
+  return nm::paged_workspace_most(Tq, sequences, heads_q, heads_kv, head_size, max_q < Tq ? max_q : Tq);
+}
+
+int32_t nm_attention_paged(const nm_paged_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!d || !d->Q.data || !d->O.data) return NM_ERR_NULL;
+  nm::PagedCall c = {};
+  if (int32_t st = pages_check(&d->pages, false, &c.p)) return st;
+  const nm_pages& p = d->pages;
+  if (!paged_sizes_ok(d->Tq, p.sequences, d->heads_q, p.heads, p.head_size, d->max_q) || d->max_k < 0) return NM_ERR_SHAPE;
+  if (!d->offsets_q && d->Tq % p.sequences) return NM_ERR_SHAPE;
+  if (d->window < 0 || d->sinks < 0 || !(d->scale > 0.f) || d->scale > 3.0e38f) return NM_ERR_SHAPE;
+  if (!strides_ok(d->Tq, d->heads_q, p.head_size, d->Q.token, d->Q.head, false) ||
+      !strides_ok(d->Tq, d->heads_q, p.head_size, d->O.token, d->O.head, true))
+    return NM_ERR_SHAPE;
+  if (!aligned(d->Q.data, 2) || !aligned(d->O.data, 2) || !aligned(d->lse, 4) || !aligned(d->offsets_q, 4)) return NM_ERR_ALIGN;
+  c.Q = nm::HeadRows{d->Q.data, d->Q.token, d->Q.head};
+  c.O = nm::HeadRows{d->O.data, d->O.token, d->O.head};
+  c.lse = d->lse; c.offsets_q = d->offsets_q;
+  c.Tq = d->Tq; c.Hq = d->heads_q;
+  const int64_t room = (int64_t)p.table_width * p.page_size;
+  c.max_q = d->max_q < d->Tq ? d->max_q : d->Tq;
+  c.max_k = d->max_k < room ? d->max_k : room;
+  c.window = d->window; c.sinks = d->sinks; c.scale = d->scale;
+  if (!workspace_ok(workspace, workspace_bytes, nm::paged_workspace_bytes(c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks)))
+    return NM_ERR_WORKSPACE;
+  c.workspace = workspace;
+  return device_status(nm::launch_paged(c, (hipStream_t)stream));
 }
 
 size_t nm_probe_sink_bytes(void) { return nm::probe_sink_bytes(); }

@@ -34,45 +34,6 @@ struct AttnArgs {
   float2* part_ml;    // [column][chunk]: (maximum of the scaled scores in the exponent's base 2, sum)
 };
 
-// A column's running maximum and sum.  The reference that exponentials are taken against only follows the maximum when that
-// has grown by more than kSlack powers of two: sums and products of values up to 2^kSlack are as exact, and the
-// accumulators are rescaled a few times per row instead of once per tile.
-constexpr float kSlack = 8.f;
-
-// One tile of scores (KB accumulators of 32 keys) into the running softmax of a column: on return s holds the probabilities
-// against `ref` (scaled, base 2; -infinity: nothing seen yet), `sum` is this lane's share.
-template <int KB, int NB>
-__device__ __forceinline__ void softmax_step(f32x16_t (&s)[KB], float c, float& ref, float& sum, f32x16_t (&acc)[NB]) {
-  float top = s[0][0];
-#pragma unroll
-  for (int k = 0; k < KB; ++k)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[k][r]);
-  top = half_max(top) * c;
-  if (__any(top > ref + kSlack)) {  // (also where nothing has been seen yet: ref is -infinity)
-    const float next = fmaxf(top, ref);
-    const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - next);
-    ref = next;
-    sum *= by;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] *= by;
-  }
-  const float base = ref == kMinusInf ? 0.f : ref;
-#pragma unroll
-  for (int k = 0; k < KB; ++k)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[k][r] = fast_exp2(fmaf(s[k][r], c, -base));
-      sum += s[k][r];
-    }
-}
-
-// What a part's sums, taken against `ref`, count for against the maximum of all parts.  (-infinity: none of its scores was above
-// that; its sums are zeros, or NaN where a score was, which stays.)
-__device__ __forceinline__ float part_weight(float ref, float top) { return ref == kMinusInf ? 1.f : fast_exp2(ref - top); }
-
 constexpr int kKeys = 64;             // per tile
 constexpr int kQueries = kWaves * 32; // per block
 

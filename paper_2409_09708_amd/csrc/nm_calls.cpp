@@ -70,6 +70,13 @@ struct Library {
   decltype(&nm_attention_workspace_bytes) attention_bytes;
   decltype(&nm_attention_backward) attention_backward;
   decltype(&nm_attention_backward_workspace_bytes) attention_backward_bytes;
+  decltype(&nm_head_norm) head_norm;
+  decltype(&nm_head_norm_backward) head_norm_backward;
+  decltype(&nm_head_norm_backward_workspace_bytes) head_norm_backward_bytes;
+  decltype(&nm_cache_write) cache_write;
+  decltype(&nm_cache_read) cache_read;
+  decltype(&nm_attention_paged) attention_paged;
+  decltype(&nm_attention_paged_workspace_bytes) attention_paged_bytes;
 } lib;
 PyObject* raise_status;    // raises NmError for a status that is not NM_OK
 PyObject* find_workspace;  // the scratch tensor of a device and stream
@@ -873,6 +880,312 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// A head norm's X, weight, heads, eps, centred, positions, freqs, sections, interleaved from a on; `sections` holds what d points to.
+bool read_head_norm(PyObject* const* a, nm_head_norm_desc* d, int32_t (&sections)[4], const at::Tensor** X, const at::Tensor** weight) {
+  bool centred, interleaved, whole_numbers = false;
+  *weight = nullptr;
+  if (!floating(a[0], X, &d->X.dtype) || !heads_of(**X) || !PyFloat_CheckExact(a[3]) || !flag(a[4], &centred) || !flag(a[8], &interleaved)) return false;
+  d->T = (*X)->size(0);
+  d->H = d->heads = (*X)->size(1);
+  d->D = (*X)->size(2);
+  d->X.data = pointer<void>(*X);
+  d->X.token = (*X)->stride(0);
+  d->X.head = (*X)->stride(1);
+  if (a[2] != Py_None && !integer(a[2], 1, d->H, &d->heads)) return false;
+  if (a[1] != Py_None) {
+    if (!plain(a[1], at::kFloat, weight) || !(*weight)->is_contiguous()) return false;
+    if (d->heads < d->H ? (*weight)->dim() != 2 || (*weight)->size(0) != 2 || (*weight)->size(1) != d->D
+                        : (*weight)->dim() != 1 || (*weight)->size(0) != d->D)
+      return false;
+    d->weight = pointer<float>(*weight);
+  }
+  d->eps = (float)PyFloat_AS_DOUBLE(a[3]);
+  d->centred = centred;
+  d->interleaved = interleaved;
+  if (a[5] == Py_None) return a[6] == Py_None && a[7] == Py_None;
+  const at::Tensor *positions, *freqs;
+  if (!((whole_numbers = plain(a[5], at::kInt, &positions)) || plain(a[5], at::kFloat, &positions)) || !positions->is_contiguous() ||
+      !plain(a[6], at::kFloat, &freqs) || freqs->dim() != 1 || !freqs->is_contiguous() || freqs->size(0) > 1 << 20)
+    return false;
+  d->axes = 1;
+  sections[0] = (int32_t)freqs->size(0);
+  if (a[7] != Py_None) {
+    if (!PyTuple_CheckExact(a[7]) || PyTuple_GET_SIZE(a[7]) < 1 || PyTuple_GET_SIZE(a[7]) > 4) return false;
+    d->axes = (int32_t)PyTuple_GET_SIZE(a[7]);
+    for (int32_t i = 0; i < d->axes; ++i) {
+      int64_t v;
+      if (!integer(PyTuple_GET_ITEM(a[7], i), 0, 1 << 30, &v)) return false;
+      sections[i] = (int32_t)v;
+    }
+  }
+  if (positions->dim() == 2 ? positions->size(0) != d->T || positions->size(1) != d->axes
+                            : positions->dim() != 1 || d->axes != 1 || positions->size(0) != d->T)
+    return false;
+  d->positions = pointer<void>(positions);
+  d->positions_f32 = !whole_numbers;
+  d->freqs = pointer<float>(freqs);
+  d->rotated = 2 * freqs->size(0);
+  d->sections = sections;
+  return true;
+}
+// The output of a head norm, or of its backward pass: `out`, or one to be made in X's type or `dtype`.
+bool head_norm_output(PyObject* dtype, PyObject* out, const at::Tensor& X, nm_typed_heads* y, at::ScalarType* type) {
+  const at::Tensor* t = nullptr;
+  *type = X.scalar_type();
+  if (out != Py_None) {
+    if (!floating(out, &t, &y->dtype) || !heads_of(*t) || t->sizes() != X.sizes()) return false;
+    y->data = pointer<void>(t);
+    y->token = t->stride(0);
+    y->head = t->stride(1);
+    return true;
+  }
+  if (dtype != Py_None) {
+    if (!THPDtype_Check(dtype)) return false;
+    *type = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+  }
+  if (*type != at::kFloat && *type != at::kBFloat16) return false;
+  y->dtype = *type == at::kFloat ? NM_OUT_F32 : NM_OUT_BF16;
+  y->token = X.size(1) * X.size(2);
+  y->head = X.size(2);
+  return true;
+}
+
+// head_norm(X, weight, heads, eps, centred, positions, freqs, sections, interleaved, out_dtype, out, stream)
+PyObject* head_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_head_norm_desc d = {};
+  int32_t sections[4];
+  const at::Tensor *X, *weight;
+  at::ScalarType type;
+  void* s;
+  if (n != 12 || lib.head_norm == nullptr || observed() || !read_head_norm(a, &d, sections, &X, &weight) ||
+      !head_norm_output(a[9], a[10], *X, &d.Y, &type) || !stream_of(a[11], &s))
+    return declined();
+  const at::Device device = X->device();
+  at::Tensor made;
+  const int32_t st = unlocked([&] {
+    if (d.Y.data == nullptr) {
+      made = fresh_like(device, {d.T, d.H, d.D}, type);
+      d.Y.data = made.data_ptr();
+    }
+    return lib.head_norm(&d, s);
+  });
+  if (a[10] != Py_None) {
+    Py_INCREF(a[10]);
+    return result(st, a[10]);
+  }
+  return result(st, THPVariable_Wrap(std::move(made)));
+  END_HANDLE_TH_ERRORS
+}
+
+// head_norm_backward(dY, X, weight, heads, eps, centred, positions, freqs, sections, interleaved, out_dtype, out, params, workspace, stream)
+PyObject* head_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_head_norm_desc d = {};
+  int32_t sections[4];
+  const at::Tensor *X, *weight, *dY;
+  at::ScalarType type;
+  bool params;
+  void* s;
+  if (n != 15 || lib.head_norm_backward == nullptr || lib.head_norm_backward_bytes == nullptr || observed() ||
+      !read_head_norm(a + 1, &d, sections, &X, &weight) || !floating(a[0], &dY, &d.dY.dtype) || !heads_of(*dY) || dY->sizes() != X->sizes() ||
+      !head_norm_output(a[10], a[11], *X, &d.Y, &type) || !flag(a[12], &params) || !stream_of(a[14], &s))
+    return declined();
+  d.dY.data = pointer<void>(dY);
+  d.dY.token = dY->stride(0);
+  d.dY.head = dY->stride(1);
+  params = params && weight != nullptr;
+  Workspace ws;
+  if (const Take t = given_workspace(a[13], &ws); t != TAKEN) return t == DECLINED ? declined() : nullptr;
+  const size_t need = params && a[13] == Py_None ? lib.head_norm_backward_bytes(d.T, d.H, d.heads, d.D, d.rotated) : 0;
+  const at::Device device = X->device();
+  const std::vector<int64_t> sizes = params ? weight->sizes().vec() : std::vector<int64_t>();
+  at::Tensor made, dw;
+  const int32_t st = unlocked([&] {
+    if (d.Y.data == nullptr) {
+      made = fresh_like(device, {d.T, d.H, d.D}, type);
+      d.Y.data = made.data_ptr();
+    }
+    if (params) {
+      dw = fresh_like(device, sizes, at::kFloat);
+      d.dweight = static_cast<float*>(dw.data_ptr());
+    }
+    if (need == 0) return lib.head_norm_backward(&d, ws.ptr, ws.bytes, s);
+    const Scratch own(s, device, need);
+    return lib.head_norm_backward(&d, own.ptr, need, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* dx;
+  if (a[11] != Py_None) {
+    Py_INCREF(a[11]);
+    dx = a[11];
+  } else {
+    dx = THPVariable_Wrap(std::move(made));
+  }
+  if (!params) return Py_BuildValue("(NO)", dx, Py_None);
+  PyObject* dwp = THPVariable_Wrap(std::move(dw));
+  return Py_BuildValue("(NN)", dx, dwp);
+  END_HANDLE_TH_ERRORS
+}
+
+// A cache in pages: K_pages, V_pages, page_table, lengths; K_scales, V_scales.
+bool read_pages(PyObject* const* a, PyObject* k_scales, PyObject* v_scales, nm_pages* p, const at::Tensor** K) {
+  const at::Tensor *V, *table, *ks, *vs;
+  if (plain(a[0], at::kFloat8_e4m3fn, K)) p->dtype = NM_E4M3;
+  else if (plain(a[0], at::kBFloat16, K)) p->dtype = NM_OUT_BF16;
+  else return false;
+  if (!plain(a[1], (*K)->scalar_type(), &V) || (*K)->dim() != 4 || (*K)->sizes() != V->sizes() || (*K)->strides() != V->strides() ||
+      ((*K)->stride(3) != 1 && (*K)->size(3) > 1))
+    return false;
+  constexpr int64_t limit = 1 << 30;
+  for (int i = 1; i < 4; ++i)
+    if ((*K)->size(i) > limit) return false;
+  p->pages = (*K)->size(0);
+  p->page_size = (int32_t)(*K)->size(1);
+  p->heads = (int32_t)(*K)->size(2);
+  p->head_size = (int32_t)(*K)->size(3);
+  p->page = (*K)->stride(0);
+  p->token = (*K)->stride(1);
+  p->head = (*K)->stride(2);
+  p->K = pointer<void>(*K);
+  p->V = pointer<void>(V);
+  if (p->dtype == NM_E4M3) {
+    if (!plain(k_scales, at::kByte, &ks) || !plain(v_scales, at::kByte, &vs) || ks->dim() != 3 || ks->sizes() != (*K)->sizes().slice(0, 3) ||
+        vs->sizes() != ks->sizes() || vs->strides() != ks->strides())
+      return false;
+    p->scale_page = ks->stride(0);
+    p->scale_token = ks->stride(1);
+    p->scale_head = ks->stride(2);
+    p->K_scales = pointer<uint8_t>(ks);
+    p->V_scales = pointer<uint8_t>(vs);
+  } else if (k_scales != Py_None || v_scales != Py_None) {
+    return false;
+  }
+  if (!plain(a[2], at::kInt, &table) || !whole(*table) || table->size(0) > limit || table->size(1) > limit) return false;
+  p->sequences = (int32_t)table->size(0);
+  p->table_width = (int32_t)table->size(1);
+  p->table = pointer<int32_t>(table);
+  return per_sequence(a[3], p->sequences, &p->lengths) && p->lengths != nullptr;
+}
+bool packed_tokens(PyObject* obj, const nm_pages& p, nm_heads* h, int64_t* tokens) {
+  const at::Tensor* t;
+  if (!read_heads(obj, h, &t) || t->size(1) != p.heads || t->size(2) != p.head_size) return false;
+  if (*tokens < 0) *tokens = t->size(0);
+  return t->size(0) == *tokens;
+}
+
+// cache_write(K, V, K_pages, V_pages, page_table, lengths, offsets, K_scales, V_scales, stream)
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_pages p = {};
+  nm_heads K, V;
+  const at::Tensor* pages;
+  const int32_t* offsets;
+  int64_t T = -1;
+  void* s;
+  if (n != 10 || lib.cache_write == nullptr || observed() || !read_pages(a + 2, a[7], a[8], &p, &pages) || !packed_tokens(a[0], p, &K, &T) ||
+      !packed_tokens(a[1], p, &V, &T) || !per_sequence(a[6], p.sequences + 1, &offsets) || !stream_of(a[9], &s))
+    return declined();
+  const int32_t st = unlocked([&] { return lib.cache_write(&p, &K, &V, offsets, T, s); });
+  Py_INCREF(Py_None);
+  return result(st, Py_None);
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_read(K_pages, V_pages, page_table, lengths, offsets, tokens, first, K_scales, V_scales, out, stream)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_pages p = {};
+  nm_heads K = {}, V = {};
+  const at::Tensor* pages;
+  const int32_t *offsets, *first;
+  int64_t T = -1;
+  void* s;
+  if (n != 11 || lib.cache_read == nullptr || observed() || !read_pages(a, a[7], a[8], &p, &pages) ||
+      (a[5] != Py_None && !integer(a[5], 0, 1 << 30, &T)) || !per_sequence(a[4], p.sequences + 1, &offsets) ||
+      !per_sequence(a[6], p.sequences, &first) || !stream_of(a[10], &s))
+    return declined();
+  const bool given = a[9] != Py_None;
+  if (given ? !PyTuple_CheckExact(a[9]) || PyTuple_GET_SIZE(a[9]) != 2 || !packed_tokens(PyTuple_GET_ITEM(a[9], 0), p, &K, &T) ||
+                  !packed_tokens(PyTuple_GET_ITEM(a[9], 1), p, &V, &T)
+            : T < 0)
+    return declined();
+  const at::Device device = pages->device();
+  at::Tensor k, v;
+  const int32_t st = unlocked([&] {
+    if (!given) {
+      k = fresh_like(device, {T, p.heads, p.head_size}, at::kBFloat16);
+      v = fresh_like(device, {T, p.heads, p.head_size}, at::kBFloat16);
+      K = contiguous_heads(k);
+      V = contiguous_heads(v);
+    }
+    return lib.cache_read(&p, &K, &V, offsets, first, T, s);
+  });
+  if (given) {
+    Py_INCREF(a[9]);
+    return result(st, a[9]);
+  }
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* kp = THPVariable_Wrap(std::move(k));
+  PyObject* vp = THPVariable_Wrap(std::move(v));
+  return Py_BuildValue("(NN)", kp, vp);
+  END_HANDLE_TH_ERRORS
+}
+
+// attention_paged(Q, K_pages, V_pages, page_table, lengths, scale, offsets_q, window, sinks, K_scales, V_scales, max_q, max_k, lse, out,
+//                 workspace, stream)
+PyObject* attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  nm_paged_desc d = {};
+  const at::Tensor *Q, *pages, *O = nullptr;
+  bool lse;
+  int64_t window, sinks;
+  void* s;
+  if (n != 17 || lib.attention_paged == nullptr || lib.attention_paged_bytes == nullptr || observed() || !read_heads(a[0], &d.Q, &Q) ||
+      !read_pages(a + 1, a[9], a[10], &d.pages, &pages) || Q->size(2) != d.pages.head_size || Q->size(1) > 1 << 30 ||
+      !per_sequence(a[6], d.pages.sequences + 1, &d.offsets_q) || !integer(a[7], 0, 1 << 30, &window) || !integer(a[8], 0, 1 << 30, &sinks) ||
+      d.pages.sequences < 1 || !most(a[11], (Q->size(0) + d.pages.sequences - 1) / d.pages.sequences, &d.max_q) ||
+      !most(a[12], (int64_t)d.pages.table_width * d.pages.page_size, &d.max_k) || !flag(a[13], &lse) ||
+      (a[14] != Py_None && (!read_heads(a[14], &d.O, &O) || !same_sizes(*O, *Q))) || !stream_of(a[16], &s))
+    return declined();
+  if (a[5] == Py_None) d.scale = (float)(1.0 / std::sqrt((double)Q->size(2)));
+  else if (PyFloat_CheckExact(a[5])) d.scale = (float)PyFloat_AS_DOUBLE(a[5]);
+  else return declined();
+  d.Tq = Q->size(0);
+  d.heads_q = (int32_t)Q->size(1);
+  d.window = (int32_t)window;
+  d.sinks = (int32_t)sinks;
+  Workspace ws;
+  if (const Take t = given_workspace(a[15], &ws); t != TAKEN) return t == DECLINED ? declined() : nullptr;
+  const size_t need = a[15] == Py_None ? lib.attention_paged_bytes(d.Tq, d.pages.sequences, d.heads_q, d.pages.heads, d.pages.head_size, d.max_q) : 0;
+  const at::Device device = Q->device();
+  const std::vector<int64_t> sizes = Q->sizes().vec();
+  at::Tensor made, sums;
+  const int32_t st = unlocked([&] {
+    if (O == nullptr) {
+      made = fresh_like(device, sizes, at::kBFloat16);
+      d.O = contiguous_heads(made);
+    }
+    if (lse) {
+      sums = fresh(device, d.heads_q, d.Tq, at::kFloat);
+      d.lse = static_cast<float*>(sums.data_ptr());
+    }
+    if (need == 0) return lib.attention_paged(&d, ws.ptr, ws.bytes, s);
+    const Scratch own(s, device, need);
+    return lib.attention_paged(&d, own.ptr, need, s);
+  });
+  if (st != NM_OK) return result(st, nullptr);
+  PyObject* out;
+  if (O != nullptr) {
+    Py_INCREF(a[14]);
+    out = a[14];
+  } else {
+    out = THPVariable_Wrap(std::move(made));
+  }
+  return lse ? Py_BuildValue("(NN)", out, THPVariable_Wrap(std::move(sums))) : out;
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(addresses by name, raise_status, find_workspace[, where that keeps its tensors])
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *table, *raise, *find, *kept = nullptr;
@@ -898,7 +1211,11 @@ PyObject* bind(PyObject*, PyObject* args) {
       {"nm_layer_norm_backward_workspace_bytes", &l.layer_norm_backward_bytes, true}, {"nm_rotary", &l.rotary, true},
       {"nm_attention", &l.attention, true}, {"nm_attention_workspace_bytes", &l.attention_bytes, true},
       {"nm_attention_backward", &l.attention_backward, true},
-      {"nm_attention_backward_workspace_bytes", &l.attention_backward_bytes, true}};
+      {"nm_attention_backward_workspace_bytes", &l.attention_backward_bytes, true},
+      {"nm_head_norm", &l.head_norm, true}, {"nm_head_norm_backward", &l.head_norm_backward, true},
+      {"nm_head_norm_backward_workspace_bytes", &l.head_norm_backward_bytes, true}, {"nm_cache_write", &l.cache_write, true},
+      {"nm_cache_read", &l.cache_read, true}, {"nm_attention_paged", &l.attention_paged, true},
+      {"nm_attention_paged_workspace_bytes", &l.attention_paged_bytes, true}};
   for (auto& e : slots) {
     PyObject* address = PyDict_GetItemString(table, e.name);
     if (address == nullptr && e.optional) continue;
@@ -934,6 +1251,11 @@ PyMethodDef methods[] = {
     {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
     {"attention_backward", (PyCFunction)(void (*)())attention_backward, METH_FASTCALL, nullptr},
+    {"head_norm", (PyCFunction)(void (*)())head_norm, METH_FASTCALL, nullptr},
+    {"head_norm_backward", (PyCFunction)(void (*)())head_norm_backward, METH_FASTCALL, nullptr},
+    {"cache_write", (PyCFunction)(void (*)())cache_write, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)())cache_read, METH_FASTCALL, nullptr},
+    {"attention_paged", (PyCFunction)(void (*)())attention_paged, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nm_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

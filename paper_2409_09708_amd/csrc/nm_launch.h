@@ -303,4 +303,67 @@ size_t attention_grad_workspace_bytes(int64_t Tq, int64_t Tk, int B, int Hq, int
                                       bool causal);
 hipError_t launch_attention_grad(const AttentionCall& c, hipStream_t s);
 
+// nm_head_norm.hip: norm of heads and their rotary turn, and the backward pass of both
+struct HeadNormCall {
+  const void* X;
+  const void* dY;         // backward only
+  const float* w;         // nullable; [1 or 2][D]
+  void* Y;                // backward: dX
+  float* dw;              // backward only; nullable
+  const void* positions;  // [T, axes]; not used where R is 0
+  const float* freqs;     // [R / 2]
+  int64_t T, H, heads, D, R;                                       // heads from `heads` on take the second row of w
+  int64_t x_token, x_head, dy_token, dy_head, y_token, y_head;     // strides in elements
+  int section_end[kMaxRotaryAxes];
+  int axes;
+  float eps;
+  bool centred, positions_f32, interleaved, x_f32, dy_f32, y_f32;
+  void* workspace;        // head_norm_grad_workspace_bytes, needed where dw is asked for
+};
+hipError_t launch_head_norm(const HeadNormCall& c, hipStream_t s);
+size_t head_norm_grad_workspace_bytes(int64_t T, int64_t H, int64_t D, int64_t R, int sets);
+hipError_t launch_head_norm_grad(const HeadNormCall& c, hipStream_t s);
+
+// nm_pages.hip, nm_paged.hip: a cache of keys and values in pages.  Strides in elements (of bfloat16, of codes, of exponent bytes).
+struct PagesCall {
+  void* K;
+  void* V;
+  uint8_t* K_scales;  // e4m3 only
+  uint8_t* V_scales;
+  int64_t page, token, head, scale_page, scale_token, scale_head;
+  const int32_t* table;    // [B, width]
+  const int32_t* lengths;  // [B]
+  int64_t pages;
+  int page_size, width, B, H, D;
+  bool e4m3;
+};
+struct CacheWriteCall {
+  PagesCall p;
+  HeadRows K, V;
+  const int32_t* offsets;  // nullable: T / B tokens of each sequence
+  int64_t T;
+};
+hipError_t launch_cache_write(const CacheWriteCall& c, hipStream_t s);
+struct CacheReadCall {
+  PagesCall p;
+  HeadRows K, V;           // out
+  const int32_t* offsets;  // rows of the outputs; nullable: T / B of each sequence
+  const int32_t* first;    // nullable: from the first token on
+  int64_t T;
+};
+hipError_t launch_cache_read(const CacheReadCall& c, hipStream_t s);
+struct PagedCall {
+  PagesCall p;
+  HeadRows Q, O;
+  float* lse;                // nullable; [Hq, Tq]
+  const int32_t* offsets_q;  // nullable: Tq / B queries of each sequence
+  int64_t Tq, max_q, max_k;
+  int Hq, window, sinks;     // window 0: none
+  float scale;
+  void* workspace;
+};
+size_t paged_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks);
+size_t paged_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q);  // ... of any max_k, window and sinks
+hipError_t launch_paged(const PagedCall& c, hipStream_t s);
+
 }  // namespace nm

@@ -1,0 +1,734 @@
+// Softmax attention of new tokens over a cache in pages, one token or a chunk of them per sequence, grouped heads.  Query i of the Lq
+// new tokens of a sequence of n tokens stands at p = n - Lq + i and sees the keys
+//
+//   j <= p  with  j > p - window (where there is one)  or  j < sinks,   whose pages are there;
+//   s_j = scale q_i . k_j,  o_i = sum_j exp(s_j - lse_i) v_j,  lse_i = log sum_j exp(s_j);   none: o_i = 0, lse_i = -infinity.
+//
+// Scores are computed transposed, as nm_attention.h has it; the columns are the (query, head of the group) pairs that share a key head, so
+// that all of them share the keys that are read.  The keys that any query of a run can see are numbered without the gap between sinks and
+// window ("views"), so tiles hold no keys that nobody sees, and what is masked, past the end or on a page that is not there is never read:
+// its value is a zero and its score minus infinity.  A lane looks up the page of one row of a tile, two tiles ahead of its use, and
+// rows come through registers: 8-bit rows become bfloat16 on the way to LDS, exactly.
+//
+// Two kernels.  paged_few_kernel: 32 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
+// the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
+// paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves; keys cut evenly where there are few blocks.
+#include "nm_attention.h"
+#include "nm_pages.h"
+
+namespace nm {
+
+namespace {
+
+struct PagedArgs {
+  PagedCall c;
+  PageDivide divide;
+  int group;         // heads that share a key head
+  float scale_log2;  // scale * log2(e)
+  int n_tiles;       // column tiles of a unit that the grid has
+  int cuts;          // few: whether units are dealt to blocks; chunk: pieces of a unit's keys
+  float* part_o;     // few: [slot][32][DP]; chunk: [query][head][cut][DP]
+  float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
+  int slots;         // few: that the workspace holds
+  bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
+};
+
+// Sequence b: its first packed query, how many there are, and its tokens.  Whatever the caller's numbers are, rows stay inside the tensors.
+struct PagedSequence {
+  int q0, len, n;
+};
+__device__ __forceinline__ PagedSequence paged_sequence(const PagedCall& c, int b) {
+  const int lane = threadIdx.x & 63;
+  const int each = (int)(c.Tq / c.p.B);
+  int v = lane == 0 ? b * each : (b + 1) * each;
+  if (lane == 2) v = c.p.lengths[b];
+  else if (lane < 2 && c.offsets_q != nullptr) v = c.offsets_q[b + lane];
+  const int n = page_clamped(c.p, __builtin_amdgcn_readlane(v, 2));
+  int q0 = __builtin_amdgcn_readlane(v, 0), q1 = __builtin_amdgcn_readlane(v, 1);
+  q0 = q0 < 0 ? 0 : q0 < c.Tq ? q0 : (int)c.Tq;
+  q1 = q1 < q0 ? q0 : q1 < c.Tq ? q1 : (int)c.Tq;
+  return {q0, q1 - q0, n};
+}
+
+// The keys that queries at positions first .. last may see, numbered without the gap: view v is key v below `sinks`, else v + gap.
+// ALIGN: both parts begin at multiples of it, which adds views that nobody sees.
+struct Views {
+  int sinks, gap, count;
+  int hidden_from, hidden_to;  // keys in between are seen by none of the queries
+  __device__ __forceinline__ int key(int v) const { return v < sinks ? v : v + gap; }
+};
+template <int ALIGN>
+__device__ __forceinline__ Views paged_views(const PagedCall& c, int first, int last) {
+  const int end = last + 1 > 0 ? last + 1 : 0;
+  int64_t lo = 0;
+  if (c.window > 0) lo = (int64_t)first - c.window + 1;
+  const int from = lo > 0 ? (int)(lo < end ? lo : end) : 0, sinks = c.sinks < from ? c.sinks : from;
+  const int from_a = from / ALIGN * ALIGN, sinks_a = (sinks + ALIGN - 1) / ALIGN * ALIGN;
+  if (from_a <= sinks_a) return {0, 0, end, sinks, from};
+  return {sinks_a, from_a - sinks_a, sinks_a + end - from_a, sinks, from};
+}
+
+// Rows of a tile as one lane knows them: lane r (< ROWS) has row r's place in a page, or that it is not there.
+struct RowPlaces {
+  int entry, slot;  // of the next tile: the table's entry, and the slot in its page (-1: not there)
+  __device__ __forceinline__ void look_up(const PagedArgs& a, const int32_t* table, const Views& w, int v, bool in_tile) {
+    const int key = w.key(v);
+    slot = -1;
+    entry = -1;
+    if (in_tile && v < w.count && (key < w.hidden_from || key >= w.hidden_to)) {
+      const int page = page_of(a.divide, key);
+      slot = key - page * a.c.p.page_size;
+      entry = table[page];
+    }
+  }
+};
+
+// A tile of ROWS rows of keys and of values, by LANES lanes (a wave or a block), through registers to LDS as bfloat16.  They come as
+// bfloat16 or as CODES, of exactly DP elements in 16-byte aligned rows (WHOLE) or any.
+//   look_up(v0)   starts the look-up of the pages of views v0 ..
+//   fetch()       starts the loads of the tile looked up last
+//   settle(stage) rows to LDS, zeros for those that are not there (a block's barrier follows)
+//   seen          the rows of the tile fetched last that are there, a bit each
+template <int DP, int ROWS, bool CODES, bool WHOLE, int LANES>
+struct PagedTile {
+  using Tile = RowTile<DP>;
+  static constexpr int kBytes = ROWS * Tile::kRowBytes;
+  static constexpr int kPer = CODES ? DP / 16 : DP / 8, kPieces = ROWS * kPer;  // 16-byte pieces as they come
+  static constexpr int kLoads = (kPieces + LANES - 1) / LANES;
+  const PagedArgs* a;
+  const int32_t* table;
+  Views w;
+  const unsigned char* base[2];
+  const uint8_t* scales[2];
+  unsigned char* smem;  // stages of 2 * kBytes
+  RowPlaces next;
+  u32x4_t in[2][kLoads];
+  uint32_t exponents;  // lane r: those of row r's keys and values
+  uint64_t seen;
+
+  __device__ __forceinline__ void begin(const PagedArgs& args, int seq, int head, const Views& views, unsigned char* lds) {
+    a = &args;
+    w = views;
+    smem = lds;
+    const PagesCall& p = args.c.p;
+    table = p.table + (int64_t)seq * p.width;
+    const int64_t at = (int64_t)head * p.head * (CODES ? 1 : 2);
+    base[0] = static_cast<const unsigned char*>(p.K) + at;
+    base[1] = static_cast<const unsigned char*>(p.V) + at;
+    if constexpr (CODES) {
+      scales[0] = p.K_scales + head * p.scale_head;
+      scales[1] = p.V_scales + head * p.scale_head;
+    }
+  }
+  __device__ __forceinline__ void look_up(int v0) {
+    const int lane = threadIdx.x & 63;
+    next.look_up(*a, table, w, v0 + lane, lane < ROWS);
+  }
+  __device__ __forceinline__ void fetch() {
+    const PagesCall& p = a->c.p;
+    const int tid = threadIdx.x % LANES;
+    const bool there = next.slot >= 0 && (uint32_t)next.entry < (uint64_t)p.pages;
+    seen = __ballot(there);
+    const int64_t at = there ? (int64_t)next.entry * p.page + (int64_t)next.slot * p.token : 0;
+    const int lo = (int)(uint32_t)at, hi = (int)(at >> 32);
+    if constexpr (CODES) {
+      exponents = 0;
+      if (there) {
+        const int64_t s = (int64_t)next.entry * p.scale_page + (int64_t)next.slot * p.scale_token;
+        exponents = scales[0][s] | (uint32_t)scales[1][s] << 8;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int i = n * LANES + tid, row = i / kPer, piece = i % kPer;
+      const int src = row < 64 ? row : 0;
+      const int64_t from = ((int64_t)__shfl(hi, src, 64) << 32 | (uint32_t)__shfl(lo, src, 64)) * (CODES ? 1 : 2) + piece * 16;
+      const bool live = (kPieces % LANES == 0 || i < kPieces) && (seen >> src & 1);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        in[t][n] = u32x4_t{0, 0, 0, 0};
+        if (!live) continue;
+        if constexpr (WHOLE) in[t][n] = *reinterpret_cast<const u32x4_t*>(base[t] + from);
+        else if constexpr (CODES) in[t][n] = load_codes(base[t] + from, 0, a->c.p.D - piece * 16);
+        else in[t][n] = load_piece(reinterpret_cast<const bf16_t*>(base[t] + from), 0, a->c.p.D - piece * 8, true);
+      }
+    }
+  }
+  __device__ __forceinline__ void settle(int stage) {
+    const int tid = threadIdx.x % LANES;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int i = n * LANES + tid, row = i / kPer, piece = i % kPer;
+      const uint32_t e = CODES ? (uint32_t)__shfl((int)exponents, row < 64 ? row : 0, 64) : 0;
+      if (kPieces % LANES == 0 || i < kPieces) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          unsigned char* to = smem + (2 * stage + t) * kBytes;
+          if constexpr (CODES) {
+            u32x4_t v[2];
+            decode16(in[t][n], t ? e >> 8 : e & 255, v);
+            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece)) = v[0];
+            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece + 1)) = v[1];
+          } else {
+            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, piece)) = in[t][n];
+          }
+        }
+      }
+    }
+  }
+};
+
+// Whether a tile of views v0 .. v0 + ROWS - 1 whose rows are all there is seen whole by queries at positions first .. last.
+template <int ROWS>
+__device__ __forceinline__ bool seen_whole(const PagedCall& c, const Views& w, int v0, int first, int last) {
+  const int from = w.key(v0), to = w.key(v0 + ROWS - 1);
+  return to <= first && (c.window <= 0 || (int64_t)from > (int64_t)last - c.window || to < c.sinks);
+}
+
+// Scores that the query at position p does not see are minus infinity: rows v0 + acc_row(r) of the accumulator, `seen` from bit `bit` on.
+__device__ __forceinline__ void hide_unseen(f32x16_t& s, const PagedCall& c, const Views& w, int v0, int p, uint64_t seen, int bit) {
+  const int64_t low = c.window > 0 ? (int64_t)p - c.window : -1;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int key = w.key(v0 + acc_row(r));
+    const bool sees = key <= p && (key > low || key < c.sinks) && (seen >> (bit + acc_row(r)) & 1);
+    s[r] = sees ? s[r] : kMinusInf;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------
+// few queries
+// ------------------------------------------------------------------------------------------------------
+constexpr int kRun = 32, kStep = kWaves * kRun;  // keys of a wave, of a block, at a time
+
+// The list of all units' steps, key heads outermost, then sequences, then their column tiles; every tile of a sequence has as many steps.
+// 64 sequences at a time: a lane has one's steps and tiles, and their running sums.
+struct Units {
+  int b0;             // first sequence of those at hand
+  int steps, tiles;   // of the lane's sequence
+  int64_t upto;       // steps of all tiles, up to the lane's sequence and with it
+  int tiles_upto;
+};
+__device__ __forceinline__ Views few_views(const PagedCall& c, const PagedSequence& of) {
+  return paged_views<1>(c, of.n - of.len, of.n - 1);
+}
+__device__ __forceinline__ void few_units(const PagedArgs& a, int b0, Units* u) {
+  const int lane = threadIdx.x & 63, b = b0 + lane;
+  u->b0 = b0;
+  u->steps = u->tiles = 0;
+  if (b < a.c.p.B) {
+    const int each = (int)(a.c.Tq / a.c.p.B);
+    PagedSequence of = {b * each, each, page_clamped(a.c.p, a.c.p.lengths[b])};
+    if (a.c.offsets_q != nullptr) {
+      const int Tq = (int)a.c.Tq;
+      int q0 = a.c.offsets_q[b], q1 = a.c.offsets_q[b + 1];
+      q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
+      q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
+      of.len = q1 - q0;
+    }
+    const int steps = (few_views(a.c, of).count + kStep - 1) / kStep;
+    u->steps = steps > 0 ? steps : 1;
+    u->tiles = (of.len * a.group + 31) / 32;
+  }
+  u->upto = (int64_t)u->steps * u->tiles;
+  u->tiles_upto = u->tiles;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int lo = __shfl_up((int)(uint32_t)u->upto, m, 64), hi = __shfl_up((int)(u->upto >> 32), m, 64), t = __shfl_up(u->tiles_upto, m, 64);
+    if (lane >= m) {
+      u->upto += (int64_t)hi << 32 | (uint32_t)lo;
+      u->tiles_upto += t;
+    }
+  }
+}
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+  return (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+// Steps and tiles of all sequences, for one key head; `u` is left at the first 64.
+__device__ __forceinline__ void few_totals(const PagedArgs& a, Units* u, int64_t* steps, int* tiles) {
+  *steps = 0;
+  *tiles = 0;
+  for (int b0 = (a.c.p.B - 1) / 64 * 64; b0 >= 0; b0 -= 64) {
+    few_units(a, b0, u);
+    *steps += lane_value(u->upto, 63);
+    *tiles += __builtin_amdgcn_readlane(u->tiles_upto, 63);
+  }
+}
+
+// Where step `at` of a key head's list (or, BY_TILE, tile `at`) lies.
+struct UnitPlace {
+  int seq, tile, step, steps;  // a tile of `steps` steps, `step` of which are before this one
+  int unit;                    // tiles before it
+  int64_t begin;               // steps before its first
+};
+template <bool BY_TILE>
+__device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int64_t at) {
+  int64_t steps_before = 0;
+  int tiles_before = 0;
+  for (int b0 = 0;; b0 += 64) {
+    if (u->b0 != b0) few_units(a, b0, u);
+    const int64_t all = lane_value(u->upto, 63);
+    const int all_tiles = __builtin_amdgcn_readlane(u->tiles_upto, 63);
+    const bool here = BY_TILE ? at < tiles_before + all_tiles : at < steps_before + all;
+    if (here || b0 + 64 >= a.c.p.B) {
+      const uint64_t above = BY_TILE ? __ballot((int64_t)tiles_before + u->tiles_upto > at) : __ballot(steps_before + u->upto > at);
+      const int l = above ? __ffsll((unsigned long long)above) - 1 : 63;
+      UnitPlace p;
+      p.seq = b0 + l < a.c.p.B ? b0 + l : a.c.p.B - 1;
+      p.steps = __builtin_amdgcn_readlane(u->steps, l);
+      const int tiles = __builtin_amdgcn_readlane(u->tiles, l);
+      const int64_t first = steps_before + lane_value(u->upto, l) - (int64_t)p.steps * tiles;
+      const int first_tile = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles;
+      p.tile = BY_TILE ? (int)(at - first_tile) : (int)((at - first) / (p.steps > 0 ? p.steps : 1));
+      p.begin = first + (int64_t)p.tile * p.steps;
+      p.step = BY_TILE ? 0 : (int)(at - p.begin);
+      p.unit = first_tile + p.tile;
+      return p;
+    }
+    steps_before += all;
+    tiles_before += all_tiles;
+  }
+}
+constexpr int64_t kLeastShare = 2;  // steps that a block takes at least
+__device__ __forceinline__ int64_t few_share(int64_t all, int blocks) {
+  const int64_t even = (all + blocks - 1) / blocks;
+  return even < kLeastShare ? kLeastShare : even;
+}
+
+template <int DP, bool CODES, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs a) {
+  using Tile = RowTile<DP>;
+  using Load = PagedTile<DP, kRun, CODES, WHOLE, 64>;
+  constexpr int NB = DP / 32, STEPS = DP / 16;
+  constexpr int JOIN = 32 * (DP + 4) * 4;  // one wave's output, columns padded against bank conflicts
+  constexpr int OWN = 2 * Load::kBytes;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * (OWN > JOIN ? OWN : JOIN)];
+  __shared__ float2 wave_ml[kWaves][32];
+  const PagedCall& c = a.c;
+  const int D = WHOLE ? DP : c.p.D;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  // this block's run of the list of steps -- or, uncut, every (gridDim.x)-th of the units that the grid was made for
+  Units units;
+  units.b0 = -1;
+  int64_t at, end = 0, per_head = 0;
+  int tiles_per_head = 0;
+  if (a.cuts) {
+    few_totals(a, &units, &per_head, &tiles_per_head);
+    const int64_t share = few_share(per_head * c.p.H, (int)gridDim.x);
+    at = blockIdx.x * share;
+    end = at + share < per_head * c.p.H ? at + share : per_head * c.p.H;
+  } else {
+    at = blockIdx.x;
+    end = (int64_t)c.p.B * c.p.H * a.n_tiles;
+  }
+  while (at < end) {
+    int seq, kv_head, tile, step, steps, slot = 0;
+    bool alone = true;  // the whole unit is this block's
+    if (a.cuts) {
+      kv_head = (int)(at / per_head);
+      const UnitPlace p = few_place<false>(a, &units, at - kv_head * per_head);
+      seq = p.seq; tile = p.tile; step = p.step;
+      steps = (int)(end - at < p.steps - step ? end - at : p.steps - step);
+      alone = steps == p.steps;
+      slot = kv_head * tiles_per_head + p.unit + (int)blockIdx.x;  // (each further unit, and each further block, is one more)
+      at += steps;
+    } else {
+      seq = (int)(at / (c.p.H * a.n_tiles));
+      kv_head = (int)(at / a.n_tiles % c.p.H);
+      tile = (int)(at % a.n_tiles);
+      step = steps = 0;
+      at += gridDim.x;
+    }
+    const PagedSequence of = paged_sequence(c, seq);
+    const Views views = few_views(c, of);
+    const int last_view = a.cuts && (step + steps) * kStep < views.count ? (step + steps) * kStep : views.count;
+    Load load;
+    load.begin(a, seq, kv_head, views, smem + wave * OWN);
+    const int columns = of.len * a.group;
+    // (a sequence of more queries than the grid was made for has further tiles)
+    for (; tile * 32 < columns; tile += a.n_tiles) {
+      const int n = tile * 32 + col;
+      const bool live = n < columns;
+      const int qi = n / a.group, head = kv_head * a.group + n % a.group;
+      const int first = of.n - of.len, p = first + qi;  // positions
+      const int least_p = first + tile * 32 / a.group, most_p = first + (tile * 32 + 31 < columns ? tile * 32 + 31 : columns - 1) / a.group;
+      const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
+      __syncthreads();  // (what the waves joined last has been read)
+      int v0 = step * kStep + wave * kRun;
+      load.look_up(v0);
+      u32x4_t q[STEPS];
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+      if (v0 < last_view) {
+        load.fetch();
+        load.look_up(v0 + kStep);
+      }
+      f32x16_t acc[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+      float ref = kMinusInf, sum = 0.f;
+      for (; v0 < last_view; v0 += kStep) {
+        const uint64_t seen = load.seen;
+        load.settle(0);
+        if (v0 + kStep < last_view) {
+          load.fetch();
+          load.look_up(v0 + 2 * kStep);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t k_tile = NM_LDS_ADDRESS(smem) + wave * OWN;
+        const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = k_tile + Load::kBytes + Tile::column_base(lane);
+        constexpr int NV = kRun / 16 * NB;
+        auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
+        auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
+        f32x16_t s[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+        u32x4_t f[kAhead];
+        read_ahead<STEPS>(f, keys);
+        products<STEPS>(f, keys, [&](int i, u32x4_t k) { s[0] = mma32(k, q[i], s[0]); });
+        read_ahead<NV>(f, values);
+        if ((uint32_t)seen != 0xFFFFFFFFu || !seen_whole<kRun>(c, views, v0, least_p, most_p))
+          hide_unseen(s[0], c, views, v0 + 4 * half, p, seen, 4 * half);
+        softmax_step(s, a.scale_log2, ref, sum, acc);
+        const u32x4_t pr[2] = {acc_operand(s[0], 0), acc_operand(s[0], 1)};
+        products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
+        __builtin_amdgcn_wave_barrier();
+      }
+      // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
+      sum = half_sum(sum);
+      if (half == 0) wave_ml[wave][col] = float2{ref, sum};
+      __syncthreads();
+      float top = kMinusInf, total = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_ml[w][col].x);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) total += wave_ml[w][col].y * part_weight(wave_ml[w][col].x, top);
+      const float by = part_weight(ref, top);
+      float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4*>(joined + col * (DP + 4) + 32 * b + acc_row(r) + 4 * half) =
+              float4{acc[b][r] * by, acc[b][r + 1] * by, acc[b][r + 2] * by, acc[b][r + 3] * by};
+      __syncthreads();
+      // lane -> (column, four elements)
+      constexpr int PER_COL = DP / 4;
+#pragma unroll
+      for (int i = 0; i < 32 * PER_COL / kThreads; ++i) {
+        const int to = i * kThreads + tid, cc = to / PER_COL, d = to % PER_COL * 4;
+        const int cn = tile * 32 + cc;
+        if (cn >= columns || d >= D) continue;
+        const float* from = reinterpret_cast<const float*>(smem) + cc * (DP + 4) + d;
+        float4 o = *reinterpret_cast<const float4*>(from);
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+          const float4 x = *reinterpret_cast<const float4*>(from + w * 32 * (DP + 4));
+          o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        }
+        if (alone) {
+          const int64_t tok = of.q0 + cn / a.group;
+          const int hd = kv_head * a.group + cn % a.group;
+          float t = kMinusInf, l = 0.f;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) t = fmaxf(t, wave_ml[w][cc].x);
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) l += wave_ml[w][cc].y * part_weight(wave_ml[w][cc].x, t);
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          store4(c.O.p + tok * c.O.token + hd * c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        } else if (slot < a.slots) {  // (always, of offsets that do not decrease)
+          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * 32 + cc) * DP + d) = o;
+        }
+      }
+      if (wave == 0 && half == 0 && live) {
+        if (!alone) {
+          if (slot < a.slots) a.part_ml[(int64_t)slot * 32 + col] = float2{top, total};
+        } else if (c.lse != nullptr)
+          c.lse[(int64_t)head * c.Tq + of.q0 + qi] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
+      }
+      if (a.cuts) break;
+    }
+  }
+}
+
+// One column's parts, `stride` columns of DP elements apart, joined in order by a wave: DP / 4 lanes take four elements each of every
+// (256 / DP)-th part, so that several parts' loads are under way.
+template <int DP>
+__device__ __forceinline__ void join_parts(const PagedCall& c, const float* part_o, const float2* part_ml, int64_t stride, int parts,
+                                           int64_t tok, int head) {
+  constexpr int LANES = DP / 4, GROUPS = 64 / LANES;
+  const int lane = threadIdx.x & 63, part = lane / LANES, d = lane % LANES * 4;
+  float top = kMinusInf;
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[k * stride].x);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+  float total = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = part; k < parts; k += GROUPS) {
+    const float2 ml = part_ml[k * stride];
+    const float by = part_weight(ml.x, top);
+    total = fmaf(ml.y, by, total);
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(part_o + k * stride * DP + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = d + e < c.p.D ? fmaf(x[e], by, o[e]) : 0.f;
+  }
+#pragma unroll
+  for (int m = LANES; m < 64; m <<= 1) {
+    total += __shfl_xor(total, m, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m, 64);
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  if (part == 0)
+    store4(c.O.p + tok * c.O.token + head * c.O.head, d, c.p.D, pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  if (c.lse != nullptr && lane == 0) c.lse[(int64_t)head * c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
+}
+
+// A block takes units in turn, a wave a unit's columns; units that one block of the first launch had whole are done.
+template <int DP>
+__global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a, int blocks) {
+  const PagedCall& c = a.c;
+  Units units;
+  int64_t per_head;
+  int tiles_per_head;
+  few_totals(a, &units, &per_head, &tiles_per_head);
+  const int64_t share = few_share(per_head * c.p.H, blocks);
+  for (int64_t i = blockIdx.x; i < (int64_t)tiles_per_head * c.p.H; i += gridDim.x) {
+    const int kv_head = (int)(i / tiles_per_head);
+    const UnitPlace p = few_place<true>(a, &units, i - (int64_t)kv_head * tiles_per_head);
+    const int64_t begin = kv_head * per_head + p.begin;
+    const int64_t from = begin / share, to = (begin + p.steps - 1) / share;
+    const int64_t slot = i + from;
+    if (from == to || slot + (to - from) >= a.slots) continue;
+    const PagedSequence of = paged_sequence(c, p.seq);
+    const int columns = of.len * a.group;
+    for (int col = threadIdx.x >> 6; col < 32 && p.tile * 32 + col < columns; col += kWaves) {
+      const int n = p.tile * 32 + col;
+      join_parts<DP>(c, a.part_o + (slot * 32 + col) * DP, a.part_ml + slot * 32 + col, 32, (int)(to - from + 1), of.q0 + n / a.group,
+                     kv_head * a.group + n % a.group);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------
+// chunks of queries
+// ------------------------------------------------------------------------------------------------------
+constexpr int kChunkKeys = 64, kChunkColumns = kWaves * 32;
+
+template <int DP, bool CODES, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArgs a) {
+  using Tile = RowTile<DP>;
+  using Load = PagedTile<DP, kChunkKeys, CODES, WHOLE, kThreads>;
+  constexpr int NB = DP / 32, STEPS = DP / 16;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * Load::kBytes];
+  const PagedCall& c = a.c;
+  TilePlace place;
+  if (!tile_place(c.p.B, c.p.H, 1, a.n_tiles * a.cuts, true, true, &place)) return;
+  const int kv_head = place.kv_head, seq = place.seq, cut = place.tile % a.cuts;
+  const int D = WHOLE ? DP : c.p.D;
+  const PagedSequence of = paged_sequence(c, seq);
+  const int columns = of.len * a.group;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+  const int first = of.n - of.len;  // the first query's position
+  for (int tile = place.tile / a.cuts; tile * kChunkColumns < columns; tile += a.n_tiles) {
+    const int c0 = tile * kChunkColumns, c_wave = c0 + wave * 32, n = c_wave + (lane & 31);
+    auto position = [&](int column) { return first + (column < columns ? column : columns - 1) / a.group; };
+    const bool live = n < columns;
+    const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + qi;
+    const int least_p = position(c_wave), most_p = position(c_wave + 31);
+    const Views views = paged_views<kChunkKeys>(c, position(c0), position(c0 + kChunkColumns - 1));
+    const int all = (views.count + kChunkKeys - 1) / kChunkKeys;
+    const int from = (int)((int64_t)all * cut / a.cuts), to = (int)((int64_t)all * (cut + 1) / a.cuts);
+    Load load;
+    load.begin(a, seq, kv_head, views, smem[0]);
+    __syncthreads();  // (a block's second tile: the first one's keys are no longer read)
+    load.look_up(from * kChunkKeys);
+    u32x4_t q[STEPS];
+    const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+    if (from < to) load.fetch();
+    load.look_up((from + 1) * kChunkKeys);
+    f32x16_t acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+    float ref = kMinusInf, sum = 0.f;
+    for (int kt = from; kt < to; ++kt) {
+      const int stage = (kt - from) & 1, v0 = kt * kChunkKeys;
+      const uint64_t seen = load.seen;
+      load.settle(stage);
+      __syncthreads();
+      if (kt + 1 < to) {
+        load.fetch();
+        load.look_up(v0 + 2 * kChunkKeys);
+      }
+      // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
+      const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
+      if (c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= (int64_t)least_p - c.window && k_first >= c.sinks)) continue;
+      const uint32_t k_tile = NM_LDS_ADDRESS(smem[0]) + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
+      const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
+      constexpr int KB = kChunkKeys / 32, NS = KB * STEPS, NV = kChunkKeys / 16 * NB;
+      // (products on the same sums wait for each other: the two runs of keys in turn)
+      auto keys = [&](int i) { return Tile::rows(k_at, i % KB * 32, i / KB); };
+      auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
+      f32x16_t s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+      u32x4_t f[kAhead];
+      read_ahead<NS>(f, keys);
+      products<NS>(f, keys, [&](int i, u32x4_t k) { s[i % KB] = mma32(k, q[i / KB], s[i % KB]); });
+      read_ahead<NV>(f, values);
+      if (seen != ~0ull || !seen_whole<kChunkKeys>(c, views, v0, least_p, most_p)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) hide_unseen(s[kb], c, views, v0 + 32 * kb + 4 * half, p, seen, 32 * kb + 4 * half);
+      }
+      softmax_step(s, a.scale_log2, ref, sum, acc);
+      u32x4_t pr[kChunkKeys / 16];
+#pragma unroll
+      for (int st = 0; st < kChunkKeys / 16; ++st) pr[st] = acc_operand(s[st / 2], st % 2);
+      products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
+    }
+    sum = half_sum(sum);
+    if (a.cuts > 1) {
+      if (live) {
+        const int64_t part = ((int64_t)(of.q0 + qi) * c.Hq + head) * a.cuts + cut;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<float4*>(a.part_o + part * DP + 32 * b + acc_row(r) + 4 * half) =
+                float4{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
+        if (half == 0) a.part_ml[part] = float2{ref, sum};
+      }
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    auto o_row = [&](int column) {
+      return c.O.p + (int64_t)(of.q0 + column / a.group) * c.O.token + (kv_head * a.group + column % a.group) * c.O.head;
+    };
+    if (WHOLE && a.whole_o) {
+      WaveRows<DP>::store([&](int r) { return o_row(c_wave + r); }, columns - c_wave, acc, lane, inv);
+    } else if (live) {
+      store_column<DP>(o_row(n), acc, lane, D, inv);
+    }
+    if (live && c.lse != nullptr && half == 0)
+      c.lse[(int64_t)head * c.Tq + of.q0 + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
+  }
+}
+
+// A wave per (query, head).
+template <int DP>
+__global__ void __launch_bounds__(kThreads) paged_chunk_join_kernel(const PagedArgs a) {
+  const PagedSequence of = paged_sequence(a.c, (int)blockIdx.y);
+  for (int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); i < (int64_t)of.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
+    const int64_t tok = of.q0 + i / a.c.Hq, at = (tok * a.c.Hq + i % a.c.Hq) * a.cuts;
+    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, 1, a.cuts, tok, (int)(i % a.c.Hq));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------
+// How a call is cut
+// ------------------------------------------------------------------------------------------------------
+constexpr int64_t kFewColumns = 128;           // (query, head) pairs of a key head up to which the first kernel serves
+constexpr int64_t kFewSequences = 512;         // up to which the list of steps is dealt out
+constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences, likewise
+constexpr int64_t kFewBlocks = 512;            // blocks that the list is dealt to: two of each compute unit
+constexpr int64_t kUncutKeys = 4 * kStep;      // most keys of a call whose units are left whole
+constexpr int64_t kChunkBlocks = 512, kMostCuts = 16, kLeastCut = 8;  // blocks wanted; key tiles of a cut at least
+struct PagedPlan {
+  bool few;
+  int cuts;
+  int64_t n_tiles, blocks;
+  size_t columns;  // of DP sums, in the workspace
+};
+PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int64_t max_q, int64_t views) {
+  PagedPlan p = {};
+  const int64_t group = Hq / Hkv, units = (int64_t)B * Hkv;
+  p.few = max_q * group <= kFewColumns;
+  const int64_t per_tile = p.few ? 32 : kChunkColumns;
+  p.n_tiles = (max_q * group + per_tile - 1) / per_tile;
+  if (p.n_tiles < 1) p.n_tiles = 1;
+  if (p.few) {
+    const int64_t tiles = B + Tq * group / 32;  // at most
+    p.cuts = B <= kFewSequences && tiles <= kFewTiles && views > kUncutKeys;
+    p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
+    p.columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * 32 : 0;
+  } else {
+    while (tile_blocks(B, Hkv, 1, (int)p.n_tiles) >= kMostBlocks) p.n_tiles = (p.n_tiles + 1) / 2;  // (blocks take several then)
+    int64_t cuts = kChunkBlocks / (units * p.n_tiles), key_tiles = (views + kChunkKeys - 1) / kChunkKeys;
+    if (cuts > kMostCuts) cuts = kMostCuts;
+    if (cuts > key_tiles / kLeastCut) cuts = key_tiles / kLeastCut;
+    p.cuts = (int)(cuts < 1 ? 1 : cuts);
+    p.columns = p.cuts > 1 ? (size_t)Tq * Hq * p.cuts : 0;
+  }
+  return p;
+}
+// keys that one query may see
+int64_t paged_most_views(int64_t max_q, int64_t max_k, int window, int sinks) {
+  if (window <= 0) return max_k;
+  const int64_t some = (int64_t)window + sinks + max_q;
+  return some < max_k ? some : max_k;
+}
+size_t paged_bytes(size_t columns, int D) { return columns ? round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2) : 0; }
+
+}  // namespace
+
+size_t paged_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
+  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, max_q, paged_most_views(max_q, max_k, window, sinks)).columns, D);
+}
+size_t paged_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q) {
+  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, max_q, (int64_t)1 << 31).columns, D);
+}
+
+hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
+  PagedArgs a = {};
+  a.c = c;
+  a.divide = page_divide(c.p.page_size);
+  a.group = c.Hq / c.p.H;
+  a.scale_log2 = c.scale * kLog2e;
+  const PagedPlan plan = paged_plan(c.Tq, c.p.B, c.Hq, c.p.H, c.max_q, paged_most_views(c.max_q, c.max_k, c.window, c.sinks));
+  a.n_tiles = (int)plan.n_tiles;
+  a.cuts = plan.cuts;
+  a.slots = (int)(plan.columns / 32);
+  a.whole_o = whole_rows(c.O);
+  if (plan.columns) {
+    a.part_o = static_cast<float*>(c.workspace);
+    a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) + round256(plan.columns * padded_head(c.p.D) * sizeof(float)));
+  }
+  const int64_t unit = c.p.e4m3 ? 16 : 8;  // elements of 16 bytes
+  const bool whole = (((uintptr_t)c.p.K | (uintptr_t)c.p.V) & 15) == 0 && (c.p.page | c.p.token | c.p.head) % unit == 0;
+  with_head(c.p.D, whole, [&](auto dp, auto is_whole) {
+    constexpr int DP = decltype(dp)::value;
+    constexpr bool WHOLE = decltype(is_whole)::value;
+    auto go = [&](auto codes) {
+      constexpr bool CODES = decltype(codes)::value;
+      if (plan.few) {
+        paged_few_kernel<DP, CODES, WHOLE><<<dim3((unsigned)plan.blocks), kThreads, 0, s>>>(a);
+        if (a.cuts) {
+          const int64_t units = (c.p.B + c.Tq * a.group / 32) * c.p.H;
+          paged_few_join_kernel<DP><<<dim3((unsigned)(units < 4096 ? units : 4096)), kThreads, 0, s>>>(a, (int)plan.blocks);
+        }
+      } else {
+        paged_chunk_kernel<DP, CODES, WHOLE><<<dim3((unsigned)tile_blocks(c.p.B, c.p.H, 1, a.n_tiles * a.cuts)), kThreads, 0, s>>>(a);
+        if (a.cuts > 1) {
+          const int64_t waves = c.max_q * c.Hq, blocks = (waves + kWaves - 1) / kWaves;
+          paged_chunk_join_kernel<DP><<<dim3((unsigned)(blocks < 1 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks - 1), (unsigned)c.p.B), kThreads, 0, s>>>(a);
+        }
+      }
+    };
+    if (c.p.e4m3) go(std::true_type{});
+    else go(std::false_type{});
+  });
+  return hipGetLastError();
+}
+
+}  // namespace nm
