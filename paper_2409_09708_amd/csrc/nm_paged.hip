@@ -10,7 +10,7 @@
 // its value is a zero and its score minus infinity.  A lane looks up the page of one row of a tile, two tiles ahead of its use, and
 // rows come through registers: 8-bit rows become bfloat16 on the way to LDS, exactly.
 //
-// Two kernels.  paged_few_kernel: 32 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
+// Two kernels.  paged_few_kernel: 16 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
 // the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
 // paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves; keys cut evenly where there are few blocks.
 #include "nm_attention.h"
@@ -27,7 +27,7 @@ struct PagedArgs {
   float scale_log2;  // scale * log2(e)
   int n_tiles;       // column tiles of a unit that the grid has
   int cuts;          // few: whether units are dealt to blocks; chunk: pieces of a unit's keys
-  float* part_o;     // few: [slot][32][DP]; chunk: [query][head][cut][DP]
+  float* part_o;     // few: [slot][16][DP]; chunk: [query][head][cut][DP]
   float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
   int slots;         // few: that the workspace holds
   bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
@@ -182,12 +182,12 @@ struct PagedTile {
 template <int ROWS>
 __device__ __forceinline__ bool seen_whole(const PagedCall& c, const Views& w, int v0, int first, int last) {
   const int from = w.key(v0), to = w.key(v0 + ROWS - 1);
-  return to <= first && (c.window <= 0 || (int64_t)from > (int64_t)last - c.window || to < c.sinks);
+  return to <= first && (c.window <= 0 || from > last - c.window || to < c.sinks);
 }
 
 // Scores that the query at position p does not see are minus infinity: rows v0 + acc_row(r) of the accumulator, `seen` from bit `bit` on.
 __device__ __forceinline__ void hide_unseen(f32x16_t& s, const PagedCall& c, const Views& w, int v0, int p, uint64_t seen, int bit) {
-  const int64_t low = c.window > 0 ? (int64_t)p - c.window : -1;
+  const int low = c.window > 0 ? p - c.window : -1;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int key = w.key(v0 + acc_row(r));
@@ -199,13 +199,175 @@ __device__ __forceinline__ void hide_unseen(f32x16_t& s, const PagedCall& c, con
 // ------------------------------------------------------------------------------------------------------
 // few queries
 // ------------------------------------------------------------------------------------------------------
+// 16 columns on the 16 x 16 x 32 instruction: lane l has, as an operand, eight elements of row (column) l % 16, and in an accumulator
+// rows 4 (l / 16) .. + 3 of column l % 16.  A wave takes 32 keys at a time, each lane the rows l % 16 and l % 16 + 16: it looks up their
+// pages, loads 16-byte pieces l / 16, l / 16 + 4, .. of their keys and values, and brings them to bfloat16 with their own powers of two,
+// with no exchange between lanes.  Pieces of keys are operands as they are: the elements of a product may come in any order that the
+// queries share.  Values go through LDS, to be read transposed.
 constexpr int kRun = 32, kStep = kWaves * kRun;  // keys of a wave, of a block, at a time
+constexpr int kCols = 16;
+
+__device__ __forceinline__ f32x4_t mma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// Values in LDS: rows of DP bfloat16, their 16-byte pieces permuted so that 16 rows at one piece (as they are written) and two pieces of
+// eight rows (as half a wave reads them) touch every bank once.
+template <int DP>
+struct ValueRun {
+  static constexpr int kRowBytes = DP * 2, kBytes = kRun * kRowBytes;
+  static __device__ __forceinline__ int swizzle(int row) {
+    return DP == 128 ? ((row & 7) << 1) | (row >> 3 & 1) : DP == 64 ? ((row >> 1 & 3) << 1) | (row >> 3 & 1) : ((row >> 2 & 1) << 1) | (row >> 3 & 1);
+  }
+  static __device__ __forceinline__ int place(int row, int piece) { return row * kRowBytes + ((piece ^ swizzle(row)) << 4); }
+  // columns 16 block .. + 15 as the first operand, rows in the order {0 .. 3, 16 .. 19} + 4 (lane / 16);  at = address + base(lane)
+  static __device__ __forceinline__ uint32_t base(int lane) { return place(lane >> 2 & 15, lane >> 1 & 1) + (lane & 1) * 8; }
+  static __device__ __forceinline__ u32x4_t columns(uint32_t at, int block) {
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    const uint32_t from = at ^ (block << 5);
+    const u32x2_t l = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(uintptr_t)from));
+    const u32x2_t h = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_ptr)(uintptr_t)(from + 16 * kRowBytes)));
+    return u32x4_t{l[0], l[1], h[0], h[1]};
+  }
+};
+
+// A wave's run of 32 keys and values, from the pages to operands.
+template <int DP, bool CODES, bool WHOLE>
+struct FewRun {
+  // elements of a load, and loads of a lane's row (codes of a row of 32: eight each)
+  static constexpr int kWide = CODES && DP >= 64 ? 16 : 8, kLoads = DP / (4 * kWide);
+  const int32_t* table;
+  Views w;
+  const unsigned char* base[2];  // of the key head
+  const uint8_t* scales[2];
+  int entry[2], slot[2];         // of the next run: the tables' entries and the slots of the lane's two rows (-1: not there)
+  u32x4_t in[2][2][kLoads];      // [keys, values][row]
+  uint32_t exponents[2];         // keys' and values', of each row
+  uint32_t seen;                 // rows of the run loaded last that are there
+
+  __device__ __forceinline__ void begin(const PagedCall& c, int seq, int head, const Views& views) {
+    w = views;
+    table = c.p.table + (int64_t)seq * c.p.width;
+    const int64_t at = (int64_t)head * c.p.head * (CODES ? 1 : 2);
+    base[0] = static_cast<const unsigned char*>(c.p.K) + at;
+    base[1] = static_cast<const unsigned char*>(c.p.V) + at;
+    if constexpr (CODES) {
+      scales[0] = c.p.K_scales + head * c.p.scale_head;
+      scales[1] = c.p.V_scales + head * c.p.scale_head;
+    }
+  }
+  __device__ __forceinline__ void look_up(const PagedArgs& a, int v0, int lane) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int v = v0 + 16 * r + (lane & 15);
+      slot[r] = entry[r] = -1;
+      if (v < w.count) {
+        const int key = w.key(v), page = page_of(a.divide, key);
+        slot[r] = key - page * a.c.p.page_size;
+        entry[r] = table[page];
+      }
+    }
+  }
+  __device__ __forceinline__ void fetch(const PagedArgs& a, int lane) {
+    const PagesCall& p = a.c.p;
+    const int group = lane >> 4;
+    seen = 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const bool there = slot[r] >= 0 && (uint32_t)entry[r] < (uint64_t)p.pages;
+      seen |= ((uint32_t)__ballot(there) & 0xFFFFu) << (16 * r);
+      exponents[r] = 0;
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) in[0][r][n] = in[1][r][n] = u32x4_t{0, 0, 0, 0};
+      if (!there) continue;
+      const int64_t at = ((int64_t)entry[r] * p.page + (int64_t)slot[r] * p.token) * (CODES ? 1 : 2);
+      if constexpr (CODES) {
+        const int64_t s = (int64_t)entry[r] * p.scale_page + (int64_t)slot[r] * p.scale_token;
+        exponents[r] = scales[0][s] | (uint32_t)scales[1][s] << 8;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          const int d = (4 * n + group) * kWide;
+          const unsigned char* row = base[t] + at;
+          if constexpr (CODES && kWide == 8) {
+            typedef uint32_t u32x2_byte_t __attribute__((ext_vector_type(2), aligned(1)));
+            if constexpr (WHOLE) {
+              const u32x2_byte_t v = *reinterpret_cast<const u32x2_byte_t*>(row + d);
+              in[t][r][n][0] = v[0];
+              in[t][r][n][1] = v[1];
+            } else {
+              const int there_d = p.D - d;
+              in[t][r][n] = load_codes(row, d, there_d < 8 ? there_d : 8);
+            }
+          } else if constexpr (CODES) {
+            if constexpr (WHOLE) in[t][r][n] = *reinterpret_cast<const u32x4_t*>(row + d);
+            else in[t][r][n] = load_codes(row, d, p.D - d);
+          } else {
+            if constexpr (WHOLE) in[t][r][n] = *reinterpret_cast<const u32x4_t*>(row + 2 * d);
+            else in[t][r][n] = load_piece(reinterpret_cast<const bf16_t*>(row), d, p.D, true);
+          }
+        }
+    }
+  }
+  // Eight elements of the keys (t 0) or values (t 1) of row r; i counts them: element(i, lane) is the first.
+  static constexpr int kPieces = DP / 32;
+  static __device__ __forceinline__ int element(int i, int lane) {
+    return kWide == 16 ? (4 * (i / 2) + (lane >> 4)) * 16 + i % 2 * 8 : (4 * i + (lane >> 4)) * 8;
+  }
+  __device__ __forceinline__ u32x4_t piece(int t, int r, int i) const {
+    if constexpr (!CODES) {
+      return in[t][r][i];
+    } else {
+      const float scale = __uint_as_float((t ? exponents[r] >> 8 : exponents[r] & 255) << 23);
+      const u32x4_t& v = in[t][r][kWide == 16 ? i / 2 : i];
+      u32x4_t out;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t codes = v[(kWide == 16 ? i % 2 * 2 : 0) + h];
+        out[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
+        out[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true));
+      }
+      return out;
+    }
+  }
+};
+
+// A column's running maximum and sum, as softmax_step has them, for 32 scores of four lanes (eight each).
+template <int NB>
+__device__ __forceinline__ void few_softmax(f32x4_t (&s)[2], float c, float& ref, float& sum, f32x4_t (&acc)[NB]) {
+  float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+  for (int r = 1; r < 4; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64)) * c;
+  if (__any(top > ref + kSlack)) {
+    const float next = fmaxf(top, ref);
+    const float by = ref == kMinusInf ? 0.f : fast_exp2(ref - next);
+    ref = next;
+    sum *= by;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[b][r] *= by;
+  }
+  const float base = ref == kMinusInf ? 0.f : ref;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[k][r] = fast_exp2(fmaf(s[k][r], c, -base));
+      sum += s[k][r];
+    }
+}
 
 // The list of all units' steps, key heads outermost, then sequences, then their column tiles; every tile of a sequence has as many steps.
-// 64 sequences at a time: a lane has one's steps and tiles, and their running sums.
+// 64 sequences at a time: a lane has one's queries and tokens, its steps and tiles, and their running sums.
 struct Units {
   int b0;             // first sequence of those at hand
-  int steps, tiles;   // of the lane's sequence
+  PagedSequence of;
+  int steps, tiles;
   int64_t upto;       // steps of all tiles, up to the lane's sequence and with it
   int tiles_upto;
 };
@@ -217,18 +379,18 @@ __device__ __forceinline__ void few_units(const PagedArgs& a, int b0, Units* u) 
   u->b0 = b0;
   u->steps = u->tiles = 0;
   if (b < a.c.p.B) {
-    const int each = (int)(a.c.Tq / a.c.p.B);
-    PagedSequence of = {b * each, each, page_clamped(a.c.p, a.c.p.lengths[b])};
+    const int each = (int)(a.c.Tq / a.c.p.B), Tq = (int)a.c.Tq;
+    int q0 = b * each, q1 = q0 + each;
     if (a.c.offsets_q != nullptr) {
-      const int Tq = (int)a.c.Tq;
-      int q0 = a.c.offsets_q[b], q1 = a.c.offsets_q[b + 1];
-      q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
-      q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
-      of.len = q1 - q0;
+      q0 = a.c.offsets_q[b];
+      q1 = a.c.offsets_q[b + 1];
     }
-    const int steps = (few_views(a.c, of).count + kStep - 1) / kStep;
+    q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
+    q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
+    u->of = {q0, q1 - q0, page_clamped(a.c.p, a.c.p.lengths[b])};
+    const int steps = (few_views(a.c, u->of).count + kStep - 1) / kStep;
     u->steps = steps > 0 ? steps : 1;
-    u->tiles = (of.len * a.group + 31) / 32;
+    u->tiles = (u->of.len * a.group + kCols - 1) / kCols;
   }
   u->upto = (int64_t)u->steps * u->tiles;
   u->tiles_upto = u->tiles;
@@ -261,6 +423,7 @@ struct UnitPlace {
   int seq, tile, step, steps;  // a tile of `steps` steps, `step` of which are before this one
   int unit;                    // tiles before it
   int64_t begin;               // steps before its first
+  PagedSequence of;
 };
 template <bool BY_TILE>
 __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int64_t at) {
@@ -273,14 +436,15 @@ __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int
     const bool here = BY_TILE ? at < tiles_before + all_tiles : at < steps_before + all;
     if (here || b0 + 64 >= a.c.p.B) {
       const uint64_t above = BY_TILE ? __ballot((int64_t)tiles_before + u->tiles_upto > at) : __ballot(steps_before + u->upto > at);
-      const int l = above ? __ffsll((unsigned long long)above) - 1 : 63;
+      const int l = above ? __ffsll((unsigned long long)above) - 1 : 0;
       UnitPlace p;
-      p.seq = b0 + l < a.c.p.B ? b0 + l : a.c.p.B - 1;
+      p.seq = b0 + l;
+      p.of = {__builtin_amdgcn_readlane(u->of.q0, l), __builtin_amdgcn_readlane(u->of.len, l), __builtin_amdgcn_readlane(u->of.n, l)};
       p.steps = __builtin_amdgcn_readlane(u->steps, l);
       const int tiles = __builtin_amdgcn_readlane(u->tiles, l);
       const int64_t first = steps_before + lane_value(u->upto, l) - (int64_t)p.steps * tiles;
       const int first_tile = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles;
-      p.tile = BY_TILE ? (int)(at - first_tile) : (int)((at - first) / (p.steps > 0 ? p.steps : 1));
+      p.tile = BY_TILE ? (int)(at - first_tile) : tiles == 1 ? 0 : (int)((at - first) / p.steps);
       p.begin = first + (int64_t)p.tile * p.steps;
       p.step = BY_TILE ? 0 : (int)(at - p.begin);
       p.unit = first_tile + p.tile;
@@ -298,17 +462,20 @@ __device__ __forceinline__ int64_t few_share(int64_t all, int blocks) {
 
 template <int DP, bool CODES, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs a) {
-  using Tile = RowTile<DP>;
-  using Load = PagedTile<DP, kRun, CODES, WHOLE, 64>;
-  constexpr int NB = DP / 32, STEPS = DP / 16;
-  constexpr int JOIN = 32 * (DP + 4) * 4;  // one wave's output, columns padded against bank conflicts
-  constexpr int OWN = 2 * Load::kBytes;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * (OWN > JOIN ? OWN : JOIN)];
-  __shared__ float2 wave_ml[kWaves][32];
+  using Load = FewRun<DP, CODES, WHOLE>;
+  using Value = ValueRun<DP>;
+  constexpr int NB = DP / 16, STEPS = DP / 32;
+  constexpr int JOIN = kCols * (DP + 4) * 4;  // one wave's output, columns padded against bank conflicts
+  constexpr int OWN = Value::kBytes > JOIN ? Value::kBytes : JOIN;
+  static_assert(OWN % 256 == 0, "operand addresses change bits below 256");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kWaves * OWN];
+  __shared__ float2 wave_ml[kWaves][kCols];
   const PagedCall& c = a.c;
   const int D = WHOLE ? DP : c.p.D;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, col = lane & 31;
+  const int quarter = lane >> 4, col = lane & 15;
+  unsigned char* own = smem + wave * OWN;
+  const uint32_t v_at = NM_LDS_ADDRESS(smem) + wave * OWN + Value::base(lane);
   // this block's run of the list of steps -- or, uncut, every (gridDim.x)-th of the units that the grid was made for
   Units units;
   units.b0 = -1;
@@ -324,12 +491,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
     end = (int64_t)c.p.B * c.p.H * a.n_tiles;
   }
   while (at < end) {
-    int seq, kv_head, tile, step, steps, slot = 0;
+    int seq, kv_head, tile, step = 0, steps = 0, slot = 0;
     bool alone = true;  // the whole unit is this block's
+    PagedSequence of;
     if (a.cuts) {
-      kv_head = (int)(at / per_head);
+      kv_head = (int)((uint64_t)at / (uint64_t)per_head);
       const UnitPlace p = few_place<false>(a, &units, at - kv_head * per_head);
-      seq = p.seq; tile = p.tile; step = p.step;
+      seq = p.seq; tile = p.tile; step = p.step; of = p.of;
       steps = (int)(end - at < p.steps - step ? end - at : p.steps - step);
       alone = steps == p.steps;
       slot = kv_head * tiles_per_head + p.unit + (int)blockIdx.x;  // (each further unit, and each further block, is one more)
@@ -338,69 +506,74 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       seq = (int)(at / (c.p.H * a.n_tiles));
       kv_head = (int)(at / a.n_tiles % c.p.H);
       tile = (int)(at % a.n_tiles);
-      step = steps = 0;
       at += gridDim.x;
+      of = paged_sequence(c, seq);
     }
-    const PagedSequence of = paged_sequence(c, seq);
     const Views views = few_views(c, of);
     const int last_view = a.cuts && (step + steps) * kStep < views.count ? (step + steps) * kStep : views.count;
     Load load;
-    load.begin(a, seq, kv_head, views, smem + wave * OWN);
+    load.begin(c, seq, kv_head, views);
     const int columns = of.len * a.group;
     // (a sequence of more queries than the grid was made for has further tiles)
-    for (; tile * 32 < columns; tile += a.n_tiles) {
-      const int n = tile * 32 + col;
+    for (; tile * kCols < columns; tile += a.n_tiles) {
+      int v0 = step * kStep + wave * kRun;
+      load.look_up(a, v0, lane);
+      const int n = tile * kCols + col;
       const bool live = n < columns;
       const int qi = n / a.group, head = kv_head * a.group + n % a.group;
       const int first = of.n - of.len, p = first + qi;  // positions
-      const int least_p = first + tile * 32 / a.group, most_p = first + (tile * 32 + 31 < columns ? tile * 32 + 31 : columns - 1) / a.group;
+      const int least_p = first + tile * kCols / a.group, most_p = first + (tile * kCols + kCols - 1 < columns ? tile * kCols + kCols - 1 : columns - 1) / a.group;
       const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
-      __syncthreads();  // (what the waves joined last has been read)
-      int v0 = step * kStep + wave * kRun;
-      load.look_up(v0);
       u32x4_t q[STEPS];
 #pragma unroll
-      for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+      for (int i = 0; i < STEPS; ++i) q[i] = load_piece(q_row, Load::element(i, lane), D, live);
       if (v0 < last_view) {
-        load.fetch();
-        load.look_up(v0 + kStep);
+        load.fetch(a, lane);
+        load.look_up(a, v0 + kStep, lane);
       }
-      f32x16_t acc[NB];
+      f32x4_t acc[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+      for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       float ref = kMinusInf, sum = 0.f;
+      __syncthreads();  // (what the waves joined last has been read)
       for (; v0 < last_view; v0 += kStep) {
-        const uint64_t seen = load.seen;
-        load.settle(0);
+        const uint32_t seen = load.seen;
+        f32x4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) s[r] = mma16(load.piece(0, r, i), q[i], s[r]);
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int i = 0; i < Load::kPieces; ++i)
+            *reinterpret_cast<u32x4_t*>(own + Value::place(16 * r + col, Load::element(i, lane) / 8)) = load.piece(1, r, i);
         if (v0 + kStep < last_view) {
-          load.fetch();
-          load.look_up(v0 + 2 * kStep);
+          load.fetch(a, lane);
+          load.look_up(a, v0 + 2 * kStep, lane);
         }
         __builtin_amdgcn_wave_barrier();
-        const uint32_t k_tile = NM_LDS_ADDRESS(smem) + wave * OWN;
-        const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = k_tile + Load::kBytes + Tile::column_base(lane);
-        constexpr int NV = kRun / 16 * NB;
-        auto keys = [&](int i) { return Tile::rows(k_at, 0, i); };
-        auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
-        f32x16_t s[1];
+        if (seen != 0xFFFFFFFFu || !seen_whole<kRun>(c, views, v0, least_p, most_p)) {
+          const int low = c.window > 0 ? p - c.window : -1;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
-        u32x4_t f[kAhead];
-        read_ahead<STEPS>(f, keys);
-        products<STEPS>(f, keys, [&](int i, u32x4_t k) { s[0] = mma32(k, q[i], s[0]); });
-        read_ahead<NV>(f, values);
-        if ((uint32_t)seen != 0xFFFFFFFFu || !seen_whole<kRun>(c, views, v0, least_p, most_p))
-          hide_unseen(s[0], c, views, v0 + 4 * half, p, seen, 4 * half);
-        softmax_step(s, a.scale_log2, ref, sum, acc);
-        const u32x4_t pr[2] = {acc_operand(s[0], 0), acc_operand(s[0], 1)};
-        products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int row = 16 * k + 4 * quarter + r, key = views.key(v0 + row);
+              const bool sees = key <= p && (key > low || key < c.sinks) && (seen >> row & 1);
+              s[k][r] = sees ? s[k][r] : kMinusInf;
+            }
+        }
+        few_softmax(s, a.scale_log2, ref, sum, acc);
+        const u32x4_t pr = {pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])};
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = mma16(Value::columns(v_at, b), pr, acc[b]);
         __builtin_amdgcn_wave_barrier();
       }
       // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
-      sum = half_sum(sum);
-      if (half == 0) wave_ml[wave][col] = float2{ref, sum};
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      if (quarter == 0) wave_ml[wave][col] = float2{ref, sum};
       __syncthreads();
       float top = kMinusInf, total = 0.f;
 #pragma unroll
@@ -408,26 +581,23 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) total += wave_ml[w][col].y * part_weight(wave_ml[w][col].x, top);
       const float by = part_weight(ref, top);
-      float* joined = reinterpret_cast<float*>(smem) + wave * 32 * (DP + 4);
+      float* joined = reinterpret_cast<float*>(own);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<float4*>(joined + col * (DP + 4) + 32 * b + acc_row(r) + 4 * half) =
-              float4{acc[b][r] * by, acc[b][r + 1] * by, acc[b][r + 2] * by, acc[b][r + 3] * by};
+        *reinterpret_cast<float4*>(joined + col * (DP + 4) + 16 * b + 4 * quarter) = float4{acc[b][0] * by, acc[b][1] * by, acc[b][2] * by, acc[b][3] * by};
       __syncthreads();
       // lane -> (column, four elements)
       constexpr int PER_COL = DP / 4;
 #pragma unroll
-      for (int i = 0; i < 32 * PER_COL / kThreads; ++i) {
+      for (int i = 0; i < (kCols * PER_COL + kThreads - 1) / kThreads; ++i) {
         const int to = i * kThreads + tid, cc = to / PER_COL, d = to % PER_COL * 4;
-        const int cn = tile * 32 + cc;
-        if (cn >= columns || d >= D) continue;
+        const int cn = tile * kCols + cc;
+        if (cc >= kCols || cn >= columns || d >= D) continue;
         const float* from = reinterpret_cast<const float*>(smem) + cc * (DP + 4) + d;
         float4 o = *reinterpret_cast<const float4*>(from);
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) {
-          const float4 x = *reinterpret_cast<const float4*>(from + w * 32 * (DP + 4));
+          const float4 x = *reinterpret_cast<const float4*>(from + w * (OWN / 4));
           o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
         }
         if (alone) {
@@ -441,14 +611,15 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
           const float inv = l == 0.f ? 0.f : 1.f / l;
           store4(c.O.p + tok * c.O.token + hd * c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
         } else if (slot < a.slots) {  // (always, of offsets that do not decrease)
-          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * 32 + cc) * DP + d) = o;
+          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kCols + cc) * DP + d) = o;
         }
       }
-      if (wave == 0 && half == 0 && live) {
+      if (wave == 0 && quarter == 0 && live) {
         if (!alone) {
-          if (slot < a.slots) a.part_ml[(int64_t)slot * 32 + col] = float2{top, total};
-        } else if (c.lse != nullptr)
+          if (slot < a.slots) a.part_ml[(int64_t)slot * kCols + col] = float2{top, total};
+        } else if (c.lse != nullptr) {
           c.lse[(int64_t)head * c.Tq + of.q0 + qi] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
+        }
       }
       if (a.cuts) break;
     }
@@ -489,7 +660,7 @@ __device__ __forceinline__ void join_parts(const PagedCall& c, const float* part
   if (c.lse != nullptr && lane == 0) c.lse[(int64_t)head * c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
 }
 
-// A block takes units in turn, a wave a unit's columns; units that one block of the first launch had whole are done.
+// A block takes units in turn, a wave a column of one (and further ones, of sequences with more queries than the grid was made for); units that one block of the first launch had whole are done.
 template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a, int blocks) {
   const PagedCall& c = a.c;
@@ -502,14 +673,12 @@ __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArg
     const int kv_head = (int)(i / tiles_per_head);
     const UnitPlace p = few_place<true>(a, &units, i - (int64_t)kv_head * tiles_per_head);
     const int64_t begin = kv_head * per_head + p.begin;
-    const int64_t from = begin / share, to = (begin + p.steps - 1) / share;
-    const int64_t slot = i + from;
+    const int64_t from = begin / share, to = (begin + p.steps - 1) / share, slot = i + from;
     if (from == to || slot + (to - from) >= a.slots) continue;
-    const PagedSequence of = paged_sequence(c, p.seq);
-    const int columns = of.len * a.group;
-    for (int col = threadIdx.x >> 6; col < 32 && p.tile * 32 + col < columns; col += kWaves) {
-      const int n = p.tile * 32 + col;
-      join_parts<DP>(c, a.part_o + (slot * 32 + col) * DP, a.part_ml + slot * 32 + col, 32, (int)(to - from + 1), of.q0 + n / a.group,
+    const int columns = p.of.len * a.group - p.tile * kCols;
+    for (int col = blockIdx.y * kWaves + (threadIdx.x >> 6); col < kCols && col < columns; col += gridDim.y * kWaves) {
+      const int n = p.tile * kCols + col;
+      join_parts<DP>(c, a.part_o + (slot * kCols + col) * DP, a.part_ml + slot * kCols + col, kCols, (int)(to - from + 1), p.of.q0 + n / a.group,
                      kv_head * a.group + n % a.group);
     }
   }
@@ -571,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
       }
       // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
       const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
-      if (c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= (int64_t)least_p - c.window && k_first >= c.sinks)) continue;
+      if (c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= least_p - c.window && k_first >= c.sinks)) continue;
       const uint32_t k_tile = NM_LDS_ADDRESS(smem[0]) + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
       const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
       constexpr int KB = kChunkKeys / 32, NS = KB * STEPS, NV = kChunkKeys / 16 * NB;
@@ -654,14 +823,14 @@ PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int64_t max_q, int64_t 
   PagedPlan p = {};
   const int64_t group = Hq / Hkv, units = (int64_t)B * Hkv;
   p.few = max_q * group <= kFewColumns;
-  const int64_t per_tile = p.few ? 32 : kChunkColumns;
+  const int64_t per_tile = p.few ? kCols : kChunkColumns;
   p.n_tiles = (max_q * group + per_tile - 1) / per_tile;
   if (p.n_tiles < 1) p.n_tiles = 1;
   if (p.few) {
-    const int64_t tiles = B + Tq * group / 32;  // at most
+    const int64_t tiles = B + Tq * group / kCols;  // at most
     p.cuts = B <= kFewSequences && tiles <= kFewTiles && views > kUncutKeys;
     p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
-    p.columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * 32 : 0;
+    p.columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
   } else {
     while (tile_blocks(B, Hkv, 1, (int)p.n_tiles) >= kMostBlocks) p.n_tiles = (p.n_tiles + 1) / 2;  // (blocks take several then)
     int64_t cuts = kChunkBlocks / (units * p.n_tiles), key_tiles = (views + kChunkKeys - 1) / kChunkKeys;
@@ -698,7 +867,7 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   const PagedPlan plan = paged_plan(c.Tq, c.p.B, c.Hq, c.p.H, c.max_q, paged_most_views(c.max_q, c.max_k, c.window, c.sinks));
   a.n_tiles = (int)plan.n_tiles;
   a.cuts = plan.cuts;
-  a.slots = (int)(plan.columns / 32);
+  a.slots = (int)(plan.columns / kCols);
   a.whole_o = whole_rows(c.O);
   if (plan.columns) {
     a.part_o = static_cast<float*>(c.workspace);
@@ -714,8 +883,9 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
       if (plan.few) {
         paged_few_kernel<DP, CODES, WHOLE><<<dim3((unsigned)plan.blocks), kThreads, 0, s>>>(a);
         if (a.cuts) {
-          const int64_t units = (c.p.B + c.Tq * a.group / 32) * c.p.H;
-          paged_few_join_kernel<DP><<<dim3((unsigned)(units < 4096 ? units : 4096)), kThreads, 0, s>>>(a, (int)plan.blocks);
+          const int64_t units = (c.p.B + c.Tq * a.group / kCols) * c.p.H, columns = c.max_q * a.group < kCols ? c.max_q * a.group : kCols;
+          const dim3 join((unsigned)(units < 4096 ? units : 4096), (unsigned)(columns > kWaves ? (columns + kWaves - 1) / kWaves : 1));
+          paged_few_join_kernel<DP><<<join, kThreads, 0, s>>>(a, (int)plan.blocks);
         }
       } else {
         paged_chunk_kernel<DP, CODES, WHOLE><<<dim3((unsigned)tile_blocks(c.p.B, c.p.H, 1, a.n_tiles * a.cuts)), kThreads, 0, s>>>(a);
