@@ -8,7 +8,7 @@
 // that all of them share the keys that are read.  The keys that any query of a run can see are numbered without the gap between sinks and
 // window ("views"), so tiles hold no keys that nobody sees, and what is masked, past the end or on a page that is not there is never read:
 // its value is a zero and its score minus infinity.  A lane looks up the page of one row of a tile, two tiles ahead of its use, and
-// rows come through registers: 8-bit rows become bfloat16 on the way to LDS, exactly.
+// 8-bit rows become bfloat16 on the way, exactly.
 //
 // Two kernels.  paged_few_kernel: 16 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
 // the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
@@ -68,109 +68,138 @@ __device__ __forceinline__ Views paged_views(const PagedCall& c, int first, int 
   return {sinks_a, from_a - sinks_a, sinks_a + end - from_a, sinks, from};
 }
 
-// Rows of a tile as one lane knows them: lane r (< ROWS) has row r's place in a page, or that it is not there.
-struct RowPlaces {
-  int entry, slot;  // of the next tile: the table's entry, and the slot in its page (-1: not there)
-  __device__ __forceinline__ void look_up(const PagedArgs& a, const int32_t* table, const Views& w, int v, bool in_tile) {
-    const int key = w.key(v);
-    slot = -1;
-    entry = -1;
-    if (in_tile && v < w.count && (key < w.hidden_from || key >= w.hidden_to)) {
+// How a block's tiles come: asynchronous copies straight to LDS (bfloat16 rows of exactly DP elements, 16-byte aligned, in pages that
+// hold whole runs of the rows that a wave's copy brings), or through registers, bfloat16 or codes, whole rows or any.
+enum { kPagedDirect, kPagedBf16, kPagedCodes, kPagedAnyBf16, kPagedAnyCodes };
+constexpr int copy_rows(int DP) { return 512 / DP; }  // that a wave's copy of a kilobyte brings
+
+// A block's tile of 64 keys and values in LDS, as bfloat16.
+//   look_up(v0)    starts the look-up of the pages of views v0 .. (every wave for itself)
+//   fetch(stage)   starts the loads of the tile looked up last
+//   settle(stage)  the rows that this wave brings are in LDS, zeros for those that are not there (of the values, where copies are
+//                  direct: scores of such keys have to be hidden anyway); a block's barrier follows
+//   seen           the rows of the tile fetched last that are there, a bit each
+constexpr int kChunkKeys = 64, kChunkColumns = kWaves * 32;
+template <int DP, int HOW>
+struct ChunkTile {
+  using Tile = RowTile<DP>;
+  static constexpr bool CODES = HOW == kPagedCodes || HOW == kPagedAnyCodes, DIRECT = HOW == kPagedDirect;
+  static constexpr int kBytes = kChunkKeys * Tile::kRowBytes;
+  static constexpr int kPer = CODES ? DP / 16 : DP / 8, kPieces = kChunkKeys * kPer;  // 16-byte pieces as they come
+  static constexpr int kLoads = (kPieces + kThreads - 1) / kThreads;
+  const int32_t* table;
+  Views w;
+  const unsigned char* base[2];  // of the key head
+  const uint8_t* scales[2];
+  unsigned char* smem;           // stages of 2 * kBytes
+  uint32_t lds;                  // its address
+  int entry, slot;               // lane r: row r of the next tile, its table's entry and the slot in its page (-1: not there)
+  bool shown;                    // ... and whether any query sees it
+  u32x4_t in[DIRECT ? 1 : 2][DIRECT ? 1 : kLoads];
+  uint32_t exponents;            // lane r: those of row r's keys and values
+  uint64_t seen;
+
+  __device__ __forceinline__ void begin(const PagedCall& c, int seq, int head, const Views& views) {
+    w = views;
+    table = c.p.table + (int64_t)seq * c.p.width;
+    const int64_t at = (int64_t)head * c.p.head * (CODES ? 1 : 2);
+    base[0] = static_cast<const unsigned char*>(c.p.K) + at;
+    base[1] = static_cast<const unsigned char*>(c.p.V) + at;
+    if constexpr (CODES) {
+      scales[0] = c.p.K_scales + head * c.p.scale_head;
+      scales[1] = c.p.V_scales + head * c.p.scale_head;
+    }
+  }
+  __device__ __forceinline__ void look_up(const PagedArgs& a, int v0) {
+    const int v = v0 + (threadIdx.x & 63), key = w.key(v);
+    slot = entry = -1;
+    shown = key < w.hidden_from || key >= w.hidden_to;
+    if (v < w.count && (DIRECT || shown)) {  // (a copy's rows lie on one page, whose place the first of them gives)
       const int page = page_of(a.divide, key);
       slot = key - page * a.c.p.page_size;
       entry = table[page];
     }
   }
-};
-
-// A tile of ROWS rows of keys and of values, by LANES lanes (a wave or a block), through registers to LDS as bfloat16.  They come as
-// bfloat16 or as CODES, of exactly DP elements in 16-byte aligned rows (WHOLE) or any.
-//   look_up(v0)   starts the look-up of the pages of views v0 ..
-//   fetch()       starts the loads of the tile looked up last
-//   settle(stage) rows to LDS, zeros for those that are not there (a block's barrier follows)
-//   seen          the rows of the tile fetched last that are there, a bit each
-template <int DP, int ROWS, bool CODES, bool WHOLE, int LANES>
-struct PagedTile {
-  using Tile = RowTile<DP>;
-  static constexpr int kBytes = ROWS * Tile::kRowBytes;
-  static constexpr int kPer = CODES ? DP / 16 : DP / 8, kPieces = ROWS * kPer;  // 16-byte pieces as they come
-  static constexpr int kLoads = (kPieces + LANES - 1) / LANES;
-  const PagedArgs* a;
-  const int32_t* table;
-  Views w;
-  const unsigned char* base[2];
-  const uint8_t* scales[2];
-  unsigned char* smem;  // stages of 2 * kBytes
-  RowPlaces next;
-  u32x4_t in[2][kLoads];
-  uint32_t exponents;  // lane r: those of row r's keys and values
-  uint64_t seen;
-
-  __device__ __forceinline__ void begin(const PagedArgs& args, int seq, int head, const Views& views, unsigned char* lds) {
-    a = &args;
-    w = views;
-    smem = lds;
-    const PagesCall& p = args.c.p;
-    table = p.table + (int64_t)seq * p.width;
-    const int64_t at = (int64_t)head * p.head * (CODES ? 1 : 2);
-    base[0] = static_cast<const unsigned char*>(p.K) + at;
-    base[1] = static_cast<const unsigned char*>(p.V) + at;
-    if constexpr (CODES) {
-      scales[0] = p.K_scales + head * p.scale_head;
-      scales[1] = p.V_scales + head * p.scale_head;
-    }
-  }
-  __device__ __forceinline__ void look_up(int v0) {
-    const int lane = threadIdx.x & 63;
-    next.look_up(*a, table, w, v0 + lane, lane < ROWS);
-  }
-  __device__ __forceinline__ void fetch() {
-    const PagesCall& p = a->c.p;
-    const int tid = threadIdx.x % LANES;
-    const bool there = next.slot >= 0 && (uint32_t)next.entry < (uint64_t)p.pages;
-    seen = __ballot(there);
-    const int64_t at = there ? (int64_t)next.entry * p.page + (int64_t)next.slot * p.token : 0;
-    const int lo = (int)(uint32_t)at, hi = (int)(at >> 32);
-    if constexpr (CODES) {
-      exponents = 0;
-      if (there) {
-        const int64_t s = (int64_t)next.entry * p.scale_page + (int64_t)next.slot * p.scale_token;
-        exponents = scales[0][s] | (uint32_t)scales[1][s] << 8;
+  __device__ __forceinline__ void fetch(const PagedArgs& a, int stage) {
+    const PagesCall& p = a.c.p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool there = slot >= 0 && (uint32_t)entry < (uint64_t)p.pages;
+    seen = __ballot(there && shown);
+    if constexpr (DIRECT) {
+      // (rows that are not there: others of the same page, or of the first)
+      const int known = there ? entry : -1;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (uint32_t)stage * 2 * kBytes);
+      constexpr int ROWS = copy_rows(DP), PIECES = Tile::kPieces;
+      const int row = lane / PIECES;
+      const uint32_t from_lane = (uint32_t)row * (uint32_t)p.token * 2 + ((lane % PIECES) ^ Tile::swizzle(wave * ROWS + row)) * 16;
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) {
+        if (kPieces % kThreads != 0 && wave * 64 >= kPieces) break;
+        const int row0 = (n * kWaves + wave) * ROWS;
+        int page = __builtin_amdgcn_readlane(known, row0), in_page = __builtin_amdgcn_readlane(slot, row0);
+        if (page < 0) page = in_page = 0;
+        const int64_t at = ((int64_t)page * p.page + (int64_t)in_page * p.token) * 2;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          dma16(make_uniform(base[t] + at), from_lane, to + t * kBytes + (n * kWaves + wave) * 1024);
       }
-    }
+    } else {
+      const int64_t at = there ? (int64_t)entry * p.page + (int64_t)slot * p.token : 0;
+      const int lo = (int)(uint32_t)at, hi = (int)(at >> 32);
+      if constexpr (CODES) {
+        exponents = 0;
+        if (there) {
+          const int64_t s = (int64_t)entry * p.scale_page + (int64_t)slot * p.scale_token;
+          exponents = scales[0][s] | (uint32_t)scales[1][s] << 8;
+        }
+      }
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int i = n * LANES + tid, row = i / kPer, piece = i % kPer;
-      const int src = row < 64 ? row : 0;
-      const int64_t from = ((int64_t)__shfl(hi, src, 64) << 32 | (uint32_t)__shfl(lo, src, 64)) * (CODES ? 1 : 2) + piece * 16;
-      const bool live = (kPieces % LANES == 0 || i < kPieces) && (seen >> src & 1);
+      for (int n = 0; n < kLoads; ++n) {
+        const int i = n * kThreads + tid, piece = i % kPer, row = kPieces % kThreads == 0 ? i / kPer : i / kPer & 63;
+        const int64_t from = ((int64_t)__shfl(hi, row, 64) << 32 | (uint32_t)__shfl(lo, row, 64)) * (CODES ? 1 : 2) + piece * 16;
+        const bool live = (kPieces % kThreads == 0 || i < kPieces) && (seen >> row & 1);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        in[t][n] = u32x4_t{0, 0, 0, 0};
-        if (!live) continue;
-        if constexpr (WHOLE) in[t][n] = *reinterpret_cast<const u32x4_t*>(base[t] + from);
-        else if constexpr (CODES) in[t][n] = load_codes(base[t] + from, 0, a->c.p.D - piece * 16);
-        else in[t][n] = load_piece(reinterpret_cast<const bf16_t*>(base[t] + from), 0, a->c.p.D - piece * 8, true);
+        for (int t = 0; t < 2; ++t) {
+          in[t][n] = u32x4_t{0, 0, 0, 0};
+          if (!live) continue;
+          if constexpr (HOW == kPagedAnyCodes) in[t][n] = load_codes(base[t] + from, 0, p.D - piece * 16);
+          else if constexpr (HOW == kPagedAnyBf16) in[t][n] = load_piece(reinterpret_cast<const bf16_t*>(base[t] + from), 0, p.D - piece * 8, true);
+          else in[t][n] = *reinterpret_cast<const u32x4_t*>(base[t] + from);
+        }
       }
     }
   }
   __device__ __forceinline__ void settle(int stage) {
-    const int tid = threadIdx.x % LANES;
+    if constexpr (DIRECT) {
+      wait_loads_outstanding<0>();
+      if (seen == ~0ull) return;
+      int tid = threadIdx.x;
+      uint32_t zero = 0;
+      asm volatile("" : "+v"(tid), "+v"(zero));  // (computed here, in a few tiles: held over the loop it would cost registers)
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int i = n * LANES + tid, row = i / kPer, piece = i % kPer;
-      const uint32_t e = CODES ? (uint32_t)__shfl((int)exponents, row < 64 ? row : 0, 64) : 0;
-      if (kPieces % LANES == 0 || i < kPieces) {
+      for (int n = 0; n < kLoads; ++n) {
+        const int i = n * kThreads + tid;  // the piece that this lane's copy brought
+        if ((kPieces % kThreads == 0 || i < kPieces) && !(seen >> (i / Tile::kPieces) & 1))
+          *(lds_u32x4_out_ptr)(uintptr_t)(lds + (2 * stage + 1) * kBytes + i * 16) = u32x4_t{zero, zero, zero, zero};
+      }
+    } else {
+      const int tid = threadIdx.x;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          unsigned char* to = smem + (2 * stage + t) * kBytes;
-          if constexpr (CODES) {
-            u32x4_t v[2];
-            decode16(in[t][n], t ? e >> 8 : e & 255, v);
-            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece)) = v[0];
-            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece + 1)) = v[1];
-          } else {
-            *reinterpret_cast<u32x4_t*>(to + Tile::place(row, piece)) = in[t][n];
+      for (int n = 0; n < kLoads; ++n) {
+        const int i = n * kThreads + tid, piece = i % kPer, row = kPieces % kThreads == 0 ? i / kPer : i / kPer & 63;
+        const uint32_t e = CODES ? (uint32_t)__shfl((int)exponents, row, 64) : 0;
+        if (kPieces % kThreads == 0 || i < kPieces) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            unsigned char* to = smem + (2 * stage + t) * kBytes;
+            if constexpr (CODES) {
+              u32x4_t v[2];
+              decode16(in[t][n], t ? e >> 8 : e & 255, v);
+              *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece)) = v[0];
+              *reinterpret_cast<u32x4_t*>(to + Tile::place(row, 2 * piece + 1)) = v[1];
+            } else {
+              *reinterpret_cast<u32x4_t*>(to + Tile::place(row, piece)) = in[t][n];
+            }
           }
         }
       }
@@ -185,16 +214,16 @@ __device__ __forceinline__ bool seen_whole(const PagedCall& c, const Views& w, i
   return to <= first && (c.window <= 0 || from > last - c.window || to < c.sinks);
 }
 
-// Scores that the query at position p does not see are minus infinity: rows v0 + acc_row(r) of the accumulator, `seen` from bit `bit` on.
-__device__ __forceinline__ void hide_unseen(f32x16_t& s, const PagedCall& c, const Views& w, int v0, int p, uint64_t seen, int bit) {
-  const int low = c.window > 0 ? p - c.window : -1;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int key = w.key(v0 + acc_row(r));
-    const bool sees = key <= p && (key > low || key < c.sinks) && (seen >> (bit + acc_row(r)) & 1);
-    s[r] = sees ? s[r] : kMinusInf;
+// Which keys the query at position p sees, in two comparisons: key - from < count (unsigned), or key < sinks.
+struct Sight {
+  int from, count, sinks;
+  __device__ __forceinline__ Sight(const PagedCall& c, int p) {
+    from = c.window > 0 && p - c.window + 1 > 0 ? p - c.window + 1 : 0;
+    count = p + 1 - from > 0 ? p + 1 - from : 0;
+    sinks = c.sinks < p + 1 ? c.sinks : p + 1;
   }
-}
+  __device__ __forceinline__ bool sees(int key) const { return (uint32_t)(key - from) < (uint32_t)count || key < sinks; }
+};
 
 // ------------------------------------------------------------------------------------------------------
 // few queries
@@ -554,14 +583,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
         }
         __builtin_amdgcn_wave_barrier();
         if (seen != 0xFFFFFFFFu || !seen_whole<kRun>(c, views, v0, least_p, most_p)) {
-          const int low = c.window > 0 ? p - c.window : -1;
+          const Sight sight(c, p);
 #pragma unroll
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const int row = 16 * k + 4 * quarter + r, key = views.key(v0 + row);
-              const bool sees = key <= p && (key > low || key < c.sinks) && (seen >> row & 1);
-              s[k][r] = sees ? s[k][r] : kMinusInf;
+              const int row = 16 * k + 4 * quarter + r;
+              s[k][r] = sight.sees(views.key(v0 + row)) && (seen >> row & 1) ? s[k][r] : kMinusInf;
             }
         }
         few_softmax(s, a.scale_log2, ref, sum, acc);
@@ -687,12 +715,11 @@ __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArg
 // ------------------------------------------------------------------------------------------------------
 // chunks of queries
 // ------------------------------------------------------------------------------------------------------
-constexpr int kChunkKeys = 64, kChunkColumns = kWaves * 32;
-
-template <int DP, bool CODES, bool WHOLE>
+template <int DP, int HOW>
 __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArgs a) {
   using Tile = RowTile<DP>;
-  using Load = PagedTile<DP, kChunkKeys, CODES, WHOLE, kThreads>;
+  using Load = ChunkTile<DP, HOW>;
+  constexpr bool WHOLE = HOW <= kPagedCodes;
   constexpr int NB = DP / 32, STEPS = DP / 16;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * Load::kBytes];
   const PagedCall& c = a.c;
@@ -714,15 +741,18 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
     const int all = (views.count + kChunkKeys - 1) / kChunkKeys;
     const int from = (int)((int64_t)all * cut / a.cuts), to = (int)((int64_t)all * (cut + 1) / a.cuts);
     Load load;
-    load.begin(a, seq, kv_head, views, smem[0]);
+    load.begin(c, seq, kv_head, views);
+    load.smem = smem[0];
+    load.lds = NM_LDS_ADDRESS(smem[0]);
     __syncthreads();  // (a block's second tile: the first one's keys are no longer read)
-    load.look_up(from * kChunkKeys);
+    load.look_up(a, from * kChunkKeys);
     u32x4_t q[STEPS];
     const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-    if (from < to) load.fetch();
-    load.look_up((from + 1) * kChunkKeys);
+    if (from < to) load.fetch(a, 0);
+    load.look_up(a, (from + 1) * kChunkKeys);
+    if constexpr (Load::DIRECT) arrived(q);
     f32x16_t acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -731,12 +761,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
     float ref = kMinusInf, sum = 0.f;
     for (int kt = from; kt < to; ++kt) {
       const int stage = (kt - from) & 1, v0 = kt * kChunkKeys;
-      const uint64_t seen = load.seen;
       load.settle(stage);
+      const uint64_t seen = load.seen;
       __syncthreads();
       if (kt + 1 < to) {
-        load.fetch();
-        load.look_up(v0 + 2 * kChunkKeys);
+        load.fetch(a, stage ^ 1);
+        load.look_up(a, v0 + 2 * kChunkKeys);
       }
       // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
       const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
@@ -757,8 +787,17 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
       products<NS>(f, keys, [&](int i, u32x4_t k) { s[i % KB] = mma32(k, q[i / KB], s[i % KB]); });
       read_ahead<NV>(f, values);
       if (seen != ~0ull || !seen_whole<kChunkKeys>(c, views, v0, least_p, most_p)) {
+        const Sight sight(c, p);
+        int key = k_first + 4 * half;  // (a tile lies on one side of the gap)
+        uint64_t there = seen >> (4 * half);
+        asm volatile("" : "+v"(key), "+v"(there));  // (or the sums with rows' constants would be held over the loop)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) hide_unseen(s[kb], c, views, v0 + 32 * kb + 4 * half, p, seen, 32 * kb + 4 * half);
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int row = 32 * kb + acc_row(r);
+            s[kb][r] = sight.sees(key + row) && (there >> row & 1) ? s[kb][r] : kMinusInf;
+          }
       }
       softmax_step(s, a.scale_log2, ref, sum, acc);
       u32x4_t pr[kChunkKeys / 16];
@@ -875,6 +914,7 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   }
   const int64_t unit = c.p.e4m3 ? 16 : 8;  // elements of 16 bytes
   const bool whole = (((uintptr_t)c.p.K | (uintptr_t)c.p.V) & 15) == 0 && (c.p.page | c.p.token | c.p.head) % unit == 0;
+  const bool direct = whole && !c.p.e4m3 && c.p.page_size % copy_rows(padded_head(c.p.D)) == 0 && c.p.token <= kMostStride;
   with_head(c.p.D, whole, [&](auto dp, auto is_whole) {
     constexpr int DP = decltype(dp)::value;
     constexpr bool WHOLE = decltype(is_whole)::value;
@@ -888,7 +928,10 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
           paged_few_join_kernel<DP><<<join, kThreads, 0, s>>>(a, (int)plan.blocks);
         }
       } else {
-        paged_chunk_kernel<DP, CODES, WHOLE><<<dim3((unsigned)tile_blocks(c.p.B, c.p.H, 1, a.n_tiles * a.cuts)), kThreads, 0, s>>>(a);
+        const dim3 grid((unsigned)tile_blocks(c.p.B, c.p.H, 1, a.n_tiles * a.cuts));
+        if constexpr (CODES) paged_chunk_kernel<DP, WHOLE ? kPagedCodes : kPagedAnyCodes><<<grid, kThreads, 0, s>>>(a);
+        else if (WHOLE && direct) paged_chunk_kernel<DP, kPagedDirect><<<grid, kThreads, 0, s>>>(a);
+        else paged_chunk_kernel<DP, WHOLE ? kPagedBf16 : kPagedAnyBf16><<<grid, kThreads, 0, s>>>(a);
         if (a.cuts > 1) {
           const int64_t waves = c.max_q * c.Hq, blocks = (waves + kWaves - 1) / kWaves;
           paged_chunk_join_kernel<DP><<<dim3((unsigned)(blocks < 1 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks - 1), (unsigned)c.p.B), kThreads, 0, s>>>(a);
