@@ -26,7 +26,8 @@ struct PagedArgs {
   int group;         // heads that share a key head
   float scale_log2;  // scale * log2(e)
   int n_tiles;       // column tiles of a unit that the grid has
-  int cuts;          // few: whether units are dealt to blocks; chunk: pieces of a unit's keys
+  int cuts;          // few: whether units are dealt to blocks; chunk: pieces of a unit's keys, at most
+  int piece;         // chunk: tiles of keys above which a unit is cut
   float* part_o;     // few: [slot][16][DP]; chunk: [query][head][cut][DP]
   float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
   int slots;         // few: that the workspace holds
@@ -715,6 +716,19 @@ __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArg
 // ------------------------------------------------------------------------------------------------------
 // chunks of queries
 // ------------------------------------------------------------------------------------------------------
+// The keys that a tile's columns see, and how many blocks share them.
+__device__ __forceinline__ int chunk_position(const PagedSequence& of, int group, int column) {
+  const int columns = of.len * group;
+  return of.n - of.len + (column < columns ? column : columns - 1) / group;
+}
+__device__ __forceinline__ Views chunk_views(const PagedArgs& a, const PagedSequence& of, int tile) {
+  return paged_views<kChunkKeys>(a.c, chunk_position(of, a.group, tile * kChunkColumns), chunk_position(of, a.group, (tile + 1) * kChunkColumns - 1));
+}
+__device__ __forceinline__ int chunk_pieces(const PagedArgs& a, int all) {
+  const int pieces = (all + a.piece - 1) / a.piece;
+  return pieces < 1 ? 1 : pieces < a.cuts ? pieces : a.cuts;
+}
+
 template <int DP, int HOW>
 __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArgs a) {
   using Tile = RowTile<DP>;
@@ -733,13 +747,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
   const int first = of.n - of.len;  // the first query's position
   for (int tile = place.tile / a.cuts; tile * kChunkColumns < columns; tile += a.n_tiles) {
     const int c0 = tile * kChunkColumns, c_wave = c0 + wave * 32, n = c_wave + (lane & 31);
-    auto position = [&](int column) { return first + (column < columns ? column : columns - 1) / a.group; };
+    auto position = [&](int column) { return chunk_position(of, a.group, column); };
     const bool live = n < columns;
     const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + qi;
     const int least_p = position(c_wave), most_p = position(c_wave + 31);
-    const Views views = paged_views<kChunkKeys>(c, position(c0), position(c0 + kChunkColumns - 1));
-    const int all = (views.count + kChunkKeys - 1) / kChunkKeys;
-    const int from = (int)((int64_t)all * cut / a.cuts), to = (int)((int64_t)all * (cut + 1) / a.cuts);
+    const Views views = chunk_views(a, of, tile);
+    const int all = (views.count + kChunkKeys - 1) / kChunkKeys, pieces = chunk_pieces(a, all);
+    if (cut >= pieces) continue;
+    const int from = (int)((int64_t)all * cut / pieces), to = (int)((int64_t)all * (cut + 1) / pieces);
     Load load;
     load.begin(c, seq, kv_head, views);
     load.smem = smem[0];
@@ -806,7 +821,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
       products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
     }
     sum = half_sum(sum);
-    if (a.cuts > 1) {
+    if (pieces > 1) {
       if (live) {
         const int64_t part = ((int64_t)(of.q0 + qi) * c.Hq + head) * a.cuts + cut;
 #pragma unroll
@@ -838,8 +853,11 @@ template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_chunk_join_kernel(const PagedArgs a) {
   const PagedSequence of = paged_sequence(a.c, (int)blockIdx.y);
   for (int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); i < (int64_t)of.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
-    const int64_t tok = of.q0 + i / a.c.Hq, at = (tok * a.c.Hq + i % a.c.Hq) * a.cuts;
-    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, 1, a.cuts, tok, (int)(i % a.c.Hq));
+    const int query = (int)(i / a.c.Hq), head = (int)(i % a.c.Hq), tile = (query * a.group + head % a.group) / kChunkColumns;
+    const int pieces = chunk_pieces(a, (chunk_views(a, of, tile).count + kChunkKeys - 1) / kChunkKeys);
+    if (pieces == 1) continue;
+    const int64_t tok = of.q0 + query, at = (tok * a.c.Hq + head) * a.cuts;
+    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, 1, pieces, tok, head);
   }
 }
 
@@ -851,14 +869,42 @@ constexpr int64_t kFewSequences = 512;         // up to which the list of steps 
 constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences, likewise
 constexpr int64_t kFewBlocks = 512;            // blocks that the list is dealt to: two of each compute unit
 constexpr int64_t kUncutKeys = 4 * kStep;      // most keys of a call whose units are left whole
-constexpr int64_t kChunkBlocks = 512, kMostCuts = 16, kLeastCut = 8;  // blocks wanted; key tiles of a cut at least
 struct PagedPlan {
   bool few;
-  int cuts;
+  int cuts, piece;
   int64_t n_tiles, blocks;
-  size_t columns;  // of DP sums, in the workspace
+  size_t columns, most_columns;  // of DP sums, in the workspace; of any max_k, window and sinks
 };
-PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int64_t max_q, int64_t views) {
+// Chunks: pieces of the longest unit's keys, by what the call takes if all units are as long; shorter ones get fewer of the same size.  A
+// step of 64 keys takes a block 1.9 us alone on its compute unit and 2.2 beside another one, of which there is room for two a unit (two causal
+// prompts of 8191 and 342: 2.17; chunks of 2047 and 1080 on caches of 16k, one block to most units: 1.92); a block takes three steps to begin
+// and end, and where blocks are many the last ones end alone.  The pieces' sums are written and read at 5 TB/s, and a launch joins them.
+constexpr int64_t kUnits = 256, kMostCuts = 16;
+int chunk_most_cuts(int64_t units) {
+  const int64_t cuts = 8 * kUnits / units;
+  return (int)(cuts < 1 ? 1 : cuts < kMostCuts ? cuts : kMostCuts);
+}
+int chunk_cuts(int64_t units, int64_t key_tiles, int64_t columns, int DP) {
+  int best = 1;
+  double least = 0;
+  for (int cuts = 1; cuts <= chunk_most_cuts(units); ++cuts) {
+    const double steps = (double)((key_tiles + cuts - 1) / cuts + 3), blocks = (double)units * cuts;
+    double us = blocks <= kUnits ? 1.9 * steps : 2.2 * steps * (blocks <= 2 * kUnits ? 1 : blocks / (2 * kUnits) + 0.3);
+    if (cuts > 1) us += 6 + (double)columns * cuts * DP * 8 / 5e6;
+    if (cuts == 1 || us < least) {
+      best = cuts;
+      least = us;
+    }
+  }
+  return best;
+}
+// keys that some queries in a row may see
+int64_t paged_most_views(int64_t queries, int64_t max_k, int window, int sinks) {
+  if (window <= 0) return max_k;
+  const int64_t some = (int64_t)window + sinks + queries;
+  return some < max_k ? some : max_k;
+}
+PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
   PagedPlan p = {};
   const int64_t group = Hq / Hkv, units = (int64_t)B * Hkv;
   p.few = max_q * group <= kFewColumns;
@@ -867,34 +913,33 @@ PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int64_t max_q, int64_t 
   if (p.n_tiles < 1) p.n_tiles = 1;
   if (p.few) {
     const int64_t tiles = B + Tq * group / kCols;  // at most
-    p.cuts = B <= kFewSequences && tiles <= kFewTiles && views > kUncutKeys;
+    p.cuts = B <= kFewSequences && tiles <= kFewTiles;
+    p.most_columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
+    if (paged_most_views(max_q, max_k, window, sinks) <= kUncutKeys) p.cuts = 0;
     p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
-    p.columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
+    p.columns = p.cuts ? p.most_columns : 0;
   } else {
     while (tile_blocks(B, Hkv, 1, (int)p.n_tiles) >= kMostBlocks) p.n_tiles = (p.n_tiles + 1) / 2;  // (blocks take several then)
-    int64_t cuts = kChunkBlocks / (units * p.n_tiles), key_tiles = (views + kChunkKeys - 1) / kChunkKeys;
-    if (cuts > kMostCuts) cuts = kMostCuts;
-    if (cuts > key_tiles / kLeastCut) cuts = key_tiles / kLeastCut;
-    p.cuts = (int)(cuts < 1 ? 1 : cuts);
+    const int64_t tiles = B + Tq * group / kChunkColumns, some = tiles < B * p.n_tiles ? tiles : B * p.n_tiles;  // with queries, at most
+    const int64_t views = paged_most_views(max_q < kChunkColumns / group ? max_q : kChunkColumns / group + 1, max_k, window, sinks);
+    const int64_t key_tiles = (views + kChunkKeys - 1) / kChunkKeys;
+    p.cuts = chunk_cuts(some * Hkv, key_tiles, Tq * Hq, padded_head(D));
+    p.piece = (int)((key_tiles + p.cuts - 1) / p.cuts > 0 ? (key_tiles + p.cuts - 1) / p.cuts : 1);
+    const int most = chunk_most_cuts(some * Hkv);
     p.columns = p.cuts > 1 ? (size_t)Tq * Hq * p.cuts : 0;
+    p.most_columns = most > 1 ? (size_t)Tq * Hq * most : 0;
   }
   return p;
-}
-// keys that one query may see
-int64_t paged_most_views(int64_t max_q, int64_t max_k, int window, int sinks) {
-  if (window <= 0) return max_k;
-  const int64_t some = (int64_t)window + sinks + max_q;
-  return some < max_k ? some : max_k;
 }
 size_t paged_bytes(size_t columns, int D) { return columns ? round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2) : 0; }
 
 }  // namespace
 
 size_t paged_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
-  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, max_q, paged_most_views(max_q, max_k, window, sinks)).columns, D);
+  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, D, max_q, max_k, window, sinks).columns, D);
 }
 size_t paged_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q) {
-  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, max_q, (int64_t)1 << 31).columns, D);
+  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, D, max_q, 0, 0, 0).most_columns, D);
 }
 
 hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
@@ -903,9 +948,10 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   a.divide = page_divide(c.p.page_size);
   a.group = c.Hq / c.p.H;
   a.scale_log2 = c.scale * kLog2e;
-  const PagedPlan plan = paged_plan(c.Tq, c.p.B, c.Hq, c.p.H, c.max_q, paged_most_views(c.max_q, c.max_k, c.window, c.sinks));
+  const PagedPlan plan = paged_plan(c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks);
   a.n_tiles = (int)plan.n_tiles;
   a.cuts = plan.cuts;
+  a.piece = plan.piece;
   a.slots = (int)(plan.columns / kCols);
   a.whole_o = whole_rows(c.O);
   if (plan.columns) {
