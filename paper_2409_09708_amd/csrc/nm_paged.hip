@@ -12,7 +12,8 @@
 //
 // Two kernels.  paged_few_kernel: 16 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
 // the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
-// paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves; keys cut evenly where there are few blocks.
+// paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves, or for each of two such teams; keys cut where there are
+// few blocks.
 #include "nm_attention.h"
 #include "nm_pages.h"
 
@@ -20,16 +21,26 @@ namespace nm {
 
 namespace {
 
+// What a block of the first launch leaves for the second: the unit that begins in it and goes on in the blocks after it.
+struct FewShared {
+  int parts;  // blocks that share it; 0: there is none
+  int slot;   // of the first part
+  int q0, columns, tile, kv_head;
+  int unused[2];
+};
+
 struct PagedArgs {
   PagedCall c;
   PageDivide divide;
   int group;         // heads that share a key head
   float scale_log2;  // scale * log2(e)
-  int n_tiles;       // column tiles of a unit that the grid has
+  int n_tiles;       // column tiles of a sequence, as far as is known
+  bool listed;       // chunk: whether blocks count the sequences' tiles
   int cuts;          // few: whether units are dealt to blocks; chunk: pieces of a unit's keys, at most
   int piece;         // chunk: tiles of keys above which a unit is cut
   float* part_o;     // few: [slot][16][DP]; chunk: [query][head][cut][DP]
   float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
+  FewShared* shared; // few: [block]
   int slots;         // few: that the workspace holds
   bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
 };
@@ -49,6 +60,19 @@ __device__ __forceinline__ PagedSequence paged_sequence(const PagedCall& c, int 
   q0 = q0 < 0 ? 0 : q0 < c.Tq ? q0 : (int)c.Tq;
   q1 = q1 < q0 ? q0 : q1 < c.Tq ? q1 : (int)c.Tq;
   return {q0, q1 - q0, n};
+}
+
+// ... of a lane's own sequence
+__device__ __forceinline__ PagedSequence lane_sequence(const PagedCall& c, int b) {
+  const int each = (int)(c.Tq / c.p.B), Tq = (int)c.Tq;
+  int q0 = b * each, q1 = q0 + each;
+  if (c.offsets_q != nullptr) {
+    q0 = c.offsets_q[b];
+    q1 = c.offsets_q[b + 1];
+  }
+  q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
+  q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
+  return {q0, q1 - q0, page_clamped(c.p, c.p.lengths[b])};
 }
 
 // The keys that queries at positions first .. last may see, numbered without the gap: view v is key v below `sinks`, else v + gap.
@@ -74,7 +98,7 @@ __device__ __forceinline__ Views paged_views(const PagedCall& c, int first, int 
 enum { kPagedDirect, kPagedBf16, kPagedCodes, kPagedAnyBf16, kPagedAnyCodes };
 constexpr int copy_rows(int DP) { return 512 / DP; }  // that a wave's copy of a kilobyte brings
 
-// A block's tile of 64 keys and values in LDS, as bfloat16.
+// A tile of 64 keys and values in LDS, as bfloat16, for a team of four waves.
 //   look_up(v0)    starts the look-up of the pages of views v0 .. (every wave for itself)
 //   fetch(stage)   starts the loads of the tile looked up last
 //   settle(stage)  the rows that this wave brings are in LDS, zeros for those that are not there (of the values, where copies are
@@ -123,7 +147,7 @@ struct ChunkTile {
   }
   __device__ __forceinline__ void fetch(const PagedArgs& a, int stage) {
     const PagesCall& p = a.c.p;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x % kThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool there = slot >= 0 && (uint32_t)entry < (uint64_t)p.pages;
     seen = __ballot(there && shown);
     if constexpr (DIRECT) {
@@ -174,7 +198,7 @@ struct ChunkTile {
     if constexpr (DIRECT) {
       wait_loads_outstanding<0>();
       if (seen == ~0ull) return;
-      int tid = threadIdx.x;
+      int tid = threadIdx.x % kThreads;
       uint32_t zero = 0;
       asm volatile("" : "+v"(tid), "+v"(zero));  // (computed here, in a few tiles: held over the loop it would cost registers)
 #pragma unroll
@@ -184,7 +208,7 @@ struct ChunkTile {
           *(lds_u32x4_out_ptr)(uintptr_t)(lds + (2 * stage + 1) * kBytes + i * 16) = u32x4_t{zero, zero, zero, zero};
       }
     } else {
-      const int tid = threadIdx.x;
+      const int tid = threadIdx.x % kThreads;
 #pragma unroll
       for (int n = 0; n < kLoads; ++n) {
         const int i = n * kThreads + tid, piece = i % kPer, row = kPieces % kThreads == 0 ? i / kPer : i / kPer & 63;
@@ -409,15 +433,7 @@ __device__ __forceinline__ void few_units(const PagedArgs& a, int b0, Units* u) 
   u->b0 = b0;
   u->steps = u->tiles = 0;
   if (b < a.c.p.B) {
-    const int each = (int)(a.c.Tq / a.c.p.B), Tq = (int)a.c.Tq;
-    int q0 = b * each, q1 = q0 + each;
-    if (a.c.offsets_q != nullptr) {
-      q0 = a.c.offsets_q[b];
-      q1 = a.c.offsets_q[b + 1];
-    }
-    q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
-    q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
-    u->of = {q0, q1 - q0, page_clamped(a.c.p, a.c.p.lengths[b])};
+    u->of = lane_sequence(a.c, b);
     const int steps = (few_views(a.c, u->of).count + kStep - 1) / kStep;
     u->steps = steps > 0 ? steps : 1;
     u->tiles = (u->of.len * a.group + kCols - 1) / kCols;
@@ -448,24 +464,20 @@ __device__ __forceinline__ void few_totals(const PagedArgs& a, Units* u, int64_t
   }
 }
 
-// Where step `at` of a key head's list (or, BY_TILE, tile `at`) lies.
+// Where step `at` of a key head's list lies.
 struct UnitPlace {
   int seq, tile, step, steps;  // a tile of `steps` steps, `step` of which are before this one
   int unit;                    // tiles before it
-  int64_t begin;               // steps before its first
   PagedSequence of;
 };
-template <bool BY_TILE>
 __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int64_t at) {
   int64_t steps_before = 0;
   int tiles_before = 0;
   for (int b0 = 0;; b0 += 64) {
     if (u->b0 != b0) few_units(a, b0, u);
     const int64_t all = lane_value(u->upto, 63);
-    const int all_tiles = __builtin_amdgcn_readlane(u->tiles_upto, 63);
-    const bool here = BY_TILE ? at < tiles_before + all_tiles : at < steps_before + all;
-    if (here || b0 + 64 >= a.c.p.B) {
-      const uint64_t above = BY_TILE ? __ballot((int64_t)tiles_before + u->tiles_upto > at) : __ballot(steps_before + u->upto > at);
+    if (at < steps_before + all || b0 + 64 >= a.c.p.B) {
+      const uint64_t above = __ballot(steps_before + u->upto > at);
       const int l = above ? __ffsll((unsigned long long)above) - 1 : 0;
       UnitPlace p;
       p.seq = b0 + l;
@@ -473,15 +485,13 @@ __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int
       p.steps = __builtin_amdgcn_readlane(u->steps, l);
       const int tiles = __builtin_amdgcn_readlane(u->tiles, l);
       const int64_t first = steps_before + lane_value(u->upto, l) - (int64_t)p.steps * tiles;
-      const int first_tile = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles;
-      p.tile = BY_TILE ? (int)(at - first_tile) : tiles == 1 ? 0 : (int)((at - first) / p.steps);
-      p.begin = first + (int64_t)p.tile * p.steps;
-      p.step = BY_TILE ? 0 : (int)(at - p.begin);
-      p.unit = first_tile + p.tile;
+      p.tile = tiles == 1 ? 0 : (int)((at - first) / p.steps);
+      p.step = (int)(at - first) - p.tile * p.steps;
+      p.unit = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles + p.tile;
       return p;
     }
     steps_before += all;
-    tiles_before += all_tiles;
+    tiles_before += __builtin_amdgcn_readlane(u->tiles_upto, 63);
   }
 }
 constexpr int64_t kLeastShare = 2;  // steps that a block takes at least
@@ -509,11 +519,12 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
   // this block's run of the list of steps -- or, uncut, every (gridDim.x)-th of the units that the grid was made for
   Units units;
   units.b0 = -1;
-  int64_t at, end = 0, per_head = 0;
+  int64_t at, end = 0, per_head = 0, share = 0;
   int tiles_per_head = 0;
+  FewShared left = {};
   if (a.cuts) {
     few_totals(a, &units, &per_head, &tiles_per_head);
-    const int64_t share = few_share(per_head * c.p.H, (int)gridDim.x);
+    share = few_share(per_head * c.p.H, (int)gridDim.x);
     at = blockIdx.x * share;
     end = at + share < per_head * c.p.H ? at + share : per_head * c.p.H;
   } else {
@@ -526,11 +537,15 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
     PagedSequence of;
     if (a.cuts) {
       kv_head = (int)((uint64_t)at / (uint64_t)per_head);
-      const UnitPlace p = few_place<false>(a, &units, at - kv_head * per_head);
+      const UnitPlace p = few_place(a, &units, at - kv_head * per_head);
       seq = p.seq; tile = p.tile; step = p.step; of = p.of;
       steps = (int)(end - at < p.steps - step ? end - at : p.steps - step);
       alone = steps == p.steps;
       slot = kv_head * tiles_per_head + p.unit + (int)blockIdx.x;  // (each further unit, and each further block, is one more)
+      if (!alone && step == 0) {
+        const int to = (int)((uint64_t)(at + p.steps - 1) / (uint64_t)share);
+        left = {to - (int)blockIdx.x + 1, slot, of.q0, of.len * a.group, tile, kv_head, {}};
+      }
       at += steps;
     } else {
       seq = (int)(at / (c.p.H * a.n_tiles));
@@ -653,6 +668,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       if (a.cuts) break;
     }
   }
+  if (a.cuts && tid == 0) a.shared[blockIdx.x] = left;
 }
 
 // One column's parts, `stride` columns of DP elements apart, joined in order by a wave: DP / 4 lanes take four elements each of every
@@ -689,27 +705,15 @@ __device__ __forceinline__ void join_parts(const PagedCall& c, const float* part
   if (c.lse != nullptr && lane == 0) c.lse[(int64_t)head * c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
 }
 
-// A block takes units in turn, a wave a column of one (and further ones, of sequences with more queries than the grid was made for); units that one block of the first launch had whole are done.
+// A block to each of the first launch, for the unit that began there; a wave takes a column at a time.
 template <int DP>
-__global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a, int blocks) {
-  const PagedCall& c = a.c;
-  Units units;
-  int64_t per_head;
-  int tiles_per_head;
-  few_totals(a, &units, &per_head, &tiles_per_head);
-  const int64_t share = few_share(per_head * c.p.H, blocks);
-  for (int64_t i = blockIdx.x; i < (int64_t)tiles_per_head * c.p.H; i += gridDim.x) {
-    const int kv_head = (int)(i / tiles_per_head);
-    const UnitPlace p = few_place<true>(a, &units, i - (int64_t)kv_head * tiles_per_head);
-    const int64_t begin = kv_head * per_head + p.begin;
-    const int64_t from = begin / share, to = (begin + p.steps - 1) / share, slot = i + from;
-    if (from == to || slot + (to - from) >= a.slots) continue;
-    const int columns = p.of.len * a.group - p.tile * kCols;
-    for (int col = blockIdx.y * kWaves + (threadIdx.x >> 6); col < kCols && col < columns; col += gridDim.y * kWaves) {
-      const int n = p.tile * kCols + col;
-      join_parts<DP>(c, a.part_o + (slot * kCols + col) * DP, a.part_ml + slot * kCols + col, kCols, (int)(to - from + 1), p.of.q0 + n / a.group,
-                     kv_head * a.group + n % a.group);
-    }
+__global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a) {
+  const FewShared u = a.shared[blockIdx.x];
+  if (u.parts == 0 || u.slot + u.parts > a.slots) return;
+  for (int col = blockIdx.y * kWaves + (threadIdx.x >> 6); col < kCols && u.tile * kCols + col < u.columns; col += gridDim.y * kWaves) {
+    const int n = u.tile * kCols + col;
+    const int64_t at = (int64_t)u.slot * kCols + col;
+    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, kCols, u.parts, u.q0 + n / a.group, u.kv_head * a.group + n % a.group);
   }
 }
 
@@ -729,44 +733,84 @@ __device__ __forceinline__ int chunk_pieces(const PagedArgs& a, int all) {
   return pieces < 1 ? 1 : pieces < a.cuts ? pieces : a.cuts;
 }
 
-template <int DP, int HOW>
-__global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArgs a) {
+// Tile `at` of all sequences' tiles, one sequence after another, a sequence's last tile first, since it sees the most keys.  False: there are
+// not so many.  (The last tiles of all sequences first, which left shorter and longer units in turn: the two chunks of 2047 and 1080 tokens 545 us
+// for 360.  Every second block went to the same compute units.)
+__device__ __forceinline__ bool chunk_place(const PagedArgs& a, int64_t at, int* seq, int* tile, PagedSequence* of) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.c.p.B; b0 += 64) {
+    PagedSequence its = {0, 0, 0};
+    if (b0 + lane < a.c.p.B) its = lane_sequence(a.c, b0 + lane);
+    const int tiles = (its.len * a.group + kChunkColumns - 1) / kChunkColumns;
+    int upto = tiles;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int before = __shfl_up(upto, m, 64);
+      if (lane >= m) upto += before;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (at < all) {
+      const int l = __ffsll((unsigned long long)__ballot(upto > (int)at)) - 1;
+      *seq = b0 + l;
+      *tile = __builtin_amdgcn_readlane(upto, l) - 1 - (int)at;
+      *of = {__builtin_amdgcn_readlane(its.q0, l), __builtin_amdgcn_readlane(its.len, l), __builtin_amdgcn_readlane(its.n, l)};
+      return true;
+    }
+    at -= all;
+  }
+  return false;
+}
+
+// A block has one or two teams of four waves, 32 columns to a wave; two teams have the same columns and take the tiles of keys in turn.
+template <int DP, int HOW, int TEAMS>
+__global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const PagedArgs a) {
   using Tile = RowTile<DP>;
   using Load = ChunkTile<DP, HOW>;
   constexpr bool WHOLE = HOW <= kPagedCodes;
   constexpr int NB = DP / 32, STEPS = DP / 16;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2][2 * Load::kBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[TEAMS][2][2 * Load::kBytes];
   const PagedCall& c = a.c;
-  TilePlace place;
-  if (!tile_place(c.p.B, c.p.H, 1, a.n_tiles * a.cuts, true, true, &place)) return;
-  const int kv_head = place.kv_head, seq = place.seq, cut = place.tile % a.cuts;
   const int D = WHOLE ? DP : c.p.D;
-  const PagedSequence of = paged_sequence(c, seq);
-  const int columns = of.len * a.group;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int first = of.n - of.len;  // the first query's position
-  for (int tile = place.tile / a.cuts; tile * kChunkColumns < columns; tile += a.n_tiles) {
-    const int c0 = tile * kChunkColumns, c_wave = c0 + wave * 32, n = c_wave + (lane & 31);
-    auto position = [&](int column) { return chunk_position(of, a.group, column); };
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x % kThreads >> 6);
+  const int team = TEAMS == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  // Consecutive blocks go to consecutive XCDs, each with an L2 of its own: key heads change fastest, so that an XCD has few of them.  Where
+  // sequences are as long as each other, or too many to count their tiles, the last tiles of all of them come first, then those before them.
+  for (int64_t item = blockIdx.x;; item += gridDim.x) {
+    const int kv_head = (int)(item % c.p.H), cut = (int)(item / c.p.H % a.cuts);
+    const int64_t at = item / c.p.H / a.cuts;
+    int seq, tile;
+    PagedSequence of;
+    if (a.listed) {
+      if (!chunk_place(a, at, &seq, &tile, &of)) return;
+    } else {
+      seq = (int)(at % c.p.B);
+      tile = (int)(at / c.p.B);
+      if ((int64_t)tile * kChunkColumns >= c.Tq * a.group) return;
+      if (tile < a.n_tiles) tile = a.n_tiles - 1 - tile;  // (behind n_tiles: those of sequences that are longer than was said)
+      of = paged_sequence(c, seq);
+      if (tile * kChunkColumns >= of.len * a.group) continue;
+    }
+    const int columns = of.len * a.group, first = of.n - of.len;  // (the first query's position)
+    const int c_wave = tile * kChunkColumns + wave * 32, n = c_wave + (lane & 31);
     const bool live = n < columns;
     const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + qi;
-    const int least_p = position(c_wave), most_p = position(c_wave + 31);
+    const int least_p = chunk_position(of, a.group, c_wave), most_p = chunk_position(of, a.group, c_wave + 31);
     const Views views = chunk_views(a, of, tile);
     const int all = (views.count + kChunkKeys - 1) / kChunkKeys, pieces = chunk_pieces(a, all);
     if (cut >= pieces) continue;
     const int from = (int)((int64_t)all * cut / pieces), to = (int)((int64_t)all * (cut + 1) / pieces);
     Load load;
     load.begin(c, seq, kv_head, views);
-    load.smem = smem[0];
-    load.lds = NM_LDS_ADDRESS(smem[0]);
-    __syncthreads();  // (a block's second tile: the first one's keys are no longer read)
-    load.look_up(a, from * kChunkKeys);
+    load.smem = smem[team][0];
+    load.lds = NM_LDS_ADDRESS(smem[team][0]);
+    __syncthreads();  // (a block's second tile: what the first one had in LDS is no longer read)
+    load.look_up(a, (from + team) * kChunkKeys);
     u32x4_t q[STEPS];
     const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-    if (from < to) load.fetch(a, 0);
-    load.look_up(a, (from + 1) * kChunkKeys);
+    if (from + team < to) load.fetch(a, 0);
+    load.look_up(a, (from + team + TEAMS) * kChunkKeys);
     if constexpr (Load::DIRECT) arrived(q);
     f32x16_t acc[NB];
 #pragma unroll
@@ -774,19 +818,21 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
     float ref = kMinusInf, sum = 0.f;
-    for (int kt = from; kt < to; ++kt) {
-      const int stage = (kt - from) & 1, v0 = kt * kChunkKeys;
-      load.settle(stage);
+    int stage = 0;
+    for (int k0 = from; k0 < to; k0 += TEAMS, stage ^= 1) {
+      const int kt = k0 + team, v0 = kt * kChunkKeys;
+      if (TEAMS == 1 || kt < to) load.settle(stage);
       const uint64_t seen = load.seen;
       __syncthreads();
-      if (kt + 1 < to) {
+      if (kt + TEAMS < to) {
         load.fetch(a, stage ^ 1);
-        load.look_up(a, v0 + 2 * kChunkKeys);
+        load.look_up(a, v0 + 2 * TEAMS * kChunkKeys);
       }
       // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
       const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
-      if (c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= least_p - c.window && k_first >= c.sinks)) continue;
-      const uint32_t k_tile = NM_LDS_ADDRESS(smem[0]) + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
+      if ((TEAMS > 1 && kt >= to) || c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= least_p - c.window && k_first >= c.sinks))
+        continue;
+      const uint32_t k_tile = load.lds + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
       const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
       constexpr int KB = kChunkKeys / 32, NS = KB * STEPS, NV = kChunkKeys / 16 * NB;
       // (products on the same sums wait for each other: the two runs of keys in turn)
@@ -821,6 +867,29 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
       products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
     }
     sum = half_sum(sum);
+    if constexpr (TEAMS == 2) {  // the second team's sums to the first, which has the same columns in the same lanes
+      static_assert(kWaves * (NB * 16 + 2) * 64 * 4 <= (int)sizeof(smem), "in LDS that tiles have left");
+      f32x4_t* box = reinterpret_cast<f32x4_t*>(smem) + wave * NB * 4 * 64 + lane;
+      float2* ml = reinterpret_cast<float2*>(reinterpret_cast<f32x4_t*>(smem) + kWaves * NB * 4 * 64) + wave * 64 + lane;
+      __syncthreads();
+      if (team == 1) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) box[(b * 4 + r) * 64] = f32x4_t{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]};
+        *ml = float2{ref, sum};
+      }
+      __syncthreads();
+      if (team == 1) continue;
+      const float2 other = *ml;
+      const float top = fmaxf(ref, other.x), mine = part_weight(ref, top), its = part_weight(other.x, top);
+      ref = top;
+      sum = sum * mine + other.y * its;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][r] = acc[b][r] * mine + box[(b * 4 + r / 4) * 64][r % 4] * its;
+    }
     if (pieces > 1) {
       if (live) {
         const int64_t part = ((int64_t)(of.q0 + qi) * c.Hq + head) * a.cuts + cut;
@@ -848,54 +917,81 @@ __global__ void __launch_bounds__(kThreads, 2) paged_chunk_kernel(const PagedArg
   }
 }
 
-// A wave per (query, head).
+// The pieces of a column joined in order: DP / 4 lanes to a (query, head), four elements each.
 template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_chunk_join_kernel(const PagedArgs a) {
-  const PagedSequence of = paged_sequence(a.c, (int)blockIdx.y);
-  for (int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); i < (int64_t)of.len * a.c.Hq; i += (int64_t)gridDim.x * kWaves) {
-    const int query = (int)(i / a.c.Hq), head = (int)(i % a.c.Hq), tile = (query * a.group + head % a.group) / kChunkColumns;
+  constexpr int LANES = DP / 4, GROUPS = kThreads / LANES;
+  const PagedCall& c = a.c;
+  const PagedSequence of = paged_sequence(c, (int)blockIdx.y);
+  const int d = threadIdx.x % LANES * 4, rows = of.len * c.Hq;
+  for (int i = blockIdx.x * GROUPS + threadIdx.x / LANES; i < rows; i += gridDim.x * GROUPS) {
+    const int query = i / c.Hq, head = i - query * c.Hq, tile = (query * a.group + head % a.group) / kChunkColumns;
     const int pieces = chunk_pieces(a, (chunk_views(a, of, tile).count + kChunkKeys - 1) / kChunkKeys);
     if (pieces == 1) continue;
-    const int64_t tok = of.q0 + query, at = (tok * a.c.Hq + head) * a.cuts;
-    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, 1, pieces, tok, head);
+    const int64_t tok = of.q0 + query, at = (tok * c.Hq + head) * a.cuts;
+    const float2* ml = a.part_ml + at;
+    const float* part = a.part_o + at * DP + d;
+    float top = kMinusInf, total = 0.f;
+    for (int k = 0; k < pieces; ++k) top = fmaxf(top, ml[k].x);
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < pieces; ++k) {
+      const float by = part_weight(ml[k].x, top);
+      total = fmaf(ml[k].y, by, total);
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * DP);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], by, o[e]);
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    if (d < c.p.D)
+      store4(c.O.p + tok * c.O.token + head * c.O.head, d, c.p.D, pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    if (c.lse != nullptr && d == 0) c.lse[(int64_t)head * c.Tq + tok] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
   }
 }
 
 // ------------------------------------------------------------------------------------------------------
 // How a call is cut
 // ------------------------------------------------------------------------------------------------------
-constexpr int64_t kFewColumns = 128;           // (query, head) pairs of a key head up to which the first kernel serves
-constexpr int64_t kFewSequences = 512;         // up to which the list of steps is dealt out
+constexpr int64_t kFewColumns = 64;            // (query, head) pairs of a key head up to which the first kernel serves
+constexpr int64_t kFewSequences = 512;         // up to which lists are made
 constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences, likewise
 constexpr int64_t kFewBlocks = 512;            // blocks that the list is dealt to: two of each compute unit
 constexpr int64_t kUncutKeys = 4 * kStep;      // most keys of a call whose units are left whole
 struct PagedPlan {
-  bool few;
-  int cuts, piece;
+  bool few, listed;
+  int cuts, piece, teams;
   int64_t n_tiles, blocks;
   size_t columns, most_columns;  // of DP sums, in the workspace; of any max_k, window and sinks
 };
-// Chunks: pieces of the longest unit's keys, by what the call takes if all units are as long; shorter ones get fewer of the same size.  A
-// step of 64 keys takes a block 1.9 us alone on its compute unit and 2.2 beside another one, of which there is room for two a unit (two causal
-// prompts of 8191 and 342: 2.17; chunks of 2047 and 1080 on caches of 16k, one block to most units: 1.92); a block takes three steps to begin
-// and end, and where blocks are many the last ones end alone.  The pieces' sums are written and read at 5 TB/s, and a launch joins them.
+// Chunks: teams of a block and pieces of the longest unit's keys, by what the call takes if all units are as long; shorter ones get fewer
+// of the same size.  A step of 64 keys takes a team 1.9 us alone on its compute unit and 2.2 beside another one, of the same block or not (two
+// causal prompts of 8191 and 342: 2.17; chunks of 2047 and 1080 on caches of 16k, one team to most units: 1.92); a block takes three steps
+// to begin and end, a block of two teams four, and where blocks are many the last ones end alone.  The pieces' sums are written and read at
+// 5 TB/s, and a launch joins them; where that wins less than a tenth, sequences are hardly ever all as long as the longest (the two chunks
+// with teams of two and one, two and three pieces: 352, 389 and 393 us; one team 439, 379 and 359).
 constexpr int64_t kUnits = 256, kMostCuts = 16;
+struct ChunkPlan {
+  int teams, cuts;
+};
 int chunk_most_cuts(int64_t units) {
   const int64_t cuts = 8 * kUnits / units;
   return (int)(cuts < 1 ? 1 : cuts < kMostCuts ? cuts : kMostCuts);
 }
-int chunk_cuts(int64_t units, int64_t key_tiles, int64_t columns, int DP) {
-  int best = 1;
+ChunkPlan chunk_plan(int64_t units, int64_t key_tiles, int64_t columns, int DP) {
+  ChunkPlan best = {1, 1};
   double least = 0;
-  for (int cuts = 1; cuts <= chunk_most_cuts(units); ++cuts) {
-    const double steps = (double)((key_tiles + cuts - 1) / cuts + 3), blocks = (double)units * cuts;
-    double us = blocks <= kUnits ? 1.9 * steps : 2.2 * steps * (blocks <= 2 * kUnits ? 1 : blocks / (2 * kUnits) + 0.3);
-    if (cuts > 1) us += 6 + (double)columns * cuts * DP * 8 / 5e6;
-    if (cuts == 1 || us < least) {
-      best = cuts;
-      least = us;
+  for (int teams = 1; teams <= 2; ++teams)
+    for (int cuts = 1; cuts <= chunk_most_cuts(units); ++cuts) {
+      const double steps = (double)((key_tiles + cuts * teams - 1) / (cuts * teams) + 2 + teams), blocks = (double)units * cuts;
+      const double rounds = blocks * teams / (2 * kUnits);
+      double us = teams == 1 && blocks <= kUnits ? 1.9 * steps : 2.2 * steps * (rounds <= 1 ? 1 : rounds + 0.3);
+      if (cuts > 1) us += 6 + (double)columns * cuts * DP * 8 / 5e6;
+      if (cuts > 1) us *= 1.1;
+      if ((teams == 1 && cuts == 1) || us < least) {
+        best = {teams, cuts};
+        least = us;
+      }
     }
-  }
   return best;
 }
 // keys that some queries in a row may see
@@ -919,11 +1015,15 @@ PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, i
     p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
     p.columns = p.cuts ? p.most_columns : 0;
   } else {
-    while (tile_blocks(B, Hkv, 1, (int)p.n_tiles) >= kMostBlocks) p.n_tiles = (p.n_tiles + 1) / 2;  // (blocks take several then)
     const int64_t tiles = B + Tq * group / kChunkColumns, some = tiles < B * p.n_tiles ? tiles : B * p.n_tiles;  // with queries, at most
     const int64_t views = paged_most_views(max_q < kChunkColumns / group ? max_q : kChunkColumns / group + 1, max_k, window, sinks);
     const int64_t key_tiles = (views + kChunkKeys - 1) / kChunkKeys;
-    p.cuts = chunk_cuts(some * Hkv, key_tiles, Tq * Hq, padded_head(D));
+    const ChunkPlan chunk = chunk_plan(some * Hkv, key_tiles, Tq * Hq, padded_head(D));
+    p.cuts = chunk.cuts;
+    p.teams = chunk.teams;
+    p.listed = B <= kFewSequences && Tq != B * max_q;
+    p.blocks = (p.listed ? some : B * p.n_tiles) * Hkv * p.cuts;
+    if (p.blocks >= kMostBlocks) p.blocks = kMostBlocks - 1;  // (blocks take several then)
     p.piece = (int)((key_tiles + p.cuts - 1) / p.cuts > 0 ? (key_tiles + p.cuts - 1) / p.cuts : 1);
     const int most = chunk_most_cuts(some * Hkv);
     p.columns = p.cuts > 1 ? (size_t)Tq * Hq * p.cuts : 0;
@@ -931,7 +1031,9 @@ PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, i
   }
   return p;
 }
-size_t paged_bytes(size_t columns, int D) { return columns ? round256(columns * padded_head(D) * sizeof(float)) + columns * sizeof(float2) : 0; }
+size_t paged_bytes(size_t columns, int D) {
+  return columns ? round256(columns * padded_head(D) * sizeof(float)) + round256(columns * sizeof(float2)) + kFewBlocks * sizeof(FewShared) : 0;
+}
 
 }  // namespace
 
@@ -952,11 +1054,14 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   a.n_tiles = (int)plan.n_tiles;
   a.cuts = plan.cuts;
   a.piece = plan.piece;
+  a.listed = plan.listed;
   a.slots = (int)(plan.columns / kCols);
   a.whole_o = whole_rows(c.O);
   if (plan.columns) {
     a.part_o = static_cast<float*>(c.workspace);
-    a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(c.workspace) + round256(plan.columns * padded_head(c.p.D) * sizeof(float)));
+    unsigned char* behind = static_cast<unsigned char*>(c.workspace) + round256(plan.columns * padded_head(c.p.D) * sizeof(float));
+    a.part_ml = reinterpret_cast<float2*>(behind);
+    a.shared = reinterpret_cast<FewShared*>(behind + round256(plan.columns * sizeof(float2)));
   }
   const int64_t unit = c.p.e4m3 ? 16 : 8;  // elements of 16 bytes
   const bool whole = (((uintptr_t)c.p.K | (uintptr_t)c.p.V) & 15) == 0 && (c.p.page | c.p.token | c.p.head) % unit == 0;
@@ -969,17 +1074,22 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
       if (plan.few) {
         paged_few_kernel<DP, CODES, WHOLE><<<dim3((unsigned)plan.blocks), kThreads, 0, s>>>(a);
         if (a.cuts) {
-          const int64_t units = (c.p.B + c.Tq * a.group / kCols) * c.p.H, columns = c.max_q * a.group < kCols ? c.max_q * a.group : kCols;
-          const dim3 join((unsigned)(units < 4096 ? units : 4096), (unsigned)(columns > kWaves ? (columns + kWaves - 1) / kWaves : 1));
-          paged_few_join_kernel<DP><<<join, kThreads, 0, s>>>(a, (int)plan.blocks);
+          const int64_t columns = c.max_q * a.group < kCols ? c.max_q * a.group : kCols;
+          const dim3 join((unsigned)plan.blocks, (unsigned)(columns > kWaves ? (columns + kWaves - 1) / kWaves : 1));
+          paged_few_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
         }
       } else {
-        const dim3 grid((unsigned)tile_blocks(c.p.B, c.p.H, 1, a.n_tiles * a.cuts));
-        if constexpr (CODES) paged_chunk_kernel<DP, WHOLE ? kPagedCodes : kPagedAnyCodes><<<grid, kThreads, 0, s>>>(a);
-        else if (WHOLE && direct) paged_chunk_kernel<DP, kPagedDirect><<<grid, kThreads, 0, s>>>(a);
-        else paged_chunk_kernel<DP, WHOLE ? kPagedBf16 : kPagedAnyBf16><<<grid, kThreads, 0, s>>>(a);
+        const dim3 grid((unsigned)plan.blocks);
+        auto launch = [&](auto how) {
+          if (plan.teams == 1) paged_chunk_kernel<DP, decltype(how)::value, 1><<<grid, kThreads, 0, s>>>(a);
+          else paged_chunk_kernel<DP, decltype(how)::value, 2><<<grid, 2 * kThreads, 0, s>>>(a);
+        };
+        if constexpr (CODES) launch(std::integral_constant<int, WHOLE ? kPagedCodes : kPagedAnyCodes>{});
+        else if (WHOLE && direct) launch(std::integral_constant<int, kPagedDirect>{});
+        else launch(std::integral_constant<int, WHOLE ? kPagedBf16 : kPagedAnyBf16>{});
         if (a.cuts > 1) {
-          const int64_t waves = c.max_q * c.Hq, blocks = (waves + kWaves - 1) / kWaves;
+          // (two rows to a group of lanes)
+          const int64_t blocks = (c.max_q * c.Hq * (DP / 4) + 2 * kThreads - 1) / (2 * kThreads);
           paged_chunk_join_kernel<DP><<<dim3((unsigned)(blocks < 1 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks - 1), (unsigned)c.p.B), kThreads, 0, s>>>(a);
         }
       }
