@@ -647,7 +647,7 @@ int32_t nm_attention_backward(const nm_attention_desc* desc, void* workspace, si
  *                dweight is NULL.  Contents undefined afterwards; concurrent calls need distinct workspaces.
  * Statistics and sums are 32-bit floats; a value is rounded once, when it is stored.  Outputs must not overlap inputs otherwise.
  * Errors: NM_ERR_NULL, NM_ERR_SHAPE (sizes <= 0, T above 2^31, D above 512, H * D above 2^20, heads outside [1, H], eps < 0 or NaN, a
- * turn that nm_rotary refuses, negative strides, tokens or heads of Y that overlap), NM_ERR_DTYPE, NM_ERR_ALIGN, NM_ERR_WORKSPACE,
+ * turn that nm_rotary refuses, strides negative or above 2^31 - 1, tokens or heads of Y that overlap), NM_ERR_DTYPE, NM_ERR_ALIGN, NM_ERR_WORKSPACE,
  * NM_ERR_DEVICE.
  */
 typedef struct nm_typed_heads {

@@ -725,7 +725,16 @@ int32_t head_norm_check(const nm_head_norm_desc* d, bool backward, nm::HeadNormC
     if (!aligned(p, 4)) return NM_ERR_ALIGN;
   c->X = d->X.data; c->Y = d->Y.data; c->w = d->weight;
   c->T = T; c->H = H; c->D = D; c->heads = d->heads;
-  c->x_token = d->X.token; c->x_head = d->X.head; c->y_token = d->Y.token; c->y_head = d->Y.head;
+  // (a stride over one token, or one head, is not used)
+  auto stride = [](int64_t s, int64_t n) { return n == 1 ? (int64_t)0 : s; };
+  c->x_token = stride(d->X.token, T); c->x_head = stride(d->X.head, H);
+  c->y_token = stride(d->Y.token, T); c->y_head = stride(d->Y.head, H);
+  if (backward) {
+    c->dy_token = stride(d->dY.token, T);
+    c->dy_head = stride(d->dY.head, H);
+  }
+  for (int64_t s : {c->x_token, c->x_head, c->y_token, c->y_head, c->dy_token, c->dy_head})
+    if (s > 0x7FFFFFFF) return NM_ERR_SHAPE;
   c->eps = d->eps; c->centred = d->centred != 0;
   c->x_f32 = d->X.dtype == NM_OUT_F32; c->y_f32 = d->Y.dtype == NM_OUT_F32;
   if (turned) {
@@ -733,7 +742,7 @@ int32_t head_norm_check(const nm_head_norm_desc* d, bool backward, nm::HeadNormC
     c->positions_f32 = d->positions_f32 != 0; c->interleaved = d->interleaved != 0;
   }
   if (backward) {
-    c->dY = d->dY.data; c->dy_token = d->dY.token; c->dy_head = d->dY.head; c->dy_f32 = d->dY.dtype == NM_OUT_F32;
+    c->dY = d->dY.data; c->dy_f32 = d->dY.dtype == NM_OUT_F32;
     c->dw = d->dweight;
   }
   return NM_OK;
@@ -749,13 +758,13 @@ int32_t nm_head_norm(const nm_head_norm_desc* desc, void* stream) {
 size_t nm_head_norm_backward_workspace_bytes(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t rotated) {
   if (T <= 0 || H <= 0 || D <= 0 || T > kMost || H > 1 << 20 || D > 512 || H * D > 1 << 20 || heads < 1 || heads > H) return 0;
   if (rotated < 0 || rotated > D || rotated % 2) return 0;
-  return nm::head_norm_grad_workspace_bytes(T, H, D, rotated, heads < H ? 2 : 1);
+  return nm::head_norm_grad_workspace_bytes(T, H, heads, D, rotated);
 }
 
 int32_t nm_head_norm_backward(const nm_head_norm_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
   nm::HeadNormCall c;
   if (int32_t st = head_norm_check(desc, true, &c)) return st;
-  if (c.dw && !workspace_ok(workspace, workspace_bytes, nm::head_norm_grad_workspace_bytes(c.T, c.H, c.D, c.R, c.heads < c.H ? 2 : 1)))
+  if (c.dw && !workspace_ok(workspace, workspace_bytes, nm::head_norm_grad_workspace_bytes(c.T, c.H, c.heads, c.D, c.R)))
     return NM_ERR_WORKSPACE;
   c.workspace = workspace;
   return device_status(nm::launch_head_norm_grad(c, (hipStream_t)stream));

@@ -24,29 +24,53 @@ namespace nm {
 namespace {
 
 constexpr int kHeadThreads = 256;  // (flat_grid_256)
-constexpr int kHeadPairs = 512;    // cosines and sines that a block keeps: 4 KiB
+constexpr int kHeadPairs = 1024;   // cosines and sines that a block keeps: 8 KiB
 constexpr int kHeadMost = 512;     // elements of a head
 
+// The heads that share a row of weights: a block takes those of a run of tokens.
+struct HeadSet {
+  int first, count;  // heads
+  int tokens;        // of a block at a time
+  int splits;        // blocks that share a token's heads (few tokens)
+  int64_t blocks;
+};
 struct HeadArgs {
   HeadNormCall c;
-  int tokens;       // per block and turn
-  int splits;       // blocks that share a token's heads (forward, few tokens)
+  HeadSet set[2];   // queries and keys (the latter with no blocks where all heads share their weights)
   int pairs;        // R / 2
   int rotate;       // pieces of a head with pairs that are turned
-  int64_t groups;   // of tokens
-  float* partial;   // backward: [blocks][sets][D], or NULL: one block, which writes dw itself
+  float* partial;   // backward: [blocks][D], those of the first set before those of the second; NULL: no gradient of the weights
 };
 
 // i / d for 0 <= i < 2^21, from 1 / d: the quotient is at least 0.5 / d away from the next integer, the product off by less
 __device__ __forceinline__ int head_quotient(int i, float inverse) { return (int)(((float)i + 0.5f) * inverse); }
 
-// Sum over the LANES lanes of a head.
+// Sum over the LANES lanes of a head.  Up to 16 lanes the exchanges are operands of the additions: neighbours, pairs, then the halves of
+// eight and of 16 lanes mirrored, which are all the same by then.  (Gradients of 8191 x 40 x 128: 77.5 us with exchanges through LDS.)
+template <int CONTROL>
+__device__ __forceinline__ float lane_moved(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CONTROL, 0xF, 0xF, true));
+}
 template <int LANES>
 __device__ __forceinline__ float head_sum(float v) {
+  v += lane_moved<0xB1>(v);
+  v += lane_moved<0x4E>(v);
+  if constexpr (LANES >= 8) v += lane_moved<0x141>(v);
+  if constexpr (LANES >= 16) v += lane_moved<0x140>(v);
 #pragma unroll
-  for (int m = 1; m < LANES; m <<= 1) v += __shfl_xor(v, m, 64);
+  for (int m = 16; m < LANES; m <<= 1) v += __shfl_xor(v, m, 64);
   return v;
 }
+
+// Where unit i of a run of tokens lies: its token in the run, its head, and the element at which they begin (strides fit 32 bits).
+struct HeadUnit {
+  int tok, head;
+  __device__ __forceinline__ HeadUnit(const HeadSet& s, int i, float by_count) {
+    tok = head_quotient(i, by_count);
+    head = s.first + i - tok * s.count;
+  }
+  __device__ __forceinline__ int64_t at(int64_t run, int token, int heads) const { return run + (int64_t)tok * token + (int64_t)head * heads; }
+};
 
 // The two runs of eight elements that lane k of a head holds: where they begin, how many there are (<= 0: none), and the first of its
 // pairs in the table of a token's turns.
@@ -73,17 +97,35 @@ __device__ __forceinline__ HeadPiece head_piece(const HeadArgs& a, int k) {
   return p;
 }
 
-template <bool F32>
+// A lane's two runs.  WHOLE: each has eight elements or none (left as it was then, which is zeros), so nothing is read or written singly.
+template <bool F32, bool WHOLE>
 struct HeadRaw {
   Raw8<F32> r[2];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int v = 0; v < (F32 ? 2 : 1); ++v) r[i].v[v] = u32x4_t{0, 0, 0, 0};
+  }
   __device__ __forceinline__ void load(const void* base, int64_t row, const HeadPiece& p) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) r[i].load(base, row + p.at[i], p.n[i]);  // (n <= 0: zeros, nothing read)
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (WHOLE) {
+        if (p.n[i] > 0) r[i].load(base, row + p.at[i], 8);
+      } else {
+        r[i].load(base, row + p.at[i], p.n[i]);
+      }
+    }
   }
 };
+template <bool WHOLE>
+__device__ __forceinline__ void head_store(void* base, int64_t row, const HeadPiece& p, const float (&u)[8], const float (&v)[8], bool f32) {
+  if (p.n[0] > 0) store8(base, row + p.at[0], WHOLE ? 8 : p.n[0], u, !f32);
+  if (p.n[1] > 0) store8(base, row + p.at[1], WHOLE ? 8 : p.n[1], v, !f32);
+}
 
 // The turn of a lane's pairs, back where `back`.
-template <bool INTERLEAVED>
+template <bool INTERLEAVED, bool WHOLE>
 __device__ __forceinline__ void head_turn(float (&u)[8], float (&v)[8], const float2* w, const HeadPiece& p, bool back) {
   if (!p.turned) return;
   if constexpr (INTERLEAVED) {
@@ -98,7 +140,7 @@ __device__ __forceinline__ void head_turn(float (&u)[8], float (&v)[8], const fl
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float2 cs = e < p.n[0] ? w[e] : float2{1.f, 0.f};
+      const float2 cs = WHOLE || e < p.n[0] ? w[e] : float2{1.f, 0.f};
       const float sn = back ? -cs.y : cs.y, x = u[e], y = v[e];
       u[e] = x * cs.x - y * sn;
       v[e] = y * cs.x + x * sn;
@@ -119,16 +161,15 @@ __device__ __forceinline__ void head_angles(const HeadArgs& a, int64_t t0, int n
     const int64_t at = (t0 + tok) * c.axes + axis;
     const double pos = c.positions_f32 ? (double)static_cast<const float*>(c.positions)[at]
                                        : (double)static_cast<const int32_t*>(c.positions)[at];
-    constexpr double kTurn = 6.283185307179586476925;
-    const double angle = pos * (double)c.freqs[pair];
+    const double turns = pos * (double)c.freqs[pair] * 0.15915494309189533577;  // (1 / 2 pi)
     float sn, cs;
-    sincosf((float)(angle - kTurn * rint(angle * (1.0 / kTurn))), &sn, &cs);
+    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
     turn[i] = float2{cs, sn};
   }
 }
 
 // c = x (- mean) and 1 / sqrt(mean(c^2) + eps) of a head; elements past it stay zero.
-template <int LANES>
+template <int LANES, bool WHOLE>
 __device__ __forceinline__ float head_stats(float (&u)[8], float (&v)[8], const HeadPiece& p, bool centred, float inv, float eps) {
   if (centred) {
     float first = 0.f;
@@ -138,15 +179,15 @@ __device__ __forceinline__ float head_stats(float (&u)[8], float (&v)[8], const 
     float off = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      u[e] = e < p.n[0] ? u[e] - first : 0.f;
-      v[e] = e < p.n[1] ? v[e] - first : 0.f;
+      u[e] = (WHOLE ? 0 : e) < p.n[0] ? u[e] - first : 0.f;
+      v[e] = (WHOLE ? 0 : e) < p.n[1] ? v[e] - first : 0.f;
       off += u[e] + v[e];
     }
     off = head_sum<LANES>(off) * inv;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (e < p.n[0]) u[e] -= off;
-      if (e < p.n[1]) v[e] -= off;
+      if ((WHOLE ? 0 : e) < p.n[0]) u[e] -= off;
+      if ((WHOLE ? 0 : e) < p.n[1]) v[e] -= off;
     }
   }
   float sq = 0.f;
@@ -159,7 +200,7 @@ __device__ __forceinline__ void head_weight(const HeadArgs& a, int set, const He
 #pragma unroll
   for (int e = 0; e < 8; ++e) wu[e] = wv[e] = 1.f;
   if (a.c.w == nullptr) return;
-  HeadRaw<true> r;
+  HeadRaw<true, false> r;
   r.load(a.c.w, (int64_t)set * a.c.D, p);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -168,165 +209,147 @@ __device__ __forceinline__ void head_weight(const HeadArgs& a, int set, const He
   }
 }
 
-template <bool XF32, bool INTERLEAVED, int LANES>
+template <bool XF32, bool INTERLEAVED, int LANES, bool WHOLE>
 __global__ void __launch_bounds__(kHeadThreads) head_norm_kernel(const HeadArgs a) {
   __shared__ __attribute__((aligned(16))) float2 turn[kHeadPairs];
   constexpr int GROUPS = kHeadThreads / LANES;
   const HeadNormCall& c = a.c;
-  const int64_t block = flat_lane_256() / kHeadThreads;
-  const int64_t t0 = block / a.splits * a.tokens;
-  if (t0 >= c.T) return;
-  const int split = (int)(block % a.splits);
-  const int n_tokens = (int)(c.T - t0 < a.tokens ? c.T - t0 : a.tokens);
-  const int k = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const HeadPiece p = head_piece<INTERLEAVED>(a, k);
-  const float inv = 1.f / (float)c.D;
-  bool ready = false;
-  for (int set = 0; set < 2; ++set) {
-    const int first = set ? (int)c.heads : 0, count = set ? (int)(c.H - c.heads) : (int)c.heads;  // the set's heads
-    if (count == 0) continue;
-    const float by_count = 1.f / (float)count;
-    const int units = n_tokens * count, step = GROUPS * a.splits;
-    HeadRaw<XF32> in;
-    auto fetch = [&](int i) {
-      if (i >= units) return;
-      const int tok = head_quotient(i, by_count);
-      in.load(c.X, (t0 + tok) * c.x_token + (int64_t)(first + i - tok * count) * c.x_head, p);
-    };
-    fetch(split * GROUPS + group);  // (on its way while the angles are computed)
-    float wu[8], wv[8];
-    head_weight(a, set, p, wu, wv);
-    if (!ready) {
-      head_angles(a, t0, n_tokens, turn);
-      __syncthreads();
-      ready = true;
-    }
-    for (int i = split * GROUPS + group; i < units; i += step) {
-      const int tok = head_quotient(i, by_count);
-      const int64_t y = (t0 + tok) * c.y_token + (int64_t)(first + i - tok * count) * c.y_head;
-      float u[8], v[8];
+  int64_t block = flat_lane_256() / kHeadThreads;
+  const int which = block >= a.set[0].blocks;
+  if (which) block -= a.set[0].blocks;
+  const HeadSet& set = a.set[which];
+  if (block >= set.blocks) return;
+  const int splits = set.splits, count = set.count;
+  const int64_t t0 = block / splits * set.tokens;
+  const int n_tokens = (int)(c.T - t0 < set.tokens ? c.T - t0 : set.tokens);
+  const HeadPiece p = head_piece<INTERLEAVED>(a, threadIdx.x % LANES);
+  const float inv = 1.f / (float)c.D, by_count = 1.f / (float)count;
+  const int units = n_tokens * count, step = GROUPS * splits;
+  int i = (int)(block % splits) * GROUPS + threadIdx.x / LANES;
+  HeadRaw<XF32, WHOLE> in;
+  in.clear();
+  const int64_t x_run = t0 * c.x_token, y_run = t0 * c.y_token;
+  auto fetch = [&](int at) {
+    if (at < units) in.load(c.X, HeadUnit(set, at, by_count).at(x_run, (int)c.x_token, (int)c.x_head), p);
+  };
+  fetch(i);  // (on its way while the angles are computed)
+  float wu[8], wv[8];
+  head_weight(a, which, p, wu, wv);
+  head_angles(a, t0, n_tokens, turn);
+  __syncthreads();
+  for (; i < units; i += step) {
+    const HeadUnit unit(set, i, by_count);
+    float u[8], v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        u[e] = in.r[0][e];
-        v[e] = in.r[1][e];
-      }
-      fetch(i + step);
-      const float rstd = head_stats<LANES>(u, v, p, c.centred, inv, c.eps);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        u[e] = u[e] * rstd * wu[e];
-        v[e] = v[e] * rstd * wv[e];
-      }
-      head_turn<INTERLEAVED>(u, v, turn + tok * a.pairs + p.pair, p, false);
-      if (p.n[0] > 0) store8(c.Y, y + p.at[0], p.n[0], u, !c.y_f32);
-      if (p.n[1] > 0) store8(c.Y, y + p.at[1], p.n[1], v, !c.y_f32);
+    for (int e = 0; e < 8; ++e) {
+      u[e] = in.r[0][e];
+      v[e] = in.r[1][e];
     }
+    fetch(i + step);
+    const float rstd = head_stats<LANES, WHOLE>(u, v, p, c.centred, inv, c.eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      u[e] = u[e] * rstd * wu[e];
+      v[e] = v[e] * rstd * wv[e];
+    }
+    head_turn<INTERLEAVED, WHOLE>(u, v, turn + unit.tok * a.pairs + p.pair, p, false);
+    head_store<WHOLE>(c.Y, unit.at(y_run, (int)c.y_token, (int)c.y_head), p, u, v, c.y_f32);
   }
 }
 
-// Blocks walk over groups of tokens and keep their shares of dw in registers; at the end the lane groups of a wave add theirs by
-// exchanges and the waves in LDS, in an order that does not change, and a second launch adds the blocks'.
-template <bool YF32, bool XF32, bool INTERLEAVED, int LANES>
+// A block keeps its share of dw in registers over its runs of tokens; at the end the lane groups of a wave add theirs by exchanges and the
+// waves in LDS, in an order that does not change, and a second launch adds the blocks'.
+template <bool YF32, bool XF32, bool INTERLEAVED, int LANES, bool WHOLE>
 __global__ void __launch_bounds__(kHeadThreads) head_norm_grad_kernel(const HeadArgs a) {
   __shared__ __attribute__((aligned(16))) float2 turn[kHeadPairs];
   __shared__ float totals[kHeadThreads / 64][kHeadMost];
   constexpr int GROUPS = kHeadThreads / LANES;
   const HeadNormCall& c = a.c;
-  const int k = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const HeadPiece p = head_piece<INTERLEAVED>(a, k);
-  const float inv = 1.f / (float)c.D;
-  float dw[2][2][8];
+  const int which = blockIdx.x >= a.set[0].blocks;
+  const HeadSet& set = a.set[which];
+  const int count = set.count;
+  const HeadPiece p = head_piece<INTERLEAVED>(a, threadIdx.x % LANES);
+  const float inv = 1.f / (float)c.D, by_count = 1.f / (float)count;
+  float wu[8], wv[8], dw[2][8];
+  head_weight(a, which, p, wu, wv);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) dw[i / 16][i / 8 % 2][i % 8] = 0.f;
-  for (int64_t g0 = blockIdx.x; g0 < a.groups; g0 += gridDim.x) {
-    const int64_t t0 = g0 * a.tokens;
-    const int n_tokens = (int)(c.T - t0 < a.tokens ? c.T - t0 : a.tokens);
-    __syncthreads();  // (the last group's angles have been read)
+  for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.f;
+  HeadRaw<XF32, WHOLE> x_in;
+  HeadRaw<YF32, WHOLE> y_in;
+  x_in.clear();
+  y_in.clear();
+  for (int64_t t0 = (blockIdx.x - (which ? a.set[0].blocks : 0)) * set.tokens; t0 < c.T; t0 += set.blocks * set.tokens) {
+    const int n_tokens = (int)(c.T - t0 < set.tokens ? c.T - t0 : set.tokens), units = n_tokens * count;
+    const int64_t x_run = t0 * c.x_token, dy_run = t0 * c.dy_token, y_run = t0 * c.y_token;
+    auto fetch = [&](int at) {
+      if (at >= units) return;
+      const HeadUnit unit(set, at, by_count);
+      x_in.load(c.X, unit.at(x_run, (int)c.x_token, (int)c.x_head), p);
+      y_in.load(c.dY, unit.at(dy_run, (int)c.dy_token, (int)c.dy_head), p);
+    };
+    int i = threadIdx.x / LANES;
+    fetch(i);
+    __syncthreads();  // (the last run's angles have been read)
     head_angles(a, t0, n_tokens, turn);
     __syncthreads();
+    for (; i < units; i += GROUPS) {
+      const HeadUnit unit(set, i, by_count);
+      float u[8], v[8], du[8], dv[8];
 #pragma unroll
-    for (int set = 0; set < 2; ++set) {
-      const int first = set ? (int)c.heads : 0, count = set ? (int)(c.H - c.heads) : (int)c.heads;
-      if (count == 0) continue;
-      const float by_count = 1.f / (float)count;
-      const int units = n_tokens * count;
-      HeadRaw<XF32> x_in;
-      HeadRaw<YF32> y_in;
-      auto fetch = [&](int i) {
-        if (i >= units) return;
-        const int tok = head_quotient(i, by_count);
-        const int64_t head = first + i - tok * count;
-        x_in.load(c.X, (t0 + tok) * c.x_token + head * c.x_head, p);
-        y_in.load(c.dY, (t0 + tok) * c.dy_token + head * c.dy_head, p);
-      };
-      fetch(group);
-      float wu[8], wv[8];
-      head_weight(a, set, p, wu, wv);
-      for (int i = group; i < units; i += GROUPS) {
-        const int tok = head_quotient(i, by_count);
-        const int64_t out = (t0 + tok) * c.y_token + (int64_t)(first + i - tok * count) * c.y_head;
-        float u[8], v[8], du[8], dv[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          u[e] = x_in.r[0][e];
-          v[e] = x_in.r[1][e];
-          du[e] = y_in.r[0][e];
-          dv[e] = y_in.r[1][e];
-        }
-        fetch(i + GROUPS);
-        const float rstd = head_stats<LANES>(u, v, p, c.centred, inv, c.eps);
-        head_turn<INTERLEAVED>(du, dv, turn + tok * a.pairs + p.pair, p, true);
-        float sum_g = 0.f, sum_gn = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {  // (elements past the head: n and d are zero)
-          u[e] *= rstd;
-          v[e] *= rstd;
-          dw[set][0][e] = fmaf(du[e], u[e], dw[set][0][e]);
-          dw[set][1][e] = fmaf(dv[e], v[e], dw[set][1][e]);
-          du[e] *= wu[e];
-          dv[e] *= wv[e];
-          sum_g += du[e] + dv[e];
-          sum_gn = fmaf(du[e], u[e], fmaf(dv[e], v[e], sum_gn));
-        }
-        sum_gn = head_sum<LANES>(sum_gn) * inv;
-        sum_g = c.centred ? head_sum<LANES>(sum_g) * inv : 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          du[e] = rstd * (du[e] - sum_g - u[e] * sum_gn);
-          dv[e] = rstd * (dv[e] - sum_g - v[e] * sum_gn);
-        }
-        if (p.n[0] > 0) store8(c.Y, out + p.at[0], p.n[0], du, !c.y_f32);
-        if (p.n[1] > 0) store8(c.Y, out + p.at[1], p.n[1], dv, !c.y_f32);
+      for (int e = 0; e < 8; ++e) {
+        u[e] = x_in.r[0][e];
+        v[e] = x_in.r[1][e];
+        du[e] = y_in.r[0][e];
+        dv[e] = y_in.r[1][e];
       }
+      fetch(i + GROUPS);
+      const float rstd = head_stats<LANES, WHOLE>(u, v, p, c.centred, inv, c.eps);
+      head_turn<INTERLEAVED, WHOLE>(du, dv, turn + unit.tok * a.pairs + p.pair, p, true);
+      float sum_g = 0.f, sum_gn = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {  // (elements past the head: n and d are zero)
+        u[e] *= rstd;
+        v[e] *= rstd;
+        dw[0][e] = fmaf(du[e], u[e], dw[0][e]);
+        dw[1][e] = fmaf(dv[e], v[e], dw[1][e]);
+        du[e] *= wu[e];
+        dv[e] *= wv[e];
+        sum_g += du[e] + dv[e];
+        sum_gn = fmaf(du[e], u[e], fmaf(dv[e], v[e], sum_gn));
+      }
+      sum_gn = head_sum<LANES>(sum_gn) * inv;
+      sum_g = c.centred ? head_sum<LANES>(sum_g) * inv : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        du[e] = rstd * (du[e] - sum_g - u[e] * sum_gn);
+        dv[e] = rstd * (dv[e] - sum_g - v[e] * sum_gn);
+      }
+      head_store<WHOLE>(c.Y, unit.at(y_run, (int)c.y_token, (int)c.y_head), p, du, dv, c.y_f32);
     }
   }
-  if (c.dw == nullptr) return;
-  const int sets = c.heads < c.H ? 2 : 1, wave = threadIdx.x >> 6;
+  if (a.partial == nullptr) return;
+  const int wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int set = 0; set < 2; ++set) {
-    if (set >= sets) break;
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int m = LANES; m < 64; m <<= 1) dw[i / 8][i % 8] += __shfl_xor(dw[i / 8][i % 8], m, 64);
+  if ((threadIdx.x & 63) < LANES) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-#pragma unroll
-      for (int m = LANES; m < 64; m <<= 1) dw[set][i / 8][i % 8] += __shfl_xor(dw[set][i / 8][i % 8], m, 64);
-    if ((threadIdx.x & 63) < LANES) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i % 8 < p.n[i / 8]) totals[wave][p.at[i / 8] + i % 8] = dw[set][i / 8][i % 8];
-    }
-    __syncthreads();
-    float* out = (a.partial ? a.partial + (int64_t)blockIdx.x * sets * c.D : c.dw) + set * c.D;
-    for (int d = threadIdx.x; d < (int)c.D; d += kHeadThreads) out[d] = (totals[0][d] + totals[1][d]) + (totals[2][d] + totals[3][d]);
-    __syncthreads();
+      if (i % 8 < p.n[i / 8]) totals[wave][p.at[i / 8] + i % 8] = dw[i / 8][i % 8];
   }
+  __syncthreads();
+  float* out = a.partial + (int64_t)blockIdx.x * c.D;
+  for (int d = threadIdx.x; d < (int)c.D; d += kHeadThreads) out[d] = (totals[0][d] + totals[1][d]) + (totals[2][d] + totals[3][d]);
 }
 
-// The blocks' sums in order: 16 columns to a block, the rows shared by 64 lanes per column, then a tree over the 64.
+// The blocks' sums in order: 16 columns of a set to a block, the rows shared by 64 lanes per column, then a tree over the 64.
 constexpr int kHeadSumCols = 16, kHeadSumRows = 64;
-__global__ void __launch_bounds__(kHeadSumCols * kHeadSumRows) head_norm_sum_kernel(const float* partial, int blocks, int cols, float* dw) {
+__global__ void __launch_bounds__(kHeadSumCols * kHeadSumRows) head_norm_sum_kernel(const HeadArgs a) {
   __shared__ float part[kHeadSumRows][kHeadSumCols + 1];
-  const int col = threadIdx.x % kHeadSumCols, r = threadIdx.x / kHeadSumCols;
-  const int at = blockIdx.x * kHeadSumCols + col;
+  const int col = threadIdx.x % kHeadSumCols, r = threadIdx.x / kHeadSumCols, cols = (int)a.c.D;
+  const int at = blockIdx.x * kHeadSumCols + col, set = blockIdx.y, blocks = (int)a.set[set].blocks;
+  const float* partial = a.partial + (set ? a.set[0].blocks * cols : 0);
   float v = 0.f;
   if (at < cols) {
 #pragma unroll 8
@@ -338,7 +361,7 @@ __global__ void __launch_bounds__(kHeadSumCols * kHeadSumRows) head_norm_sum_ker
     if (r < half) part[r][col] += part[r + half][col];
     __syncthreads();
   }
-  if (r == 0 && at < cols) dw[at] = part[0][col];
+  if (r == 0 && at < cols) a.c.dw[(int64_t)set * cols + at] = part[0][col];
 }
 
 // Lanes that hold a head, 16 elements each.
@@ -346,6 +369,8 @@ int head_lanes(int64_t D, int64_t R) {
   const int64_t pieces = (R / 2 + 7) / 8 + (D - R + 15) / 16;
   return pieces <= 4 ? 4 : pieces <= 8 ? 8 : pieces <= 16 ? 16 : 64;  // (at most 34 pieces)
 }
+// Whether all runs of eight elements are whole.
+bool head_whole(const HeadNormCall& c) { return (c.interleaved ? c.R : c.R / 2) % 8 == 0 && (c.D - c.R) % 8 == 0; }
 template <int N> struct Lanes { static constexpr int value = N; };
 template <class F>
 void with_lanes(int lanes, F&& f) {
@@ -360,27 +385,40 @@ void with_flag(bool on, F&& f) {
   else f(std::false_type{});
 }
 
-// Tokens that a block takes at a time: two heads for each of its lane groups, as far as their cosines fit and blocks are left for the chip.
-int head_tokens(int64_t T, int64_t H, int lanes, int64_t pairs) {
+// How a set's heads go to blocks: kHeadTurns of them to each lane group of a block at a time, as far as its tokens' cosines fit and blocks are
+// left for the chip.
+constexpr int64_t kHeadTurns = 4, kHeadBlocks = 1024;
+HeadSet head_set(int64_t T, int first, int count, int lanes, int64_t pairs) {
+  HeadSet s = {first, count, 1, 1, 0};
+  if (count == 0) return s;
   const int64_t groups = kHeadThreads / lanes;
-  int64_t tokens = (2 * groups + H - 1) / H;
+  int64_t tokens = kHeadTurns * groups / count;
   if (pairs > 0 && tokens > kHeadPairs / pairs) tokens = kHeadPairs / pairs;
-  const int64_t spread = (T + 1023) / 1024;
-  return (int)(tokens < spread ? tokens : spread);
+  const int64_t spread = (T * count + kHeadBlocks * groups - 1) / (kHeadBlocks * groups) * groups / count;  // (whole turns of the groups)
+  if (tokens > spread) tokens = spread;
+  s.tokens = (int)(tokens > 1 ? tokens : 1);
+  s.blocks = (T + s.tokens - 1) / s.tokens;
+  return s;
 }
-constexpr int64_t kHeadGradBlocks = 1024;  // which keep sums of dw
-int64_t head_grad_blocks(int64_t T, int64_t H, int64_t D, int64_t R) {
-  const int64_t tokens = head_tokens(T, H, head_lanes(D, R), R / 2), groups = (T + tokens - 1) / tokens;
-  return groups < kHeadGradBlocks ? groups : kHeadGradBlocks;
-}
-HeadArgs head_args(const HeadNormCall& c, int lanes) {
+HeadArgs head_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
   HeadArgs a = {};
-  a.c = c;
-  a.pairs = (int)(c.R / 2);
+  a.pairs = (int)(R / 2);
   a.rotate = (a.pairs + 7) / 8;
-  a.tokens = head_tokens(c.T, c.H, lanes, a.pairs);
-  a.groups = (c.T + a.tokens - 1) / a.tokens;
-  a.splits = 1;
+  const int lanes = head_lanes(D, R);
+  a.set[0] = head_set(T, 0, (int)heads, lanes, a.pairs);
+  a.set[1] = head_set(T, (int)heads, (int)(H - heads), lanes, a.pairs);
+  return a;
+}
+// Blocks of the backward pass, each with a row of sums: no more than the chip holds, by the sets' heads.
+HeadArgs head_grad_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
+  HeadArgs a = head_args(T, H, heads, D, R);
+  for (HeadSet& s : a.set) {
+    const int64_t most = (kHeadBlocks * s.count + H - 1) / H, room = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs;
+    if (s.blocks <= most) continue;
+    const int64_t runs = (T + most * room - 1) / (most * room);  // of each block, all as long
+    s.tokens = (int)((T + most * runs - 1) / (most * runs));
+    s.blocks = (T + s.tokens * runs - 1) / (s.tokens * runs);
+  }
   return a;
 }
 
@@ -388,44 +426,54 @@ HeadArgs head_args(const HeadNormCall& c, int lanes) {
 
 hipError_t launch_head_norm(const HeadNormCall& c, hipStream_t s) {
   const int lanes = head_lanes(c.D, c.R);
-  HeadArgs a = head_args(c, lanes);
-  const int64_t groups = kHeadThreads / lanes, most = (c.H + groups - 1) / groups;
-  if (a.tokens == 1 && a.groups < 1024) a.splits = (int)(most < 16 ? most : 16);
-  const dim3 grid = flat_grid_256(a.groups * a.splits * kHeadThreads);
+  HeadArgs a = head_args(c.T, c.H, c.heads, c.D, c.R);
+  a.c = c;
+  const int64_t groups = kHeadThreads / lanes;
+  for (HeadSet& set : a.set)
+    if (set.tokens == 1 && set.blocks < kHeadBlocks) {  // few tokens: a head to a lane group
+      const int64_t splits = (set.count + groups - 1) / groups;
+      set.splits = (int)(splits < 16 ? splits : 16);
+      set.blocks *= set.splits;
+    }
+  const dim3 grid = flat_grid_256((a.set[0].blocks + a.set[1].blocks) * kHeadThreads);
   with_lanes(lanes, [&](auto l) {
     with_flag(c.interleaved, [&](auto i) {
       with_flag(c.x_f32, [&](auto x) {
-        head_norm_kernel<decltype(x)::value, decltype(i)::value, decltype(l)::value><<<grid, kHeadThreads, 0, s>>>(a);
+        with_flag(head_whole(c), [&](auto w) {
+          head_norm_kernel<decltype(x)::value, decltype(i)::value, decltype(l)::value, decltype(w)::value><<<grid, kHeadThreads, 0, s>>>(a);
+        });
       });
     });
   });
   return hipGetLastError();
 }
 
-size_t head_norm_grad_workspace_bytes(int64_t T, int64_t H, int64_t D, int64_t R, int sets) {
-  const int64_t blocks = head_grad_blocks(T, H, D, R);
-  return blocks > 1 ? (size_t)blocks * sets * (size_t)D * sizeof(float) : 0;
+size_t head_norm_grad_workspace_bytes(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
+  const HeadArgs a = head_grad_args(T, H, heads, D, R);
+  return (size_t)(a.set[0].blocks + a.set[1].blocks) * (size_t)D * sizeof(float);
 }
 
 hipError_t launch_head_norm_grad(const HeadNormCall& c, hipStream_t s) {
   const int lanes = head_lanes(c.D, c.R);
-  HeadArgs a = head_args(c, lanes);
-  const int64_t blocks = head_grad_blocks(c.T, c.H, c.D, c.R);
-  a.partial = c.dw != nullptr && blocks > 1 ? static_cast<float*>(c.workspace) : nullptr;
+  HeadArgs a = head_grad_args(c.T, c.H, c.heads, c.D, c.R);
+  a.c = c;
+  const unsigned blocks = (unsigned)(a.set[0].blocks + a.set[1].blocks);
+  if (c.dw != nullptr) a.partial = blocks > 1 ? static_cast<float*>(c.workspace) : c.dw;
   with_lanes(lanes, [&](auto l) {
     with_flag(c.interleaved, [&](auto i) {
       with_flag(c.x_f32, [&](auto x) {
         with_flag(c.dy_f32, [&](auto y) {
-          head_norm_grad_kernel<decltype(y)::value, decltype(x)::value, decltype(i)::value, decltype(l)::value>
-              <<<dim3((unsigned)blocks), kHeadThreads, 0, s>>>(a);
+          with_flag(head_whole(c), [&](auto w) {
+            head_norm_grad_kernel<decltype(y)::value, decltype(x)::value, decltype(i)::value, decltype(l)::value, decltype(w)::value>
+                <<<dim3(blocks), kHeadThreads, 0, s>>>(a);
+          });
         });
       });
     });
   });
-  if (a.partial != nullptr) {
-    const int cols = (int)(c.heads < c.H ? 2 * c.D : c.D);
-    head_norm_sum_kernel<<<dim3((unsigned)((cols + kHeadSumCols - 1) / kHeadSumCols)), kHeadSumCols * kHeadSumRows, 0, s>>>(
-        a.partial, (int)blocks, cols, c.dw);
+  if (c.dw != nullptr && blocks > 1) {
+    const dim3 grid((unsigned)((c.D + kHeadSumCols - 1) / kHeadSumCols), c.heads < c.H ? 2 : 1);
+    head_norm_sum_kernel<<<grid, kHeadSumCols * kHeadSumRows, 0, s>>>(a);
   }
   return hipGetLastError();
 }

@@ -321,7 +321,7 @@ struct HeadNormCall {
   void* workspace;        // head_norm_grad_workspace_bytes, needed where dw is asked for
 };
 hipError_t launch_head_norm(const HeadNormCall& c, hipStream_t s);
-size_t head_norm_grad_workspace_bytes(int64_t T, int64_t H, int64_t D, int64_t R, int sets);
+size_t head_norm_grad_workspace_bytes(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R);
 hipError_t launch_head_norm_grad(const HeadNormCall& c, hipStream_t s);
 
 // nm_pages.hip, nm_paged.hip: a cache of keys and values in pages.  Strides in elements (of bfloat16, of codes, of exponent bytes).

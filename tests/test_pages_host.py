@@ -38,7 +38,7 @@ def head_norm(lib, backward=False, ws=FAKE, bytes=1 << 40, sections=(16, 16), **
     (dict(H=2 ** 15, D=512, heads=1), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE),
     (dict(rotated=66), SHAPE), (dict(rotated=63), SHAPE), (dict(rotated=0), SHAPE), (dict(axes=0), SHAPE), (dict(axes=5), SHAPE),
     (dict(sections=(16, 15)), SHAPE), (dict(sections=(33, -1)), SHAPE), (dict(X=TH(FAKE, -256, 64, BF16, 0)), SHAPE),
-    (dict(Y=TH(FAKE, 255, 64, BF16, 0)), SHAPE), (dict(Y=TH(FAKE, 256, 63, BF16, 0)), SHAPE), (dict(X=TH(FAKE, 256, 64, I32, 0)), DTYPE),
+    (dict(Y=TH(FAKE, 255, 64, BF16, 0)), SHAPE), (dict(X=TH(FAKE, 2 ** 31, 64, BF16, 0)), SHAPE), (dict(Y=TH(FAKE, 256, 63, BF16, 0)), SHAPE), (dict(X=TH(FAKE, 256, 64, I32, 0)), DTYPE),
     (dict(Y=TH(FAKE, 256, 64, E4M3, 0)), DTYPE), (dict(X=TH(FAKE + 1, 256, 64, BF16, 0)), ALIGN), (dict(Y=TH(FAKE + 2, 256, 64, F32, 0)), ALIGN),
     (dict(weight=FAKE + 2), ALIGN), (dict(positions=FAKE + 1), ALIGN), (dict(freqs=FAKE + 2), ALIGN)])
 def test_head_norm_refusals(lib, backward, kw, status):
@@ -60,11 +60,10 @@ def test_head_norm_backward_refusals(lib):
 
 def test_head_norm_workspace(lib):
     size = lib.nm_head_norm_backward_workspace_bytes
-    assert size(1, 4, 3, 64, 64) == 0 and size(0, 4, 3, 64, 64) == 0 and size(9, 4, 5, 64, 64) == 0 and size(9, 4, 3, 64, 65) == 0
+    assert size(1, 4, 4, 64, 64) == 256 and size(0, 4, 3, 64, 64) == 0 and size(9, 4, 5, 64, 64) == 0 and size(9, 4, 3, 64, 65) == 0
     assert size(9, 4, 3, 513, 0) == 0 and size(9, 4, 3, 64, 66) == 0 and size(9, 0, 0, 64, 0) == 0
     many = size(10 ** 6, 4, 3, 64, 64)
-    assert many > 0 and many % (2 * 64 * 4) == 0
-    assert size(10 ** 6, 4, 4, 64, 64) * 2 == many  # (one row of weights)
+    assert many > 0 and many % (64 * 4) == 0 and size(10 ** 7, 4, 3, 64, 64) <= 2 * many  # (a row of sums to each of so many blocks)
 
 
 def pages(codes=True, **kw):
