@@ -72,10 +72,10 @@ struct HeadUnit {
   __device__ __forceinline__ int64_t at(int64_t run, int token, int heads) const { return run + (int64_t)tok * token + (int64_t)head * heads; }
 };
 
-// The two runs of eight elements that lane k of a head holds: where they begin, how many there are (<= 0: none), and the first of its
-// pairs in the table of a token's turns.
+// The two runs of eight elements that lane k of a head holds: where they begin, how many there are (<= 0: none), and the first of their
+// pairs in the table of a token's turns.  Lanes side by side hold runs side by side, so that an access covers whole lines.
 struct HeadPiece {
-  int at[2], n[2], pair;
+  int at[2], n[2], pair[2];
   bool turned;
 };
 template <bool INTERLEAVED>
@@ -83,16 +83,19 @@ __device__ __forceinline__ HeadPiece head_piece(const HeadArgs& a, int k) {
   HeadPiece p;
   const int D = (int)a.c.D;
   p.turned = k < a.rotate;
-  p.pair = k * 8;
-  if (!INTERLEAVED && p.turned) {
-    p.at[0] = k * 8;
+  if (!INTERLEAVED && p.turned) {  // both members of eight pairs
+    p.pair[0] = p.pair[1] = p.at[0] = k * 8;
     p.at[1] = a.pairs + k * 8;
     p.n[0] = p.n[1] = a.pairs - k * 8;
-  } else {
-    p.at[0] = p.turned ? k * 16 : 2 * a.pairs + (k - a.rotate) * 16;
-    p.at[1] = p.at[0] + 8;
-    p.n[0] = (p.turned ? 2 * a.pairs : D) - p.at[0];
-    p.n[1] = p.n[0] - 8;
+  } else {                         // twice four pairs, or what is not turned
+    const int from = p.turned ? 0 : 2 * a.pairs, to = p.turned ? 2 * a.pairs : D, lanes = p.turned ? a.rotate : (D - from + 15) / 16;
+    const int i = p.turned ? k : k - a.rotate;
+    p.at[0] = from + i * 8;
+    p.at[1] = from + (lanes + i) * 8;
+    p.n[0] = i < lanes ? to - p.at[0] : 0;
+    p.n[1] = i < lanes ? to - p.at[1] : 0;
+    p.pair[0] = p.at[0] / 2;
+    p.pair[1] = p.at[1] / 2;
   }
   return p;
 }
@@ -124,23 +127,26 @@ __device__ __forceinline__ void head_store(void* base, int64_t row, const HeadPi
   if (p.n[1] > 0) store8(base, row + p.at[1], WHOLE ? 8 : p.n[1], v, !f32);
 }
 
-// The turn of a lane's pairs, back where `back`.
+// The turn of a lane's pairs, back where `back`; w: the token's cosines and sines.
 template <bool INTERLEAVED, bool WHOLE>
 __device__ __forceinline__ void head_turn(float (&u)[8], float (&v)[8], const float2* w, const HeadPiece& p, bool back) {
   if (!p.turned) return;
   if constexpr (INTERLEAVED) {
+    auto run = [&](float (&q)[8], int r) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float* q = e < 4 ? u + 2 * e : v + 2 * e - 8;
-      const float2 cs = 2 * e < p.n[0] ? w[e] : float2{1.f, 0.f};
-      const float sn = back ? -cs.y : cs.y, x = q[0], y = q[1];
-      q[0] = x * cs.x - y * sn;
-      q[1] = y * cs.x + x * sn;
-    }
+      for (int e = 0; e < 4; ++e) {
+        const float2 cs = (WHOLE ? 0 : 2 * e) < p.n[r] ? w[p.pair[r] + e] : float2{1.f, 0.f};
+        const float sn = back ? -cs.y : cs.y, x = q[2 * e], y = q[2 * e + 1];
+        q[2 * e] = x * cs.x - y * sn;
+        q[2 * e + 1] = y * cs.x + x * sn;
+      }
+    };
+    run(u, 0);
+    run(v, 1);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float2 cs = WHOLE || e < p.n[0] ? w[e] : float2{1.f, 0.f};
+      const float2 cs = WHOLE || e < p.n[0] ? w[p.pair[0] + e] : float2{1.f, 0.f};
       const float sn = back ? -cs.y : cs.y, x = u[e], y = v[e];
       u[e] = x * cs.x - y * sn;
       v[e] = y * cs.x + x * sn;
@@ -148,25 +154,56 @@ __device__ __forceinline__ void head_turn(float (&u)[8], float (&v)[8], const fl
   }
 }
 
-// Cosines and sines of the pairs of n_tokens tokens from t0 on.
-__device__ __forceinline__ void head_angles(const HeadArgs& a, int64_t t0, int n_tokens, float2* turn) {
-  const HeadNormCall& c = a.c;
-  if (a.pairs == 0) return;
-  const float by_pairs = 1.f / (float)a.pairs;
-  for (int i = threadIdx.x; i < n_tokens * a.pairs; i += kHeadThreads) {
+// Cosines and sines of the pairs of n_tokens tokens from t0 on, in two halves: what they are computed from is asked for before the heads'
+// elements are, since loads come back in order (64 images 17.3 us, 18.1 asked for after them), where registers allow.
+struct HeadAngle {
+  uint32_t position;
+  float freq;
+  __device__ __forceinline__ void load(const HeadArgs& a, int64_t t0, int i, float by_pairs) {
+    const HeadNormCall& c = a.c;
     const int tok = head_quotient(i, by_pairs), pair = i - tok * a.pairs;
     int axis = 0;
 #pragma unroll
     for (int x = 0; x < kMaxRotaryAxes - 1; ++x) axis += pair >= c.section_end[x] ? 1 : 0;
-    const int64_t at = (t0 + tok) * c.axes + axis;
-    const double pos = c.positions_f32 ? (double)static_cast<const float*>(c.positions)[at]
-                                       : (double)static_cast<const int32_t*>(c.positions)[at];
-    const double turns = pos * (double)c.freqs[pair] * 0.15915494309189533577;  // (1 / 2 pi)
+    position = static_cast<const uint32_t*>(c.positions)[(t0 + tok) * c.axes + axis];
+    freq = c.freqs[pair];
+  }
+  __device__ __forceinline__ void store(const HeadArgs& a, int i, float2* turn) const {
+    const double pos = a.c.positions_f32 ? (double)__uint_as_float(position) : (double)(int32_t)position;
+    const double turns = pos * (double)freq * 0.15915494309189533577;  // (1 / 2 pi)
     float sn, cs;
     sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
     turn[i] = float2{cs, sn};
   }
-}
+};
+template <bool EARLY>
+struct HeadAngles {
+  static constexpr int kMost = kHeadPairs / kHeadThreads;
+  HeadAngle each[EARLY ? kMost : 1];
+  __device__ __forceinline__ void load(const HeadArgs& a, int64_t t0, int n_tokens) {
+    if (!EARLY || a.pairs == 0) return;
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+      const int i = k * kHeadThreads + threadIdx.x;
+      if (i < n_tokens * a.pairs) each[k].load(a, t0, i, 1.f / (float)a.pairs);
+    }
+  }
+  __device__ __forceinline__ void store(const HeadArgs& a, int64_t t0, int n_tokens, float2* turn) {
+    if constexpr (EARLY) {
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) {
+        const int i = k * kHeadThreads + threadIdx.x;
+        if (i < n_tokens * a.pairs) each[k].store(a, i, turn);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = threadIdx.x; i < n_tokens * a.pairs; i += kHeadThreads) {
+        each[0].load(a, t0, i, 1.f / (float)a.pairs);
+        each[0].store(a, i, turn);
+      }
+    }
+  }
+};
 
 // c = x (- mean) and 1 / sqrt(mean(c^2) + eps) of a head; elements past it stay zero.
 template <int LANES, bool WHOLE>
@@ -232,10 +269,12 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_kernel(const HeadArgs 
   auto fetch = [&](int at) {
     if (at < units) in.load(c.X, HeadUnit(set, at, by_count).at(x_run, (int)c.x_token, (int)c.x_head), p);
   };
-  fetch(i);  // (on its way while the angles are computed)
+  HeadAngles<true> angles;
+  angles.load(a, t0, n_tokens);
+  fetch(i);  // (on its way while the angles are computed; two units ahead took 19.5 us for 18.1 of 64 images)
   float wu[8], wv[8];
   head_weight(a, which, p, wu, wv);
-  head_angles(a, t0, n_tokens, turn);
+  angles.store(a, t0, n_tokens, turn);
   __syncthreads();
   for (; i < units; i += step) {
     const HeadUnit unit(set, i, by_count);
@@ -252,7 +291,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_kernel(const HeadArgs 
       u[e] = u[e] * rstd * wu[e];
       v[e] = v[e] * rstd * wv[e];
     }
-    head_turn<INTERLEAVED, WHOLE>(u, v, turn + unit.tok * a.pairs + p.pair, p, false);
+    head_turn<INTERLEAVED, WHOLE>(u, v, turn + unit.tok * a.pairs, p, false);
     head_store<WHOLE>(c.Y, unit.at(y_run, (int)c.y_token, (int)c.y_head), p, u, v, c.y_f32);
   }
 }
@@ -260,7 +299,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_kernel(const HeadArgs 
 // A block keeps its share of dw in registers over its runs of tokens; at the end the lane groups of a wave add theirs by exchanges and the
 // waves in LDS, in an order that does not change, and a second launch adds the blocks'.
 template <bool YF32, bool XF32, bool INTERLEAVED, int LANES, bool WHOLE>
-__global__ void __launch_bounds__(kHeadThreads) head_norm_grad_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kHeadThreads, 3) head_norm_grad_kernel(const HeadArgs a) {
   __shared__ __attribute__((aligned(16))) float2 turn[kHeadPairs];
   __shared__ float totals[kHeadThreads / 64][kHeadMost];
   constexpr int GROUPS = kHeadThreads / LANES;
@@ -288,9 +327,11 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_grad_kernel(const Head
       y_in.load(c.dY, unit.at(dy_run, (int)c.dy_token, (int)c.dy_head), p);
     };
     int i = threadIdx.x / LANES;
+    HeadAngles<!XF32 && !YF32> angles;
+    angles.load(a, t0, n_tokens);
     fetch(i);
     __syncthreads();  // (the last run's angles have been read)
-    head_angles(a, t0, n_tokens, turn);
+    angles.store(a, t0, n_tokens, turn);
     __syncthreads();
     for (; i < units; i += GROUPS) {
       const HeadUnit unit(set, i, by_count);
@@ -304,7 +345,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_grad_kernel(const Head
       }
       fetch(i + GROUPS);
       const float rstd = head_stats<LANES, WHOLE>(u, v, p, c.centred, inv, c.eps);
-      head_turn<INTERLEAVED, WHOLE>(du, dv, turn + unit.tok * a.pairs + p.pair, p, true);
+      head_turn<INTERLEAVED, WHOLE>(du, dv, turn + unit.tok * a.pairs, p, true);
       float sum_g = 0.f, sum_gn = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {  // (elements past the head: n and d are zero)
@@ -385,9 +426,9 @@ void with_flag(bool on, F&& f) {
   else f(std::false_type{});
 }
 
-// How a set's heads go to blocks: kHeadTurns of them to each lane group of a block at a time, as far as its tokens' cosines fit and blocks are
+// How a set's heads go to blocks: kHeadTurns of them to each lane group (64 images 17.0 us with three, 17.4 with four and six) of a block at a time, as far as its tokens' cosines fit and blocks are
 // left for the chip.
-constexpr int64_t kHeadTurns = 4, kHeadBlocks = 1024;
+constexpr int64_t kHeadTurns = 3, kHeadBlocks = 1024, kHeadGradBlocks = 768;
 HeadSet head_set(int64_t T, int first, int count, int lanes, int64_t pairs) {
   HeadSet s = {first, count, 1, 1, 0};
   if (count == 0) return s;
@@ -413,7 +454,7 @@ HeadArgs head_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
 HeadArgs head_grad_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
   HeadArgs a = head_args(T, H, heads, D, R);
   for (HeadSet& s : a.set) {
-    const int64_t most = (kHeadBlocks * s.count + H - 1) / H, room = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs;
+    const int64_t most = (kHeadGradBlocks * s.count + H - 1) / H, room = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs;
     if (s.blocks <= most) continue;
     const int64_t runs = (T + most * room - 1) / (most * room);  // of each block, all as long
     s.tokens = (int)((T + most * runs - 1) / (most * runs));
