@@ -63,6 +63,15 @@ __device__ __forceinline__ uint32_t encode2(uint32_t pair, float scale) {
   return (uint32_t)(uint16_t)r[0];
 }
 
+// Eight codes to four pairs.
+__device__ __forceinline__ u32x4_t decode8(uint32_t lo, uint32_t hi, uint32_t exponent) {
+  const float scale = __uint_as_float(exponent << 23);
+  return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+}
+
 // Sixteen codes of a row, from `at` on, of which n are there (<= 0: none; zeros past them).  Any alignment.
 __device__ __forceinline__ u32x4_t load_codes(const uint8_t* row, int at, int n) {
   u32x4_t v = {0, 0, 0, 0};
