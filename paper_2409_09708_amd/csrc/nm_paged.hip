@@ -609,9 +609,21 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
             }
         }
         few_softmax(s, a.scale_log2, ref, sum, acc);
-        const u32x4_t pr = {pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])};
+        // Probabilities go in as two bfloat16 each, the second what the first leaves: the matrix instructions have time for it here, and the
+        // result is as exact as its rounding (200 keys: relative error 0.0016, 0.0025 with one).
+        u32x4_t pr, rest;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = mma16(Value::columns(v_at, b), pr, acc[b]);
+        for (int i = 0; i < 4; ++i) {
+          const float lo = s[i / 2][i % 2 * 2], hi = s[i / 2][i % 2 * 2 + 1];
+          pr[i] = pack_bf16x2(lo, hi);
+          rest[i] = pack_bf16x2(lo - __uint_as_float(pr[i] << 16), hi - __uint_as_float(pr[i] & 0xFFFF0000u));
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const u32x4_t v = Value::columns(v_at, b);
+          acc[b] = mma16(v, pr, acc[b]);
+          acc[b] = mma16(v, rest, acc[b]);
+        }
         __builtin_amdgcn_wave_barrier();
       }
       // join the four waves: each scales its output to the common maximum, then the block adds them in wave order
@@ -684,7 +696,7 @@ __device__ __forceinline__ void join_parts(const PagedCall& c, const float* part
   for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
   float total = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
   for (int k = part; k < parts; k += GROUPS) {
     const float2 ml = part_ml[k * stride];
     const float by = part_weight(ml.x, top);
