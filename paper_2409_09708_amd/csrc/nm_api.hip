@@ -882,7 +882,8 @@ int32_t nm_attention_paged(const nm_paged_desc* d, void* workspace, size_t works
   const int64_t room = (int64_t)p.table_width * p.page_size;
   c.max_q = d->max_q < d->Tq ? d->max_q : d->Tq;
   c.max_k = d->max_k < room ? d->max_k : room;
-  c.window = d->window; c.sinks = d->sinks; c.scale = d->scale;
+  c.window = d->window < kMostPageTokens ? d->window : (int)kMostPageTokens;  // (no sequence is longer; positions less it fit 32 bits)
+  c.sinks = d->sinks; c.scale = d->scale;
   if (!workspace_ok(workspace, workspace_bytes, nm::paged_workspace_bytes(c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks)))
     return NM_ERR_WORKSPACE;
   c.workspace = workspace;

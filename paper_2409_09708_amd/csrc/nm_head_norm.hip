@@ -43,6 +43,7 @@ struct HeadArgs {
 };
 
 // i / d for 0 <= i < 2^21, from 1 / d: the quotient is at least 0.5 / d away from the next integer, the product off by less
+constexpr int64_t kHeadMostUnits = 1 << 20;  // (a token has no more heads)
 __device__ __forceinline__ int head_quotient(int i, float inverse) { return (int)(((float)i + 0.5f) * inverse); }
 
 // Sum over the LANES lanes of a head.  Up to 16 lanes the exchanges are operands of the additions: neighbours, pairs, then the halves of
@@ -454,8 +455,10 @@ HeadArgs head_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
 HeadArgs head_grad_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t R) {
   HeadArgs a = head_args(T, H, heads, D, R);
   for (HeadSet& s : a.set) {
-    const int64_t most = (kHeadGradBlocks * s.count + H - 1) / H, room = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs;
+    const int64_t most = (kHeadGradBlocks * s.count + H - 1) / H;
     if (s.blocks <= most) continue;
+    // tokens of a run: their cosines fit, and its heads are no more than head_quotient counts
+    const int64_t fit = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs, counted = kHeadMostUnits / s.count, room = fit < counted ? fit : counted;
     const int64_t runs = (T + most * room - 1) / (most * room);  // of each block, all as long
     s.tokens = (int)((T + most * runs - 1) / (most * runs));
     s.blocks = (T + s.tokens * runs - 1) / (s.tokens * runs);

@@ -486,7 +486,7 @@ __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int
       const int tiles = __builtin_amdgcn_readlane(u->tiles, l);
       const int64_t first = steps_before + lane_value(u->upto, l) - (int64_t)p.steps * tiles;
       p.tile = tiles == 1 ? 0 : (int)((at - first) / p.steps);
-      p.step = (int)(at - first) - p.tile * p.steps;
+      p.step = (int)(at - first - (int64_t)p.tile * p.steps);
       p.unit = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles + p.tile;
       return p;
     }
@@ -666,13 +666,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
           for (int w = 0; w < kWaves; ++w) l += wave_ml[w][cc].y * part_weight(wave_ml[w][cc].x, t);
           const float inv = l == 0.f ? 0.f : 1.f / l;
           store4(c.O.p + tok * c.O.token + hd * c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-        } else if (slot < a.slots) {  // (always, of offsets that do not decrease)
+        } else if ((uint32_t)slot < (uint32_t)a.slots) {  // (always, of offsets that do not decrease)
           *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kCols + cc) * DP + d) = o;
         }
       }
       if (wave == 0 && quarter == 0 && live) {
         if (!alone) {
-          if (slot < a.slots) a.part_ml[(int64_t)slot * kCols + col] = float2{top, total};
+          if ((uint32_t)slot < (uint32_t)a.slots) a.part_ml[(int64_t)slot * kCols + col] = float2{top, total};
         } else if (c.lse != nullptr) {
           c.lse[(int64_t)head * c.Tq + of.q0 + qi] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
         }
@@ -721,7 +721,7 @@ __device__ __forceinline__ void join_parts(const PagedCall& c, const float* part
 template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a) {
   const FewShared u = a.shared[blockIdx.x];
-  if (u.parts == 0 || u.slot + u.parts > a.slots) return;
+  if (u.parts <= 0 || (uint32_t)u.slot >= (uint32_t)a.slots || u.parts > a.slots - u.slot) return;
   for (int col = blockIdx.y * kWaves + (threadIdx.x >> 6); col < kCols && u.tile * kCols + col < u.columns; col += gridDim.y * kWaves) {
     const int n = u.tile * kCols + col;
     const int64_t at = (int64_t)u.slot * kCols + col;

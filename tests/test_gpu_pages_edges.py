@@ -1,0 +1,36 @@
+"""The norm of heads and attention over pages at the ends of what their arguments may be."""
+import pytest
+import torch
+
+import paper_2409_09708_amd as nm
+from pages_reference import Cache
+from test_gpu_paged import check
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("window", [2 ** 30, 2 ** 31 - 1])
+@pytest.mark.parametrize("counts", [[6, 3], [40, 90], [200, 70]])
+def test_widest_window_where_queries_stand_before_the_first_token(counts, window, codes):
+    """(more new tokens than the sequence is said to have: the first of them have negative positions and see nothing)"""
+    cache = Cache([4, 66], 300, 2, 64, 16, codes).fill(window % 97)
+    o = check(cache, counts, 4, window=window, sinks=3, max_q=max(counts))
+    assert torch.equal(o, check(cache, counts, 4, max_q=max(counts)))
+    check(cache, counts, 4, sinks=2 ** 31 - 1, window=1, max_q=max(counts))
+
+
+def test_norm_gradient_of_very_many_heads():
+    H, T = 2 ** 17, 768 * 20
+    g = torch.Generator("cuda").manual_seed(5)
+    x, dy = (torch.randn(1, H, 1, generator=g, device="cuda").to(BF16) for _ in range(2))
+    w = torch.full((1,), 1.5, device="cuda")
+    one, _ = nm.nm_head_norm_backward(dy, x, w, eps=1.0, params=False)
+    n = x.double() * (x.double().square() + 1).rsqrt()
+    want = (x.double().square() + 1).rsqrt() * (dy.double() * 1.5) * (1 - n * n)
+    # (the difference of 1 and n^2 = x^2 rstd^2 in 32 bits, then the rounding)
+    assert ((one.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * dy.double().abs()).all()
+    every, _ = nm.nm_head_norm_backward(dy.expand(T, H, 1), x.expand(T, H, 1), w, eps=1.0, params=False)
+    for t in range(0, T, 1024):
+        assert torch.equal(every[t:t + 1024], one.expand_as(every[t:t + 1024])), t
