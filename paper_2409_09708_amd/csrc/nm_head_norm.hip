@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kHeadThreads = 256;  // (flat_grid_256)
 constexpr int kHeadPairs = 1024;   // cosines and sines that a block keeps: 8 KiB
+constexpr int kGradPairs = 4096;   // ... of the backward pass: 32 KiB
 constexpr int kHeadMost = 512;     // elements of a head
 
 // The heads that share a row of weights: a block takes those of a run of tokens.
@@ -181,8 +182,9 @@ template <bool EARLY>
 struct HeadAngles {
   static constexpr int kMost = kHeadPairs / kHeadThreads;
   HeadAngle each[EARLY ? kMost : 1];
+  __device__ __forceinline__ bool early(const HeadArgs& a, int n_tokens) const { return EARLY && n_tokens * a.pairs <= kHeadPairs; }
   __device__ __forceinline__ void load(const HeadArgs& a, int64_t t0, int n_tokens) {
-    if (!EARLY || a.pairs == 0) return;
+    if (a.pairs == 0 || !early(a, n_tokens)) return;
 #pragma unroll
     for (int k = 0; k < kMost; ++k) {
       const int i = k * kHeadThreads + threadIdx.x;
@@ -190,9 +192,9 @@ struct HeadAngles {
     }
   }
   __device__ __forceinline__ void store(const HeadArgs& a, int64_t t0, int n_tokens, float2* turn) {
-    if constexpr (EARLY) {
+    if (early(a, n_tokens)) {
 #pragma unroll
-      for (int k = 0; k < kMost; ++k) {
+      for (int k = 0; k < (EARLY ? kMost : 1); ++k) {
         const int i = k * kHeadThreads + threadIdx.x;
         if (i < n_tokens * a.pairs) each[k].store(a, i, turn);
       }
@@ -301,7 +303,7 @@ __global__ void __launch_bounds__(kHeadThreads) head_norm_kernel(const HeadArgs 
 // waves in LDS, in an order that does not change, and a second launch adds the blocks'.
 template <bool YF32, bool XF32, bool INTERLEAVED, int LANES, bool WHOLE>
 __global__ void __launch_bounds__(kHeadThreads, 3) head_norm_grad_kernel(const HeadArgs a) {
-  __shared__ __attribute__((aligned(16))) float2 turn[kHeadPairs];
+  __shared__ __attribute__((aligned(16))) float2 turn[kGradPairs];
   __shared__ float totals[kHeadThreads / 64][kHeadMost];
   constexpr int GROUPS = kHeadThreads / LANES;
   const HeadNormCall& c = a.c;
@@ -458,7 +460,7 @@ HeadArgs head_grad_args(int64_t T, int64_t H, int64_t heads, int64_t D, int64_t 
     const int64_t most = (kHeadGradBlocks * s.count + H - 1) / H;
     if (s.blocks <= most) continue;
     // tokens of a run: their cosines fit, and its heads are no more than head_quotient counts
-    const int64_t fit = a.pairs > 0 ? kHeadPairs / a.pairs : kHeadPairs, counted = kHeadMostUnits / s.count, room = fit < counted ? fit : counted;
+    const int64_t fit = a.pairs > 0 ? kGradPairs / a.pairs : kGradPairs, counted = kHeadMostUnits / s.count, room = fit < counted ? fit : counted;
     const int64_t runs = (T + most * room - 1) / (most * room);  // of each block, all as long
     s.tokens = (int)((T + most * runs - 1) / (most * runs));
     s.blocks = (T + s.tokens * runs - 1) / (s.tokens * runs);
