@@ -884,7 +884,7 @@ int32_t nm_attention_paged(const nm_paged_desc* d, void* workspace, size_t works
   c.max_k = d->max_k < room ? d->max_k : room;
   c.window = d->window < kMostPageTokens ? d->window : (int)kMostPageTokens;  // (no sequence is longer; positions less it fit 32 bits)
   c.sinks = d->sinks; c.scale = d->scale;
-  if (!workspace_ok(workspace, workspace_bytes, nm::paged_workspace_bytes(c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks)))
+  if (!workspace_ok(workspace, workspace_bytes, nm::paged_workspace_bytes(c)))
     return NM_ERR_WORKSPACE;
   c.workspace = workspace;
   return device_status(nm::launch_paged(c, (hipStream_t)stream));

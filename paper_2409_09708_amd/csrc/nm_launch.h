@@ -362,7 +362,7 @@ struct PagedCall {
   float scale;
   void* workspace;
 };
-size_t paged_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks);
+size_t paged_workspace_bytes(const PagedCall& c);
 size_t paged_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q);  // ... of any max_k, window and sinks
 hipError_t launch_paged(const PagedCall& c, hipStream_t s);
 

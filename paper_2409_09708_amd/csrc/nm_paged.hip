@@ -964,7 +964,11 @@ __global__ void __launch_bounds__(kThreads) paged_chunk_join_kernel(const PagedA
 // ------------------------------------------------------------------------------------------------------
 // How a call is cut
 // ------------------------------------------------------------------------------------------------------
-constexpr int64_t kFewColumns = 64;            // (query, head) pairs of a key head up to which the first kernel serves
+// (query, head) pairs of a key head up to which the first kernel serves, of bfloat16 and of codes: it reads keys once per 16 of them, the second
+// once per 128 (16 heads on 4 of 128, two caches of 16384, first and second kernel, bfloat16: 16 columns 31.7 and 35.3 us, 32 36.0 and 35.3,
+// 48 44.4 and 36.6; codes, which come to LDS through registers in the second: 32 30.3 and 38.5, 64 37.2 and 40.3, 96 50.0 and 41.8;
+// 24 ragged caches: bfloat16 32 85 and 99, 64 100 and 102, codes 64 62 and 118).
+constexpr int64_t kFewColumns = 32, kFewColumnsCodes = 64;
 constexpr int64_t kFewSequences = 512;         // up to which lists are made
 constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences, likewise
 constexpr int64_t kFewBlocks = 512;            // blocks that the list is dealt to: two of each compute unit
@@ -1012,10 +1016,10 @@ int64_t paged_most_views(int64_t queries, int64_t max_k, int window, int sinks) 
   const int64_t some = (int64_t)window + sinks + queries;
   return some < max_k ? some : max_k;
 }
-PagedPlan paged_plan(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
+PagedPlan paged_plan(bool codes, int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
   PagedPlan p = {};
   const int64_t group = Hq / Hkv, units = (int64_t)B * Hkv;
-  p.few = max_q * group <= kFewColumns;
+  p.few = max_q * group <= (codes ? kFewColumnsCodes : kFewColumns);
   const int64_t per_tile = p.few ? kCols : kChunkColumns;
   p.n_tiles = (max_q * group + per_tile - 1) / per_tile;
   if (p.n_tiles < 1) p.n_tiles = 1;
@@ -1049,11 +1053,16 @@ size_t paged_bytes(size_t columns, int D) {
 
 }  // namespace
 
-size_t paged_workspace_bytes(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q, int64_t max_k, int window, int sinks) {
-  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, D, max_q, max_k, window, sinks).columns, D);
+size_t paged_workspace_bytes(const PagedCall& c) {
+  return paged_bytes(paged_plan(c.p.e4m3, c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks).columns, c.p.D);
 }
 size_t paged_workspace_most(int64_t Tq, int B, int Hq, int Hkv, int D, int64_t max_q) {
-  return paged_bytes(paged_plan(Tq, B, Hq, Hkv, D, max_q, 0, 0, 0).most_columns, D);
+  size_t most = 0;
+  for (const bool codes : {false, true}) {
+    const size_t columns = paged_plan(codes, Tq, B, Hq, Hkv, D, max_q, 0, 0, 0).most_columns;
+    most = columns > most ? columns : most;
+  }
+  return paged_bytes(most, D);
 }
 
 hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
@@ -1062,7 +1071,7 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   a.divide = page_divide(c.p.page_size);
   a.group = c.Hq / c.p.H;
   a.scale_log2 = c.scale * kLog2e;
-  const PagedPlan plan = paged_plan(c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks);
+  const PagedPlan plan = paged_plan(c.p.e4m3, c.Tq, c.p.B, c.Hq, c.p.H, c.p.D, c.max_q, c.max_k, c.window, c.sinks);
   a.n_tiles = (int)plan.n_tiles;
   a.cuts = plan.cuts;
   a.piece = plan.piece;

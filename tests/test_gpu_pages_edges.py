@@ -34,3 +34,14 @@ def test_norm_gradient_of_very_many_heads():
     every, _ = nm.nm_head_norm_backward(dy.expand(T, H, 1), x.expand(T, H, 1), w, eps=1.0, params=False)
     for t in range(0, T, 1024):
         assert torch.equal(every[t:t + 1024], one.expand_as(every[t:t + 1024])), t
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("L", [4, 7, 8, 9, 12, 15, 16, 17, 20])
+def test_one_size_of_workspace_for_both_types(L, codes):
+    """(sixteen to eighty pairs of query and head: where one kernel takes over from the other, which is by the pages' type)"""
+    cache = Cache([3000, 40, L], 3000, 2, 64, 16, codes).fill(L)
+    size = nm.binding.load_library().nm_attention_paged_workspace_bytes(3 * L, 3, 8, 2, 64, L)
+    plain = check(cache, [L] * 3, 8, L)
+    assert torch.equal(plain, check(cache, [L] * 3, 8, L, workspace=torch.empty(size, dtype=torch.uint8, device="cuda")))
+    check(cache, [L, 1, 0], 8, L, max_q=L, window=300, sinks=5)
