@@ -494,10 +494,10 @@ __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int
     tiles_before += __builtin_amdgcn_readlane(u->tiles_upto, 63);
   }
 }
-constexpr int64_t kLeastShare = 2;  // steps that a block takes at least
+// Steps that a block takes.
 __device__ __forceinline__ int64_t few_share(int64_t all, int blocks) {
   const int64_t even = (all + blocks - 1) / blocks;
-  return even < kLeastShare ? kLeastShare : even;
+  return even > 0 ? even : 1;
 }
 
 template <int DP, bool CODES, bool WHOLE>
@@ -971,8 +971,14 @@ __global__ void __launch_bounds__(kThreads) paged_chunk_join_kernel(const PagedA
 constexpr int64_t kFewColumns = 32, kFewColumnsCodes = 64;
 constexpr int64_t kFewSequences = 512;         // up to which lists are made
 constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences, likewise
-constexpr int64_t kFewBlocks = 512;            // blocks that the list is dealt to: two of each compute unit
-constexpr int64_t kUncutKeys = 4 * kStep;      // most keys of a call whose units are left whole
+// Blocks that the list is dealt to: two of each compute unit (24 ragged caches of up to 16384: 55.6 us; 71.4 with 256, 64.2 with 768, which come
+// in two rounds).
+constexpr int64_t kFewBlocks = 512;
+// Most keys of a call whose units are left whole, and for each unit of the call: dealing costs a launch, and each unit that a block goes on to a
+// look-up and a join of waves that nothing hides; whole units leave blocks idle (one sequence, 12 heads of 64, 400 keys: 9.4 us whole, 12.4 dealt, 1000: 14.2 and
+// 10.9; ragged ones, 32 heads on 8 of 128, 192 units up to 500: 12.9 and 14.3, 1000: 21.4 and 14.5; 512 units, 1000: 22.9 and 24.0; 800, 1000: 29.5 and
+// 33.8, 2000: 53.5 and 50.1; 1600, 2000: 82 and 95, 4000: 142 and 142; 3200, 2000: 141 and 207).
+constexpr int64_t kUncutKeys = 4 * kStep, kUncutKeysOfUnit = 2;
 struct PagedPlan {
   bool few, listed;
   int cuts, piece, teams;
@@ -1027,7 +1033,8 @@ PagedPlan paged_plan(bool codes, int64_t Tq, int B, int Hq, int Hkv, int D, int6
     const int64_t tiles = B + Tq * group / kCols;  // at most
     p.cuts = B <= kFewSequences && tiles <= kFewTiles;
     p.most_columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
-    if (paged_most_views(max_q, max_k, window, sinks) <= kUncutKeys) p.cuts = 0;
+    const int64_t views = paged_most_views(max_q, max_k, window, sinks);
+    if (views <= kUncutKeys || views <= kUncutKeysOfUnit * units * p.n_tiles) p.cuts = 0;
     p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
     p.columns = p.cuts ? p.most_columns : 0;
   } else {

@@ -45,3 +45,12 @@ def test_one_size_of_workspace_for_both_types(L, codes):
     plain = check(cache, [L] * 3, 8, L)
     assert torch.equal(plain, check(cache, [L] * 3, 8, L, workspace=torch.empty(size, dtype=torch.uint8, device="cuda")))
     check(cache, [L, 1, 0], 8, L, max_q=L, window=300, sinks=5)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_units_left_whole_where_they_are_many(codes):
+    lens = [(37 * i) % 700 for i in range(300)]
+    cache = Cache(lens, 700, 1, 32, 16, codes).fill(6)
+    counts = [min(n, 1 + i % 2) for i, n in enumerate(lens)]
+    for max_k in (600, 601, 700):  # (both sides of two keys for each unit, whatever the lengths are)
+        check(cache, counts, 2, max_q=2, max_k=max_k)
