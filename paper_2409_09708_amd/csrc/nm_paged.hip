@@ -41,6 +41,7 @@ struct PagedArgs {
   float* part_o;     // few: [slot][16][DP]; chunk: [query][head][cut][DP]
   float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
   FewShared* shared; // few: [block]
+  int lead;          // few: steps that a unit counts for before those of its keys, 0 or 1
   int slots;         // few: that the workspace holds
   bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
 };
@@ -435,7 +436,7 @@ __device__ __forceinline__ void few_units(const PagedArgs& a, int b0, Units* u) 
   if (b < a.c.p.B) {
     u->of = lane_sequence(a.c, b);
     const int steps = (few_views(a.c, u->of).count + kStep - 1) / kStep;
-    u->steps = steps > 0 ? steps : 1;
+    u->steps = (steps > 0 ? steps : 1) + a.lead;
     u->tiles = (u->of.len * a.group + kCols - 1) / kCols;
   }
   u->upto = (int64_t)u->steps * u->tiles;
@@ -555,13 +556,14 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       of = paged_sequence(c, seq);
     }
     const Views views = few_views(c, of);
-    const int last_view = a.cuts && (step + steps) * kStep < views.count ? (step + steps) * kStep : views.count;
+    const int first_step = step > a.lead ? step - a.lead : 0, end_step = step + steps > a.lead ? step + steps - a.lead : 0;
+    const int last_view = a.cuts && end_step * kStep < views.count ? end_step * kStep : views.count;
     Load load;
     load.begin(c, seq, kv_head, views);
     const int columns = of.len * a.group;
     // (a sequence of more queries than the grid was made for has further tiles)
     for (; tile * kCols < columns; tile += a.n_tiles) {
-      int v0 = step * kStep + wave * kRun;
+      int v0 = first_step * kStep + wave * kRun;
       load.look_up(a, v0, lane);
       const int n = tile * kCols + col;
       const bool live = n < columns;
@@ -974,14 +976,18 @@ constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences,
 // Blocks that the list is dealt to: two of each compute unit (24 ragged caches of up to 16384: 55.6 us; 71.4 with 256, 64.2 with 768, which come
 // in two rounds).
 constexpr int64_t kFewBlocks = 512;
-// Most keys of a call whose units are left whole, and for each unit of the call: dealing costs a launch, and each unit that a block goes on to a
-// look-up and a join of waves that nothing hides; whole units leave blocks idle (one sequence, 12 heads of 64, 400 keys: 9.4 us whole, 12.4 dealt, 1000: 14.2 and
-// 10.9; ragged ones, 32 heads on 8 of 128, 192 units up to 500: 12.9 and 14.3, 1000: 21.4 and 14.5; 512 units, 1000: 22.9 and 24.0; 800, 1000: 29.5 and
-// 33.8, 2000: 53.5 and 50.1; 1600, 2000: 82 and 95, 4000: 142 and 142; 3200, 2000: 141 and 207).
-constexpr int64_t kUncutKeys = 4 * kStep, kUncutKeysOfUnit = 2;
+// Most keys of a call whose units are left whole, and for every four units of the call: dealing costs a launch, and each unit that a block goes
+// on to a look-up and a join of waves that nothing hides; whole units leave blocks idle (whole and dealt; one sequence, 12 heads of 64, 400 keys:
+// 9.4 and 12.4 us, 1000: 14.2 and 10.8; ragged ones, 32 heads on 8 of 128, 8 bits, 192 units up to 500: 12.9 and 14.3, 1000: 20.9 and 14.4; 512 units, 1000: 22.9 and
+// 22.1; 800, 1000: 29.6 and 32.3, 2000: 53 and 42; 1600, 2000: 82 and 81, 4000: 143 and 119; 3200, 2000: 142 and 172, 4000: 246 and 260).
+constexpr int64_t kUncutKeys = 4 * kStep, kUncutKeysOfUnits = 5;
+// Steps to each block, if all units were as long as the longest, from which on a unit's begin and end count for a step: a block that goes on to
+// another unit takes fewer then, and ends with the others (24 ragged caches of up to 16384: 55.8 and 51.5 us, 64 of 4000 44 and 37, 100 of 2000 51 and 42;
+// with two 53, 40 and 42; where blocks have a step or two it costs one: 24 of 1000 15.7 and 16.5).
+constexpr int64_t kLeadSteps = 4;
 struct PagedPlan {
   bool few, listed;
-  int cuts, piece, teams;
+  int cuts, piece, teams, lead;
   int64_t n_tiles, blocks;
   size_t columns, most_columns;  // of DP sums, in the workspace; of any max_k, window and sinks
 };
@@ -1034,7 +1040,8 @@ PagedPlan paged_plan(bool codes, int64_t Tq, int B, int Hq, int Hkv, int D, int6
     p.cuts = B <= kFewSequences && tiles <= kFewTiles;
     p.most_columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
     const int64_t views = paged_most_views(max_q, max_k, window, sinks);
-    if (views <= kUncutKeys || views <= kUncutKeysOfUnit * units * p.n_tiles) p.cuts = 0;
+    if (views <= kUncutKeys || 4 * views <= kUncutKeysOfUnits * units * p.n_tiles) p.cuts = 0;
+    p.lead = p.cuts && (views + kStep - 1) / kStep * units * p.n_tiles >= kLeadSteps * kFewBlocks;
     p.blocks = p.cuts ? kFewBlocks : units * p.n_tiles < kMostBlocks ? units * p.n_tiles : kMostBlocks - 1;
     p.columns = p.cuts ? p.most_columns : 0;
   } else {
@@ -1083,6 +1090,7 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   a.cuts = plan.cuts;
   a.piece = plan.piece;
   a.listed = plan.listed;
+  a.lead = plan.lead;
   a.slots = (int)(plan.columns / kCols);
   a.whole_o = whole_rows(c.O);
   if (plan.columns) {

@@ -49,8 +49,8 @@ def test_one_size_of_workspace_for_both_types(L, codes):
 
 @pytest.mark.parametrize("codes", [False, True])
 def test_units_left_whole_where_they_are_many(codes):
-    lens = [(37 * i) % 700 for i in range(300)]
+    lens = [(37 * i) % 700 for i in range(500)]
     cache = Cache(lens, 700, 1, 32, 16, codes).fill(6)
     counts = [min(n, 1 + i % 2) for i, n in enumerate(lens)]
-    for max_k in (600, 601, 700):  # (both sides of two keys for each unit, whatever the lengths are)
+    for max_k in (624, 626, 700):  # (both sides of five keys for four units, whatever the lengths are)
         check(cache, counts, 2, max_q=2, max_k=max_k)
