@@ -724,14 +724,13 @@ int32_t nm_cache_read(const nm_pages* pages, const nm_heads* K, const nm_heads* 
  *   max_q, max_k  the longest lengths, as far as the caller knows: the launch is shaped for them.  Longer ones are computed too
  *   lse        out float [heads_q, Tq], or NULL
  *   workspace  scratch of nm_attention_paged_workspace_bytes() bytes, 256-byte aligned; it does for any max_k, window and sinks.  NULL
- *              allowed where keys are few (max_k up to 512, or that size is 0).  Contents undefined afterwards; concurrent calls need
+ *              allowed where that size is 0, or max_k is up to 512 and max_q * heads_q / heads up to 32.  Contents undefined afterwards; concurrent calls need
  *              distinct workspaces.
  * Arithmetic as nm_attention's; 8-bit keys and values enter as the exact bfloat16 numbers that they stand for.  Keys that no query of its
  * sequence sees -- behind the end, between sinks and window, on pages that are not there -- are not read, whatever they hold; what one query
  * of a sequence sees and another does not is multiplied by zero for that one, so it has to be finite.
  * Errors: those of nm_attention and of the pages, Tq * heads_q above 2^30, window or sinks negative (NM_ERR_SHAPE).
- * Pages of heads of 32, 64 or 128 elements whose rows are 16-byte aligned are fastest; the heads of a page one after another (strides
- * page > head > token) a little more so.
+ * Pages of heads of 32, 64 or 128 elements whose rows are 16-byte aligned are fastest.
  */
 typedef struct nm_paged_desc {
   nm_pages pages;

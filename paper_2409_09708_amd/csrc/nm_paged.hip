@@ -14,6 +14,11 @@
 // the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
 // paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves, or for each of two such teams; keys cut where there are
 // few blocks.
+//
+// The first is bound by memory: 24 caches of up to 16384 tokens in 8 bits, 32 heads on 8 of 128, 49.4 us with the join's 5 (3.5 TB/s; caches of one
+// length 169 us, 4.8 TB/s): what is left is the latency of a block's first look-ups and of its last unit's end.  The second by the matrix cores and the
+// vector work beside them: chunks of 2047 and 1080 tokens on caches of 16384, 16 heads on 4 of 128: 318 us, 860 TFLOP/s; under windows of 1024, five
+// chunks in 8 bits, 37.6 us: ten steps of 2.2 us, and as much to begin and end.
 #include "nm_attention.h"
 #include "nm_pages.h"
 
@@ -569,7 +574,8 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       const bool live = n < columns;
       const int qi = n / a.group, head = kv_head * a.group + n % a.group;
       const int first = of.n - of.len, p = first + qi;  // positions
-      const int least_p = first + tile * kCols / a.group, most_p = first + (tile * kCols + kCols - 1 < columns ? tile * kCols + kCols - 1 : columns - 1) / a.group;
+      const int last_column = tile * kCols + kCols - 1 < columns ? tile * kCols + kCols - 1 : columns - 1;
+      const int least_p = first + tile * kCols / a.group, most_p = first + last_column / a.group;
       const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
       u32x4_t q[STEPS];
 #pragma unroll
@@ -978,8 +984,9 @@ constexpr int64_t kFewTiles = 4096;            // column tiles of all sequences,
 constexpr int64_t kFewBlocks = 512;
 // Most keys of a call whose units are left whole, and for every four units of the call: dealing costs a launch, and each unit that a block goes
 // on to a look-up and a join of waves that nothing hides; whole units leave blocks idle (whole and dealt; one sequence, 12 heads of 64, 400 keys:
-// 9.4 and 12.4 us, 1000: 14.2 and 10.8; ragged ones, 32 heads on 8 of 128, 8 bits, 192 units up to 500: 12.9 and 14.3, 1000: 20.9 and 14.4; 512 units, 1000: 22.9 and
-// 22.1; 800, 1000: 29.6 and 32.3, 2000: 53 and 42; 1600, 2000: 82 and 81, 4000: 143 and 119; 3200, 2000: 142 and 172, 4000: 246 and 260).
+// 9.4 and 12.4 us, 1000: 14.2 and 10.8; ragged ones, 32 heads on 8 of 128, 8 bits, 192 units up to 500: 12.9 and 14.3, 1000: 20.9 and 14.4;
+// 512 units, 1000: 22.9 and 22.1; 800, 1000: 29.6 and 32.3, 2000: 53 and 42; 1600, 2000: 82 and 81, 4000: 143 and 119; 3200, 2000: 142 and
+// 172, 4000: 246 and 260).
 constexpr int64_t kUncutKeys = 4 * kStep, kUncutKeysOfUnits = 5;
 // Steps to each block, if all units were as long as the longest, from which on a unit's begin and end count for a step: a block that goes on to
 // another unit takes fewer then, and ends with the others (24 ragged caches of up to 16384: 55.8 and 51.5 us, 64 of 4000 44 and 37, 100 of 2000 51 and 42;
@@ -1126,7 +1133,8 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
         if (a.cuts > 1) {
           // (two rows to a group of lanes)
           const int64_t blocks = (c.max_q * c.Hq * (DP / 4) + 2 * kThreads - 1) / (2 * kThreads);
-          paged_chunk_join_kernel<DP><<<dim3((unsigned)(blocks < 1 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks - 1), (unsigned)c.p.B), kThreads, 0, s>>>(a);
+          const dim3 join((unsigned)(blocks < 1 ? 1 : blocks < kMostBlocks ? blocks : kMostBlocks - 1), (unsigned)c.p.B);
+          paged_chunk_join_kernel<DP><<<join, kThreads, 0, s>>>(a);
         }
       }
     };
