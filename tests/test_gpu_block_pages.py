@@ -220,3 +220,27 @@ def test_a_step_captured_and_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(captured, want)), t
         assert torch.equal(cache.lengths, eager.lengths)
+
+
+def test_head_norms_without_positions_and_with_a_cache_of_rows():
+    block, normal = normed(256, 8, 2, 512, 7, centred=True)
+    T = sum(LENS)
+    branch, stream = normal(T, 256).to(BF16), normal(T, 256).to(BF16)
+    positions = torch.zeros(T, 2, dtype=torch.int32, device="cuda")
+    want = definition(block, constants(block), branch.double(), stream.double(), LENS, positions)  # (no angle: no turn)
+    norm = block.norms[0]
+    want = torch.nn.functional.layer_norm(want[0] + want[1], (256,), norm[0].double(), norm[1].double(), block.eps)
+    block.freqs = None
+    of = Sequences(starts(LENS), max(LENS), positions)
+    out, saved = block.forward(branch, stream, of, train=True)
+    near(finish(*out, norm), want, FORWARD, "prompt")
+    for cache in (Cache, PagedCache):
+        near(run_in_pieces(block, cache.empty(3, 200, 2, 32), branch, stream, positions, LENS, PIECES), want, FORWARD, cache.__name__)
+    d_branch, d_stream = normal(T, 256).to(BF16), normal(T, 256).to(BF16)
+    (dx, _), grads = block.backward(d_branch, d_stream, saved)
+    W, b, norms, w = constants(block)
+    x, w = branch.double().requires_grad_(), w.requires_grad_()
+    block.freqs = torch.zeros(block.size // 2, device="cuda")
+    torch.autograd.backward(definition(block, (W, b, norms, w), x, stream.double(), LENS, positions), (d_branch.double(), d_stream.double()))
+    near(dx, x.grad, BACKWARD, "dx")
+    near(grads["head_norms"], w.grad, BACKWARD, "head_norms")
