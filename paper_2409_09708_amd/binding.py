@@ -88,6 +88,20 @@ class ForwardDesc(ctypes.Structure):
                 ("workspace_bytes", c_size_t)]
 
 
+def _held(value: int, kind) -> int:
+    """The whole number nearest to value that an integer type of ctypes holds: too large stays too large, where ctypes drops the upper bits."""
+    most = (1 << (8 * ctypes.sizeof(kind) - 1)) - 1
+    return min(max(value, -most - 1), most)
+
+
+class _Desc(ctypes.Structure):
+    """A descriptor whose fields take a caller's whole numbers, of any size, by _held."""
+
+    def __setattr__(self, name, value):
+        kind = dict(self._fields_).get(name)
+        super().__setattr__(name, _held(value, kind) if kind in (c_int32, c_int64) else value)
+
+
 class Heads(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("token", c_int64), ("head", c_int64)]
 
@@ -104,7 +118,7 @@ class TypedHeads(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("token", c_int64), ("head", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
 
 
-class HeadNormDesc(ctypes.Structure):
+class HeadNormDesc(_Desc):
     _fields_ = [("X", TypedHeads), ("Y", TypedHeads), ("dY", TypedHeads), ("weight", c_void_p), ("dweight", c_void_p),
                 ("positions", c_void_p), ("freqs", c_void_p), ("sections", c_void_p),
                 ("T", c_int64), ("H", c_int64), ("heads", c_int64), ("D", c_int64), ("rotated", c_int64),
@@ -112,7 +126,7 @@ class HeadNormDesc(ctypes.Structure):
                 ("eps", ctypes.c_float), ("reserved", c_int32)]
 
 
-class Pages(ctypes.Structure):
+class Pages(_Desc):
     _fields_ = [("K", c_void_p), ("V", c_void_p), ("K_scales", c_void_p), ("V_scales", c_void_p),
                 ("page", c_int64), ("token", c_int64), ("head", c_int64),
                 ("scale_page", c_int64), ("scale_token", c_int64), ("scale_head", c_int64),
@@ -121,7 +135,7 @@ class Pages(ctypes.Structure):
                 ("head_size", c_int32), ("dtype", c_int32)]
 
 
-class PagedDesc(ctypes.Structure):
+class PagedDesc(_Desc):
     _fields_ = [("pages", Pages), ("Q", Heads), ("O", Heads), ("lse", c_void_p), ("offsets_q", c_void_p),
                 ("Tq", c_int64), ("max_q", c_int64), ("max_k", c_int64),
                 ("heads_q", c_int32), ("window", c_int32), ("sinks", c_int32), ("scale", ctypes.c_float)]
@@ -483,7 +497,7 @@ def _doubles(xs):
 
 
 def _ints(xs):
-    return (c_int32 * len(xs))(*[int(x) for x in xs])
+    return (c_int32 * len(xs))(*[_held(int(x), c_int32) for x in xs])
 
 
 def nm_config_cost(layer_macs, levels, fixed_cost: float = 0.0) -> float:
