@@ -681,7 +681,8 @@ int32_t nm_head_norm_backward(const nm_head_norm_desc* desc, void* workspace, si
  *   K_scales, V_scales  [pages, page_size, heads] bytes with strides of their own (both the same); NM_E4M3 only
  *   table    int32 [sequences, table_width] contiguous.  An entry outside 0 .. pages - 1 is a page that is not there: it is not
  *            written, read back as zeros, and its keys are not seen.
- *   lengths  int32 [sequences]: tokens of each sequence, new ones counted.  (Above the table's room they are taken as the room.)
+ *   lengths  int32 [sequences]: tokens of each sequence, new ones counted (below 0: none).  Tokens behind the table's room, table_width *
+ *            page_size, are not there; those before it are where they would be otherwise, and new tokens stand where they would.
  *
  * nm_cache_write -- new tokens, packed one sequence after another, become the last ones of their sequences: token i of the n new ones
  *   of sequence b is its token lengths[b] - n + i.  One that falls outside the table, or on a page that is not there, is dropped.

@@ -73,7 +73,8 @@ class PagedCache(_Room):
     sequences grow, or takes them back, writes `table` itself (an entry below 0: no page).  window, sinks: a token sees the last `window`
     tokens and the first `sinks` of its sequence (window 0: all of them), so pages in between can be taken back.
 
-    Tokens that do not fit are refused as by `Cache`; where the host cannot know, what falls outside the table is dropped."""
+    Tokens that do not fit are refused as by `Cache`.  Where the host cannot know -- a replayed graph -- what falls outside the table is
+    dropped and the lengths count on: tokens see those before them that were kept."""
     K: object
     V: object
     K_scales: object

@@ -51,7 +51,8 @@ struct PagedArgs {
   bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
 };
 
-// Sequence b: its first packed query, how many there are, and its tokens.  Whatever the caller's numbers are, rows stay inside the tensors.
+// Sequence b: its first packed query, how many there are, and its tokens (also those behind the table's room: queries stand where their
+// tokens do).  Whatever the caller's numbers are, rows stay inside the tensors.
 struct PagedSequence {
   int q0, len, n;
 };
@@ -61,11 +62,11 @@ __device__ __forceinline__ PagedSequence paged_sequence(const PagedCall& c, int 
   int v = lane == 0 ? b * each : (b + 1) * each;
   if (lane == 2) v = c.p.lengths[b];
   else if (lane < 2 && c.offsets_q != nullptr) v = c.offsets_q[b + lane];
-  const int n = page_clamped(c.p, __builtin_amdgcn_readlane(v, 2));
+  const int n = __builtin_amdgcn_readlane(v, 2);
   int q0 = __builtin_amdgcn_readlane(v, 0), q1 = __builtin_amdgcn_readlane(v, 1);
   q0 = q0 < 0 ? 0 : q0 < c.Tq ? q0 : (int)c.Tq;
   q1 = q1 < q0 ? q0 : q1 < c.Tq ? q1 : (int)c.Tq;
-  return {q0, q1 - q0, n};
+  return {q0, q1 - q0, n < 0 ? 0 : n};
 }
 
 // ... of a lane's own sequence
@@ -78,10 +79,12 @@ __device__ __forceinline__ PagedSequence lane_sequence(const PagedCall& c, int b
   }
   q0 = q0 < 0 ? 0 : q0 < Tq ? q0 : Tq;
   q1 = q1 < q0 ? q0 : q1 < Tq ? q1 : Tq;
-  return {q0, q1 - q0, page_clamped(c.p, c.p.lengths[b])};
+  const int n = c.p.lengths[b];
+  return {q0, q1 - q0, n < 0 ? 0 : n};
 }
 
-// The keys that queries at positions first .. last may see, numbered without the gap: view v is key v below `sinks`, else v + gap.
+// The keys that queries at positions first .. last may see, as far as the table has room for them (2^30 at most), numbered without the gap:
+// view v is key v below `sinks`, else v + gap.
 // ALIGN: both parts begin at multiples of it, which adds views that nobody sees.
 struct Views {
   int sinks, gap, count;
@@ -90,7 +93,7 @@ struct Views {
 };
 template <int ALIGN>
 __device__ __forceinline__ Views paged_views(const PagedCall& c, int first, int last) {
-  const int end = last + 1 > 0 ? last + 1 : 0;
+  const int room = c.p.width * c.p.page_size, end = last < 0 ? 0 : last < room ? last + 1 : room;
   int64_t lo = 0;
   if (c.window > 0) lo = (int64_t)first - c.window + 1;
   const int from = lo > 0 ? (int)(lo < end ? lo : end) : 0, sinks = c.sinks < from ? c.sinks : from;
@@ -573,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       const int n = tile * kCols + col;
       const bool live = n < columns;
       const int qi = n / a.group, head = kv_head * a.group + n % a.group;
-      const int first = of.n - of.len, p = first + qi;  // positions
+      const int first = of.n - of.len, p = first + (live ? qi : 0);  // positions
       const int last_column = tile * kCols + kCols - 1 < columns ? tile * kCols + kCols - 1 : columns - 1;
       const int least_p = first + tile * kCols / a.group, most_p = first + last_column / a.group;
       const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
@@ -813,7 +816,7 @@ __global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const P
     const int columns = of.len * a.group, first = of.n - of.len;  // (the first query's position)
     const int c_wave = tile * kChunkColumns + wave * 32, n = c_wave + (lane & 31);
     const bool live = n < columns;
-    const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + qi;
+    const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + (live ? qi : 0);
     const int least_p = chunk_position(of, a.group, c_wave), most_p = chunk_position(of, a.group, c_wave + 31);
     const Views views = chunk_views(a, of, tile);
     const int all = (views.count + kChunkKeys - 1) / kChunkKeys, pieces = chunk_pieces(a, all);

@@ -29,12 +29,6 @@ inline PageDivide page_divide(int d) {
 }
 __device__ __forceinline__ int page_of(PageDivide p, int j) { return p.shift < 0 ? j : (int)(__umulhi((uint32_t)j, p.by) >> p.shift); }
 
-// A sequence's tokens, as many as its table has room for (2^30 at most).
-__device__ __forceinline__ int page_clamped(const PagesCall& p, int length) {
-  const int room = p.width * p.page_size;
-  return length < 0 ? 0 : length < room ? length : room;
-}
-
 // Sixteen codes to eight pairs of bfloat16; `exponent` is the row's byte.
 __device__ __forceinline__ void decode16(u32x4_t codes, uint32_t exponent, u32x4_t (&out)[2]) {
   const float scale = __uint_as_float(exponent << 23);
