@@ -784,6 +784,7 @@ __device__ __forceinline__ bool chunk_place(const PagedArgs& a, int64_t at, int*
   return false;
 }
 
+constexpr int kNoTiles = 1 << 24;  // more than a sequence has (2^30 columns at most)
 // A block has one or two teams of four waves, 32 columns to a wave; two teams have the same columns and take the tiles of keys in turn.
 template <int DP, int HOW, int TEAMS>
 __global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const PagedArgs a) {
@@ -798,7 +799,8 @@ __global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const P
   const int team = TEAMS == 1 ? 0 : (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
   // Consecutive blocks go to consecutive XCDs, each with an L2 of its own: key heads change fastest, so that an XCD has few of them.  Where
   // sequences are as long as each other, or too many to count their tiles, the last tiles of all of them come first, then those before them.
-  for (int64_t item = blockIdx.x;; item += gridDim.x) {
+  const int64_t items = (int64_t)a.n_tiles * c.p.B * c.p.H * a.cuts;
+  for (int64_t item = blockIdx.x; a.listed || item < items; item += gridDim.x) {
     const int kv_head = (int)(item % c.p.H), cut = (int)(item / c.p.H % a.cuts);
     const int64_t at = item / c.p.H / a.cuts;
     int seq, tile;
@@ -807,136 +809,137 @@ __global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const P
       if (!chunk_place(a, at, &seq, &tile, &of)) return;
     } else {
       seq = (int)(at % c.p.B);
-      tile = (int)(at / c.p.B);
-      if ((int64_t)tile * kChunkColumns >= c.Tq * a.group) return;
-      if (tile < a.n_tiles) tile = a.n_tiles - 1 - tile;  // (behind n_tiles: those of sequences that are longer than was said)
+      tile = a.n_tiles - 1 - (int)(at / c.p.B);
       of = paged_sequence(c, seq);
-      if (tile * kChunkColumns >= of.len * a.group) continue;
     }
     const int columns = of.len * a.group, first = of.n - of.len;  // (the first query's position)
-    const int c_wave = tile * kChunkColumns + wave * 32, n = c_wave + (lane & 31);
-    const bool live = n < columns;
-    const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + (live ? qi : 0);
-    const int least_p = chunk_position(of, a.group, c_wave), most_p = chunk_position(of, a.group, c_wave + 31);
-    const Views views = chunk_views(a, of, tile);
-    const int all = (views.count + kChunkKeys - 1) / kChunkKeys, pieces = chunk_pieces(a, all);
-    if (cut >= pieces) continue;
-    const int from = (int)((int64_t)all * cut / pieces), to = (int)((int64_t)all * (cut + 1) / pieces);
-    Load load;
-    load.begin(c, seq, kv_head, views);
-    load.smem = smem[team][0];
-    load.lds = NM_LDS_ADDRESS(smem[team][0]);
-    __syncthreads();  // (a block's second tile: what the first one had in LDS is no longer read)
-    load.look_up(a, (from + team) * kChunkKeys);
-    u32x4_t q[STEPS];
-    const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
+    // (Without a list, a sequence of more queries than the grid was made for has further tiles, for the blocks of its first ones.  Where each
+    // block went through the tiles of all sequences' queries for them, 600 chunks of 64, 8 heads on 2 of 64, caches of 200 took 2470 us for 56.)
+    for (const int step = a.listed ? kNoTiles : a.n_tiles; (int64_t)tile * kChunkColumns < columns; tile += step) {
+      const int c_wave = tile * kChunkColumns + wave * 32, n = c_wave + (lane & 31);
+      const bool live = n < columns;
+      const int qi = n / a.group, head = kv_head * a.group + n % a.group, p = first + (live ? qi : 0);
+      const int least_p = chunk_position(of, a.group, c_wave), most_p = chunk_position(of, a.group, c_wave + 31);
+      const Views views = chunk_views(a, of, tile);
+      const int all = (views.count + kChunkKeys - 1) / kChunkKeys, pieces = chunk_pieces(a, all);
+      if (cut >= pieces) continue;
+      const int from = (int)((int64_t)all * cut / pieces), to = (int)((int64_t)all * (cut + 1) / pieces);
+      Load load;
+      load.begin(c, seq, kv_head, views);
+      load.smem = smem[team][0];
+      load.lds = NM_LDS_ADDRESS(smem[team][0]);
+      __syncthreads();  // (a block's second tile: what the first one had in LDS is no longer read)
+      load.look_up(a, (from + team) * kChunkKeys);
+      u32x4_t q[STEPS];
+      const bf16_t* q_row = c.Q.p + (int64_t)(of.q0 + qi) * c.Q.token + head * c.Q.head;
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
-    if (from + team < to) load.fetch(a, 0);
-    load.look_up(a, (from + team + TEAMS) * kChunkKeys);
-    if constexpr (Load::DIRECT) arrived(q);
-    f32x16_t acc[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
-    float ref = kMinusInf, sum = 0.f;
-    int stage = 0;
-    for (int k0 = from; k0 < to; k0 += TEAMS, stage ^= 1) {
-      const int kt = k0 + team, v0 = kt * kChunkKeys;
-      if (TEAMS == 1 || kt < to) load.settle(stage);
-      const uint64_t seen = load.seen;
-      __syncthreads();
-      if (kt + TEAMS < to) {
-        load.fetch(a, stage ^ 1);
-        load.look_up(a, v0 + 2 * TEAMS * kChunkKeys);
-      }
-      // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
-      const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
-      if ((TEAMS > 1 && kt >= to) || c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= least_p - c.window && k_first >= c.sinks))
-        continue;
-      const uint32_t k_tile = load.lds + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
-      const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
-      constexpr int KB = kChunkKeys / 32, NS = KB * STEPS, NV = kChunkKeys / 16 * NB;
-      // (products on the same sums wait for each other: the two runs of keys in turn)
-      auto keys = [&](int i) { return Tile::rows(k_at, i % KB * 32, i / KB); };
-      auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
-      f32x16_t s[KB];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-      u32x4_t f[kAhead];
-      read_ahead<NS>(f, keys);
-      products<NS>(f, keys, [&](int i, u32x4_t k) { s[i % KB] = mma32(k, q[i / KB], s[i % KB]); });
-      read_ahead<NV>(f, values);
-      if (seen != ~0ull || !seen_whole<kChunkKeys>(c, views, v0, least_p, most_p)) {
-        const Sight sight(c, p);
-        int key = k_first + 4 * half;  // (a tile lies on one side of the gap)
-        uint64_t there = seen >> (4 * half);
-        asm volatile("" : "+v"(key), "+v"(there));  // (or the sums with rows' constants would be held over the loop)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int row = 32 * kb + acc_row(r);
-            s[kb][r] = sight.sees(key + row) && (there >> row & 1) ? s[kb][r] : kMinusInf;
-          }
-      }
-      softmax_step(s, a.scale_log2, ref, sum, acc);
-      u32x4_t pr[kChunkKeys / 16];
-#pragma unroll
-      for (int st = 0; st < kChunkKeys / 16; ++st) pr[st] = acc_operand(s[st / 2], st % 2);
-      products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
-    }
-    sum = half_sum(sum);
-    if constexpr (TEAMS == 2) {  // the second team's sums to the first, which has the same columns in the same lanes
-      static_assert(kWaves * (NB * 16 + 2) * 64 * 4 <= (int)sizeof(smem), "in LDS that tiles have left");
-      f32x4_t* box = reinterpret_cast<f32x4_t*>(smem) + wave * NB * 4 * 64 + lane;
-      float2* ml = reinterpret_cast<float2*>(reinterpret_cast<f32x4_t*>(smem) + kWaves * NB * 4 * 64) + wave * 64 + lane;
-      __syncthreads();
-      if (team == 1) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) box[(b * 4 + r) * 64] = f32x4_t{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]};
-        *ml = float2{ref, sum};
-      }
-      __syncthreads();
-      if (team == 1) continue;
-      const float2 other = *ml;
-      const float top = fmaxf(ref, other.x), mine = part_weight(ref, top), its = part_weight(other.x, top);
-      ref = top;
-      sum = sum * mine + other.y * its;
+      for (int st = 0; st < STEPS; ++st) q[st] = load_piece(q_row, 16 * st + 8 * half, D, live);
+      if (from + team < to) load.fetch(a, 0);
+      load.look_up(a, (from + team + TEAMS) * kChunkKeys);
+      if constexpr (Load::DIRECT) arrived(q);
+      f32x16_t acc[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][r] = acc[b][r] * mine + box[(b * 4 + r / 4) * 64][r % 4] * its;
-    }
-    if (pieces > 1) {
-      if (live) {
-        const int64_t part = ((int64_t)(of.q0 + qi) * c.Hq + head) * a.cuts + cut;
+        for (int r = 0; r < 16; ++r) acc[b][r] = 0.f;
+      float ref = kMinusInf, sum = 0.f;
+      int stage = 0;
+      for (int k0 = from; k0 < to; k0 += TEAMS, stage ^= 1) {
+        const int kt = k0 + team, v0 = kt * kChunkKeys;
+        if (TEAMS == 1 || kt < to) load.settle(stage);
+        const uint64_t seen = load.seen;
+        __syncthreads();
+        if (kt + TEAMS < to) {
+          load.fetch(a, stage ^ 1);
+          load.look_up(a, v0 + 2 * TEAMS * kChunkKeys);
+        }
+        // (a wave whose queries are all before the tile, or past what their window holds of it, has nothing to do)
+        const int k_first = views.key(v0), k_last = views.key(v0 + kChunkKeys - 1);
+        if ((TEAMS > 1 && kt >= to) || c_wave >= columns || k_first > most_p || (c.window > 0 && k_last <= least_p - c.window && k_first >= c.sinks))
+          continue;
+        const uint32_t k_tile = load.lds + (uint32_t)stage * 2 * Load::kBytes, v_tile = k_tile + Load::kBytes;
+        const uint32_t k_at = k_tile + Tile::row_base(lane), v_at = v_tile + Tile::column_base(lane);
+        constexpr int KB = kChunkKeys / 32, NS = KB * STEPS, NV = kChunkKeys / 16 * NB;
+        // (products on the same sums wait for each other: the two runs of keys in turn)
+        auto keys = [&](int i) { return Tile::rows(k_at, i % KB * 32, i / KB); };
+        auto values = [&](int i) { return Tile::columns(v_at, i / NB * 16, i % NB); };
+        f32x16_t s[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+        u32x4_t f[kAhead];
+        read_ahead<NS>(f, keys);
+        products<NS>(f, keys, [&](int i, u32x4_t k) { s[i % KB] = mma32(k, q[i / KB], s[i % KB]); });
+        read_ahead<NV>(f, values);
+        if (seen != ~0ull || !seen_whole<kChunkKeys>(c, views, v0, least_p, most_p)) {
+          const Sight sight(c, p);
+          int key = k_first + 4 * half;  // (a tile lies on one side of the gap)
+          uint64_t there = seen >> (4 * half);
+          asm volatile("" : "+v"(key), "+v"(there));  // (or the sums with rows' constants would be held over the loop)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int row = 32 * kb + acc_row(r);
+              s[kb][r] = sight.sees(key + row) && (there >> row & 1) ? s[kb][r] : kMinusInf;
+            }
+        }
+        softmax_step(s, a.scale_log2, ref, sum, acc);
+        u32x4_t pr[kChunkKeys / 16];
+#pragma unroll
+        for (int st = 0; st < kChunkKeys / 16; ++st) pr[st] = acc_operand(s[st / 2], st % 2);
+        products<NV>(f, values, [&](int i, u32x4_t v) { acc[i % NB] = mma32(v, pr[i / NB], acc[i % NB]); });
+      }
+      sum = half_sum(sum);
+      if constexpr (TEAMS == 2) {  // the second team's sums to the first, which has the same columns in the same lanes
+        static_assert(kWaves * (NB * 16 + 2) * 64 * 4 <= (int)sizeof(smem), "in LDS that tiles have left");
+        f32x4_t* box = reinterpret_cast<f32x4_t*>(smem) + wave * NB * 4 * 64 + lane;
+        float2* ml = reinterpret_cast<float2*>(reinterpret_cast<f32x4_t*>(smem) + kWaves * NB * 4 * 64) + wave * 64 + lane;
+        __syncthreads();
+        if (team == 1) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) box[(b * 4 + r) * 64] = f32x4_t{acc[b][4 * r], acc[b][4 * r + 1], acc[b][4 * r + 2], acc[b][4 * r + 3]};
+          *ml = float2{ref, sum};
+        }
+        __syncthreads();
+        if (team == 1) continue;
+        const float2 other = *ml;
+        const float top = fmaxf(ref, other.x), mine = part_weight(ref, top), its = part_weight(other.x, top);
+        ref = top;
+        sum = sum * mine + other.y * its;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<float4*>(a.part_o + part * DP + 32 * b + acc_row(r) + 4 * half) =
-                float4{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
-        if (half == 0) a.part_ml[part] = float2{ref, sum};
+          for (int r = 0; r < 16; ++r) acc[b][r] = acc[b][r] * mine + box[(b * 4 + r / 4) * 64][r % 4] * its;
       }
-      continue;
+      if (pieces > 1) {
+        if (live) {
+          const int64_t part = ((int64_t)(of.q0 + qi) * c.Hq + head) * a.cuts + cut;
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+              *reinterpret_cast<float4*>(a.part_o + part * DP + 32 * b + acc_row(r) + 4 * half) =
+                  float4{acc[b][r], acc[b][r + 1], acc[b][r + 2], acc[b][r + 3]};
+          if (half == 0) a.part_ml[part] = float2{ref, sum};
+        }
+        continue;
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      auto o_row = [&](int column) {
+        return c.O.p + (int64_t)(of.q0 + column / a.group) * c.O.token + (kv_head * a.group + column % a.group) * c.O.head;
+      };
+      if (WHOLE && a.whole_o) {
+        WaveRows<DP>::store([&](int r) { return o_row(c_wave + r); }, columns - c_wave, acc, lane, inv);
+      } else if (live) {
+        store_column<DP>(o_row(n), acc, lane, D, inv);
+      }
+      if (live && c.lse != nullptr && half == 0)
+        c.lse[(int64_t)head * c.Tq + of.q0 + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    auto o_row = [&](int column) {
-      return c.O.p + (int64_t)(of.q0 + column / a.group) * c.O.token + (kv_head * a.group + column % a.group) * c.O.head;
-    };
-    if (WHOLE && a.whole_o) {
-      WaveRows<DP>::store([&](int r) { return o_row(c_wave + r); }, columns - c_wave, acc, lane, inv);
-    } else if (live) {
-      store_column<DP>(o_row(n), acc, lane, D, inv);
-    }
-    if (live && c.lse != nullptr && half == 0)
-      c.lse[(int64_t)head * c.Tq + of.q0 + qi] = sum == 0.f ? kMinusInf : (ref + log2f(sum)) * kLn2;
   }
 }
 
