@@ -29,10 +29,12 @@ namespace {
 // What a block of the first launch leaves for the second: the unit that begins in it and goes on in the blocks after it.
 struct FewShared {
   int parts;  // blocks that share it; 0: there is none
-  int slot;   // of the first part
   int q0, columns, tile, kv_head;
-  int unused[2];
+  int unused[3];
 };
+// Where part k of the unit that begins in a block lies: a block has at most two parts of units that others share, one that it goes on with and
+// one that it leaves for others.
+__device__ __forceinline__ int few_slot(int block, int k) { return 2 * (block + k) + (k == 0 ? 1 : 0); }
 
 struct PagedArgs {
   PagedCall c;
@@ -47,7 +49,6 @@ struct PagedArgs {
   float2* part_ml;   // likewise: (maximum of the scaled scores in the exponent's base 2, sum)
   FewShared* shared; // few: [block]
   int lead;          // few: steps that a unit counts for before those of its keys, 0 or 1
-  int slots;         // few: that the workspace holds
   bool whole_o;      // chunk: rows of the output are stored 16 bytes at a time
 };
 
@@ -432,7 +433,6 @@ struct Units {
   PagedSequence of;
   int steps, tiles;
   int64_t upto;       // steps of all tiles, up to the lane's sequence and with it
-  int tiles_upto;
 };
 __device__ __forceinline__ Views few_views(const PagedCall& c, const PagedSequence& of) {
   return paged_views<1>(c, of.n - of.len, of.n - 1);
@@ -448,40 +448,33 @@ __device__ __forceinline__ void few_units(const PagedArgs& a, int b0, Units* u) 
     u->tiles = (u->of.len * a.group + kCols - 1) / kCols;
   }
   u->upto = (int64_t)u->steps * u->tiles;
-  u->tiles_upto = u->tiles;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const int lo = __shfl_up((int)(uint32_t)u->upto, m, 64), hi = __shfl_up((int)(u->upto >> 32), m, 64), t = __shfl_up(u->tiles_upto, m, 64);
-    if (lane >= m) {
-      u->upto += (int64_t)hi << 32 | (uint32_t)lo;
-      u->tiles_upto += t;
-    }
+    const int lo = __shfl_up((int)(uint32_t)u->upto, m, 64), hi = __shfl_up((int)(u->upto >> 32), m, 64);
+    if (lane >= m) u->upto += (int64_t)hi << 32 | (uint32_t)lo;
   }
 }
 __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
   return (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
 
-// Steps and tiles of all sequences, for one key head; `u` is left at the first 64.
-__device__ __forceinline__ void few_totals(const PagedArgs& a, Units* u, int64_t* steps, int* tiles) {
-  *steps = 0;
-  *tiles = 0;
+// Steps of all sequences, for one key head; `u` is left at the first 64.
+__device__ __forceinline__ int64_t few_total(const PagedArgs& a, Units* u) {
+  int64_t steps = 0;
   for (int b0 = (a.c.p.B - 1) / 64 * 64; b0 >= 0; b0 -= 64) {
     few_units(a, b0, u);
-    *steps += lane_value(u->upto, 63);
-    *tiles += __builtin_amdgcn_readlane(u->tiles_upto, 63);
+    steps += lane_value(u->upto, 63);
   }
+  return steps;
 }
 
 // Where step `at` of a key head's list lies.
 struct UnitPlace {
   int seq, tile, step, steps;  // a tile of `steps` steps, `step` of which are before this one
-  int unit;                    // tiles before it
   PagedSequence of;
 };
 __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int64_t at) {
   int64_t steps_before = 0;
-  int tiles_before = 0;
   for (int b0 = 0;; b0 += 64) {
     if (u->b0 != b0) few_units(a, b0, u);
     const int64_t all = lane_value(u->upto, 63);
@@ -496,11 +489,9 @@ __device__ __forceinline__ UnitPlace few_place(const PagedArgs& a, Units* u, int
       const int64_t first = steps_before + lane_value(u->upto, l) - (int64_t)p.steps * tiles;
       p.tile = tiles == 1 ? 0 : (int)((at - first) / p.steps);
       p.step = (int)(at - first - (int64_t)p.tile * p.steps);
-      p.unit = tiles_before + __builtin_amdgcn_readlane(u->tiles_upto, l) - tiles + p.tile;
       return p;
     }
     steps_before += all;
-    tiles_before += __builtin_amdgcn_readlane(u->tiles_upto, 63);
   }
 }
 // Steps that a block takes.
@@ -529,10 +520,9 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
   Units units;
   units.b0 = -1;
   int64_t at, end = 0, per_head = 0, share = 0;
-  int tiles_per_head = 0;
   FewShared left = {};
   if (a.cuts) {
-    few_totals(a, &units, &per_head, &tiles_per_head);
+    per_head = few_total(a, &units);
     share = few_share(per_head * c.p.H, (int)gridDim.x);
     at = blockIdx.x * share;
     end = at + share < per_head * c.p.H ? at + share : per_head * c.p.H;
@@ -550,10 +540,10 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
       seq = p.seq; tile = p.tile; step = p.step; of = p.of;
       steps = (int)(end - at < p.steps - step ? end - at : p.steps - step);
       alone = steps == p.steps;
-      slot = kv_head * tiles_per_head + p.unit + (int)blockIdx.x;  // (each further unit, and each further block, is one more)
+      slot = step == 0 ? few_slot(blockIdx.x, 0) : 2 * (int)blockIdx.x;  // (the latter: few_slot of an earlier block)
       if (!alone && step == 0) {
         const int to = (int)((uint64_t)(at + p.steps - 1) / (uint64_t)share);
-        left = {to - (int)blockIdx.x + 1, slot, of.q0, of.len * a.group, tile, kv_head, {}};
+        left = {to - (int)blockIdx.x + 1, of.q0, of.len * a.group, tile, kv_head, {}};
       }
       at += steps;
     } else {
@@ -677,13 +667,13 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
           for (int w = 0; w < kWaves; ++w) l += wave_ml[w][cc].y * part_weight(wave_ml[w][cc].x, t);
           const float inv = l == 0.f ? 0.f : 1.f / l;
           store4(c.O.p + tok * c.O.token + hd * c.O.head, d, D, pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-        } else if ((uint32_t)slot < (uint32_t)a.slots) {  // (always, of offsets that do not decrease)
+        } else {
           *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kCols + cc) * DP + d) = o;
         }
       }
       if (wave == 0 && quarter == 0 && live) {
         if (!alone) {
-          if ((uint32_t)slot < (uint32_t)a.slots) a.part_ml[(int64_t)slot * kCols + col] = float2{top, total};
+          a.part_ml[(int64_t)slot * kCols + col] = float2{top, total};
         } else if (c.lse != nullptr) {
           c.lse[(int64_t)head * c.Tq + of.q0 + qi] = total == 0.f ? kMinusInf : (top + log2f(total)) * kLn2;
         }
@@ -694,25 +684,26 @@ __global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(const PagedArgs 
   if (a.cuts && tid == 0) a.shared[blockIdx.x] = left;
 }
 
-// One column's parts, `stride` columns of DP elements apart, joined in order by a wave: DP / 4 lanes take four elements each of every
+// A column's parts of the unit that began in a block, joined in order by a wave: DP / 4 lanes take four elements each of every
 // (256 / DP)-th part, so that several parts' loads are under way.
 template <int DP>
-__device__ __forceinline__ void join_parts(const PagedCall& c, const float* part_o, const float2* part_ml, int64_t stride, int parts,
-                                           int64_t tok, int head) {
+__device__ __forceinline__ void join_parts(const PagedArgs& a, int block, int parts, int col, int64_t tok, int head) {
+  const PagedCall& c = a.c;
+  auto at = [&](int k) { return (int64_t)few_slot(block, k) * kCols + col; };
   constexpr int LANES = DP / 4, GROUPS = 64 / LANES;
   const int lane = threadIdx.x & 63, part = lane / LANES, d = lane % LANES * 4;
   float top = kMinusInf;
-  for (int k = lane; k < parts; k += 64) top = fmaxf(top, part_ml[k * stride].x);
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, a.part_ml[at(k)].x);
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
   float total = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int k = part; k < parts; k += GROUPS) {
-    const float2 ml = part_ml[k * stride];
+    const float2 ml = a.part_ml[at(k)];
     const float by = part_weight(ml.x, top);
     total = fmaf(ml.y, by, total);
-    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(part_o + k * stride * DP + d);
+    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.part_o + at(k) * DP + d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = d + e < c.p.D ? fmaf(x[e], by, o[e]) : 0.f;
   }
@@ -732,11 +723,10 @@ __device__ __forceinline__ void join_parts(const PagedCall& c, const float* part
 template <int DP>
 __global__ void __launch_bounds__(kThreads) paged_few_join_kernel(const PagedArgs a) {
   const FewShared u = a.shared[blockIdx.x];
-  if (u.parts <= 0 || (uint32_t)u.slot >= (uint32_t)a.slots || u.parts > a.slots - u.slot) return;
+  if (u.parts <= 0 || u.parts > (int)(gridDim.x - blockIdx.x)) return;
   for (int col = blockIdx.y * kWaves + (threadIdx.x >> 6); col < kCols && u.tile * kCols + col < u.columns; col += gridDim.y * kWaves) {
     const int n = u.tile * kCols + col;
-    const int64_t at = (int64_t)u.slot * kCols + col;
-    join_parts<DP>(a.c, a.part_o + at * DP, a.part_ml + at, kCols, u.parts, u.q0 + n / a.group, u.kv_head * a.group + n % a.group);
+    join_parts<DP>(a, blockIdx.x, u.parts, col, u.q0 + n / a.group, u.kv_head * a.group + n % a.group);
   }
 }
 
@@ -1051,7 +1041,7 @@ PagedPlan paged_plan(bool codes, int64_t Tq, int B, int Hq, int Hkv, int D, int6
   if (p.few) {
     const int64_t tiles = B + Tq * group / kCols;  // at most
     p.cuts = B <= kFewSequences && tiles <= kFewTiles;
-    p.most_columns = p.cuts ? (size_t)(tiles * Hkv + kFewBlocks) * kCols : 0;
+    p.most_columns = p.cuts ? (size_t)(2 * kFewBlocks * kCols) : 0;  // (few_slot)
     const int64_t views = paged_most_views(max_q, max_k, window, sinks);
     if (views <= kUncutKeys || 4 * views <= kUncutKeysOfUnits * units * p.n_tiles) p.cuts = 0;
     p.lead = p.cuts && (views + kStep - 1) / kStep * units * p.n_tiles >= kLeadSteps * kFewBlocks;
@@ -1104,7 +1094,6 @@ hipError_t launch_paged(const PagedCall& c, hipStream_t s) {
   a.piece = plan.piece;
   a.listed = plan.listed;
   a.lead = plan.lead;
-  a.slots = (int)(plan.columns / kCols);
   a.whole_o = whole_rows(c.O);
   if (plan.columns) {
     a.part_o = static_cast<float*>(c.workspace);
