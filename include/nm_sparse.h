@@ -727,7 +727,8 @@ int32_t nm_cache_read(const nm_pages* pages, const nm_heads* K, const nm_heads* 
  *   workspace  scratch of nm_attention_paged_workspace_bytes() bytes, 256-byte aligned; it does for any max_k, window and sinks.  NULL
  *              allowed where that size is 0, or max_k is up to 512 and max_q * heads_q / heads up to 32.  Contents undefined afterwards; concurrent calls need
  *              distinct workspaces.
- * Arithmetic as nm_attention's; 8-bit keys and values enter as the exact bfloat16 numbers that they stand for.  Keys that no query of its
+ * Arithmetic as nm_attention's, but that exp(s_j - ..) is rounded to the sum of two bfloat16 where max_q * heads_q / heads is up to 32 (64 of
+ * NM_E4M3), to one above; 8-bit keys and values enter as the exact bfloat16 numbers that they stand for.  Keys that no query of its
  * sequence sees -- behind the end, between sinks and window, on pages that are not there -- are not read, whatever they hold; what one query
  * of a sequence sees and another does not is multiplied by zero for that one, so it has to be finite.
  * Errors: those of nm_attention and of the pages, Tq * heads_q above 2^30, window or sinks negative (NM_ERR_SHAPE).

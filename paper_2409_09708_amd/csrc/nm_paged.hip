@@ -876,6 +876,8 @@ __global__ void __launch_bounds__(kThreads* TEAMS, 2) paged_chunk_kernel(const P
             }
         }
         softmax_step(s, a.scale_log2, ref, sum, acc);
+        // Probabilities go in as one bfloat16 each, unlike the few queries' above: the matrix instructions have no time to spare here.  (Relative
+        // error of the two chunks 0.0023, of which the output's own rounding is 0.0017; with two 0.0017 and 423 us for 327; windows 47 for 41.)
         u32x4_t pr[kChunkKeys / 16];
 #pragma unroll
         for (int st = 0; st < kChunkKeys / 16; ++st) pr[st] = acc_operand(s[st / 2], st % 2);
