@@ -677,10 +677,11 @@ int32_t nm_head_norm_backward(const nm_head_norm_desc* desc, void* workspace, si
  * memory is handed out a page at a time, in any order, and pages may be shared between sequences as long as none of them is written.
  *   K, V     [pages, page_size, heads, head_size], elements of a head contiguous, any strides in elements otherwise (both the same)
  *   dtype    NM_OUT_BF16: as they are.  NM_E4M3: 8-bit codes (four bits of exponent, three of mantissa, 448 the largest) times a
- *            power of two for each head of a token: the value is code * 2^(byte - 127), which bfloat16 holds exactly.
+ *            power of two for each head of a token: the value is code * 2^(byte - 127), which bfloat16 holds exactly (of bytes from
+ *            27 to 246, as nm_cache_write leaves them, or of codes that are zeros).
  *   K_scales, V_scales  [pages, page_size, heads] bytes with strides of their own (both the same); NM_E4M3 only
  *   table    int32 [sequences, table_width] contiguous.  An entry outside 0 .. pages - 1 is a page that is not there: it is not
- *            written, read back as zeros, and its keys are not seen.
+ *            written, is read back as zeros, and its keys are not seen.
  *   lengths  int32 [sequences]: tokens of each sequence, new ones counted (below 0: none).  Tokens behind the table's room, table_width *
  *            page_size, are not there; those before it are where they would be otherwise, and new tokens stand where they would.
  *
@@ -729,8 +730,9 @@ int32_t nm_cache_read(const nm_pages* pages, const nm_heads* K, const nm_heads* 
  *              distinct workspaces.
  * Arithmetic as nm_attention's, but that exp(s_j - ..) is rounded to the sum of two bfloat16 where max_q * heads_q / heads is up to 32 (64 of
  * NM_E4M3), to one above; 8-bit keys and values enter as the exact bfloat16 numbers that they stand for.  Keys that no query of its
- * sequence sees -- behind the end, between sinks and window, on pages that are not there -- are not read, whatever they hold; what one query
- * of a sequence sees and another does not is multiplied by zero for that one, so it has to be finite.
+ * sequence sees -- behind the end, between sinks and window, on pages that are not there -- have no effect, whatever they hold (their
+ * rows, and rows of page 0 for those of a page that is not there, may be fetched); what one query of a sequence sees and another does not
+ * is multiplied by zero for that one, so it has to be finite.
  * Errors: those of nm_attention and of the pages, Tq * heads_q above 2^30, window or sinks negative (NM_ERR_SHAPE).
  * Pages of heads of 32, 64 or 128 elements whose rows are 16-byte aligned are fastest.
  */

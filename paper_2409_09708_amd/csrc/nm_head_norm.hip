@@ -12,9 +12,10 @@
 // in 64 bits: a 32-bit product of position 65536 is off by up to 2^-9 of a radian, as much as a rounding to bfloat16.
 // Sums and statistics are 32-bit floats; the mean is corrected by the mean difference to it, as large offsets need.
 //
-// Bound by memory: 10 flops per element forward, 18 backward, for 4 to 12 bytes.  12608 tokens of 24 heads of 64, bfloat16, two axes: 15.9 us,
-// 4.9 TB/s, where a copy of 1 GiB has 5.5; gradients of 8191 x 40 x 128, bfloat16, 60.8 us and of 16399 x 10 x 80, float, 42.9, each with 5 for the
-// second launch; one token 3.2 and the host's side of a call.
+// Bound by memory: 10 flops per element forward, 18 backward, for 4 to 12 bytes.  12608 tokens of 24 heads of 64, bfloat16, two axes: 15.8 to 17.8 us
+// (by the card, and by how much of its 78 MB the last level of cache still has; under the profiler 16.8), 4.4 to 4.9 TB/s, where a copy of 1 GiB has
+// 5.5; gradients of 8191 x 40 x 128, bfloat16, 56.5 to 60.8 us and of 16399 x 10 x 80, float, 42.8, each with 5 for the second launch; one token 3.2
+// and the host's side of a call.
 #include "nm_device.h"
 #include "nm_launch.h"
 #include "nm_rows.h"

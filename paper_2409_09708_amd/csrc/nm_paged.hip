@@ -6,19 +6,20 @@
 //
 // Scores are computed transposed, as nm_attention.h has it; the columns are the (query, head of the group) pairs that share a key head, so
 // that all of them share the keys that are read.  The keys that any query of a run can see are numbered without the gap between sinks and
-// window ("views"), so tiles hold no keys that nobody sees, and what is masked, past the end or on a page that is not there is never read:
-// its value is a zero and its score minus infinity.  A lane looks up the page of one row of a tile, two tiles ahead of its use, and
-// 8-bit rows become bfloat16 on the way, exactly.
+// window ("views"), so tiles hold no keys that nobody sees but at their edges.  What is hidden from all, past the end or on a page that is not
+// there has no effect: its value is a zero and its score minus infinity.  (Copies straight to LDS bring such rows all the same, for a page that
+// is not there rows of page 0; loads through registers leave them out.)  A lane looks up the page of one row of a tile, two tiles ahead of its
+// use, and 8-bit rows become bfloat16 on the way, exactly.
 //
 // Two kernels.  paged_few_kernel: 16 columns, waves on different keys; all keys of all sequences and heads are one list that is dealt to
 // the blocks in equal runs, and what a block leaves of a unit that others share (output, maximum, sum) a second launch joins in order.
 // paged_chunk_kernel: 128 columns to a block, 64 keys at a time for its four waves, or for each of two such teams; keys cut where there are
 // few blocks.
 //
-// The first is bound by memory: 24 caches of up to 16384 tokens in 8 bits, 32 heads on 8 of 128, 49.4 us with the join's 5 (3.5 TB/s; caches of one
+// The first is bound by memory: 24 caches of up to 16384 tokens in 8 bits, 32 heads on 8 of 128, 49.5 us with the join's 5 (3.5 TB/s; caches of one
 // length 169 us, 4.8 TB/s): what is left is the latency of a block's first look-ups and of its last unit's end.  The second by the matrix cores and the
-// vector work beside them: chunks of 2047 and 1080 tokens on caches of 16384, 16 heads on 4 of 128: 318 us, 860 TFLOP/s; under windows of 1024, five
-// chunks in 8 bits, 37.6 us: ten steps of 2.2 us, and as much to begin and end.
+// vector work beside them: chunks of 2047 and 1080 tokens on caches of 16384, 16 heads on 4 of 128: 304 us, 900 TFLOP/s (8 bits 368); under windows of
+// 1024, five chunks in 8 bits, 36.6 us: ten steps of 2.6 us for each of two teams, and eleven to begin and end (windows of 512 to 2048: 29 to 59 us).
 #include "nm_attention.h"
 #include "nm_pages.h"
 

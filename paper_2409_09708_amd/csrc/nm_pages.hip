@@ -3,10 +3,11 @@
 //   e4m3: per head of a token e = the smallest with max |x| <= 448 2^e, code = x 2^-e to four significant bits (multiples of 2^-9
 //   near zero), nearest even;  read back: code 2^e.   bfloat16: as they are.
 //
-// Bound by memory: a row is read and written once (24 caches in 8 bits read back, 172 MB and 344: 107.8 us, 4.8 TB/s; prompts of 21 thousand tokens
-// written and read back: 36 + 25).  Eight elements to a lane, so that accesses in either type run along whole rows, and
-// four rows' loads under way (119 us with sixteen elements to a lane and a row at a time).  A block takes the keys or the values of a run of
-// tokens; which sequence each belongs to, and which page and slot, its first wave finds for all of them at once.
+// Bound by memory: a row is read and written once (24 caches in 8 bits read back, 172 MB and 344: 107.8 us, 4.8 TB/s, in bfloat16 140; prompts of 21
+// thousand tokens written and read back: 36 + 25, in bfloat16 45 + 31: a token's heads are written one after another, which are rows of as many
+// places where pages keep the heads apart, with a byte of its own for each).  Eight elements to a lane, so that accesses in either type run along
+// whole rows, and four rows' loads under way (119 us with sixteen elements to a lane and a row at a time).  A block takes the keys or the values
+// of a run of tokens; which sequence each belongs to, and which page and slot, its first wave finds for all of them at once.
 #include "nm_pages.h"
 
 #include <type_traits>
